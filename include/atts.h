@@ -52,6 +52,8 @@ typedef enum {
 #define ATTS_DEV_WAIT_EXPIRED 2u   /* a pipeline wait in the scoring kernel ran out; outputs invalid */
 #define ATTS_DEV_GROUP_ID_RANGE 4u /* a group id was outside [0, G): that candidate has numer 0 */
 #define ATTS_DEV_INDEX_STALE 8u    /* an indexed call was given an index that does not describe fill n; nothing written */
+#define ATTS_DEV_PAGE_RANGE 16u    /* a block-table entry that a sequence needs is missing or outside [0, num_pages) */
+#define ATTS_DEV_SEQ_RANGE 32u     /* a sequence's lengths do not fit the call (negative, or above max_tokens / max_len) */
 
 /* Stage labels written by atts_classify (the three stages of the rejection-sampling pipeline,
  * Sec. 3.3): the highest stage a sample reaches in this turn. */
@@ -360,6 +362,141 @@ int atts_rank_classify_indexed(const float* scores, int64_t Nc, const float* cal
 #define ATTS_STATIC_SCRATCH_BYTES (4 * ATTS_STATIC_MAX_TOTAL)
 int atts_calib_update_static(float* calib, int64_t n, int64_t cap, const float* new_scores, int64_t k,
                              int64_t* n_out, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Attention of drafted tokens over a paged cache (Sec. 3.3 "Verification": the target computes the hidden states that
+ * atts_score_logprob scores; the paper leaves that forward pass to the serving engine).  One layer of one step:
+ *   atts_rope_append     rotates the drafted tokens' queries and keys, writes keys and values into the cache
+ *   atts_tree_attention  attends from every drafted token to the cache and to its own ancestors among the drafts
+ *   atts_cache_weights   adds up what attention every cached slot received
+ *   atts_cache_select, atts_cache_gather   keep the slots that received most and move them to other pages
+ *
+ * The batch.  num_seqs sequences; sequence b holds ctx_lens[b] cached tokens and drafts cu_tokens[b+1] - cu_tokens[b]
+ * further ones, rows cu_tokens[b] .. of the [M, heads, head_dim] arrays.  Slot s of sequence b is entry s % page_size of
+ * page block_table[b][s / page_size]; drafted token t of sequence b has slot ctx_lens[b] + t.
+ *   ctx_lens      dev  [num_seqs] int32, >= 0
+ *   cu_tokens     dev  [num_seqs + 1] int32, 0 = c_0 <= c_1 <= ... <= M
+ *   max_tokens, max_len  host upper bounds of the drafted tokens of a sequence and of ctx_lens[b] + drafted tokens; a
+ *                      sequence that exceeds them (or has a negative length) is left out, or cut at max_len slots, and
+ *                      ATTS_DEV_SEQ_RANGE is recorded.  Tight bounds make fast launches; they need not be exact.
+ * A needed page whose number is missing (beyond table_cols) or outside [0, num_pages) is never used as an address:
+ * ATTS_DEV_PAGE_RANGE is recorded, nothing is written there and its slots read as zeros.
+ * Rows are described by a pointer and two strides in elements (token, head); the last dimension is contiguous.
+ * Types: bf16 or fp16, one for all arrays of a call.
+ */
+#define ATTS_BF16 0
+#define ATTS_FP16 1
+typedef struct {
+  void* k;                    /* dev, 16-byte aligned: key of (page p, entry e, head h) at k + p * page_stride + e *       */
+  void* v;                    /*   slot_stride + h * head_stride elements, head_dim contiguous; v likewise                 */
+  const int32_t* block_table; /* dev [num_seqs][table_stride], the first table_cols columns used                          */
+  int64_t num_seqs, table_cols, table_stride;
+  int64_t num_pages, page_size;                     /* page_size a power of two, 8 .. 4096                                */
+  int64_t page_stride, slot_stride, head_stride;    /* elements, multiples of 8                                           */
+  int32_t heads, head_dim, dtype, reserved;         /* key / value heads; head_dim a multiple of 8, <= 256; reserved = 0  */
+} atts_kv_cache;
+
+/*
+ * Numbers the drafted tokens of each sequence's tree in preorder (host arrays, no device, runs at once).
+ *   parent        host [M] int32: index within the sequence of the token that token t continues, below t; -1 where it
+ *                      continues the cache; -2 marks padding (a row that is not a token: it sees nothing, nothing
+ *                      sees it)
+ *   cu_tokens     host [num_seqs + 1] int32
+ *   pre, end      host [M] int32 out: token j is an ancestor of token i, or i itself, iff pre[j] <= pre[i] < end[j];
+ *                      padding gets pre = end = -1
+ *   depth         host [M] int32 out, may be NULL: number of ancestors among the drafts (the token's position is
+ *                      its sequence's next position + depth); 0 for padding
+ * A parent that is not -2, -1 or an earlier token (padding has no children), or offsets that do not ascend from 0:
+ * ATTS_ERR_ARG, outputs undefined.
+ */
+int atts_tree_plan(const int32_t* parent, const int32_t* cu_tokens, int64_t num_seqs, int32_t* pre, int32_t* end,
+                   int32_t* depth);
+
+/*
+ * Rotary positions and append.  Pair i of a head's first 2 * rotary_pairs channels is turned by the angle
+ * positions[t] * freqs[i]:  (x, y) -> mscale * (x cos - y sin, y cos + x sin); the other channels are copied.
+ *   interleaved = 0: pair i is channels (i, rotary_pairs + i);  1: channels (2 i, 2 i + 1)
+ * q_out gets the rotated queries (it may be q itself, same strides); the rotated keys and the values go to the drafted
+ * tokens' slots of `cache`, rounded once.
+ *   q, k, v       dev  rows [M, Hq | cache heads, head_dim] with strides; 16-byte aligned rows (pointer and strides) take
+ *                      the wide path, any other alignment works
+ *   positions     dev  [M] int32, any value
+ *   freqs         dev  [rotary_pairs] float64, radians per position; the angle is reduced in 64 bits, so that it stays
+ *                      exact to fp32 at any position
+ *   rotary_pairs       0 <= 2 * rotary_pairs <= head_dim;  mscale: factor on cosine and sine (1 for none)
+ *   M, Hq         0 <= M <= 2^30; Hq >= 0 (0: append only, q and q_out may be NULL)
+ */
+int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                     int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                     const int32_t* positions, const double* freqs, int32_t rotary_pairs, float mscale,
+                     int32_t interleaved, const atts_kv_cache* cache, const int32_t* ctx_lens, const int32_t* cu_tokens,
+                     int64_t M, int32_t Hq, int64_t max_tokens, void* q_out, int64_t out_token_stride,
+                     int64_t out_head_stride, void* cuda_stream);
+
+/*
+ * Tree attention.  Token i of sequence b sees every cached slot of b and the drafted tokens j of b with
+ * pre[j] <= pre[i] < end[j] (their keys and values are in the cache already).  Per query head h, with the key / value
+ * head h / (Hq / heads):
+ *   out[i, h] = sum_s p_s v_s,  p = softmax over the visible slots of scale * q . k_s,   lse[i, h] = log sum_s exp(...)
+ * A row that sees nothing (padding, pre < 0) gets out = 0 and lse = -inf.
+ *   q             dev  rows [M, Hq, head_dim], 16-byte aligned, strides multiples of 8 elements; Hq a multiple of the cache's
+ *                      heads, at most 128 query heads per key head; head_dim 64 or 128
+ *   pre, end      dev  [M] int32 (atts_tree_plan); both NULL: every sequence's drafts are one chain (causal)
+ *   scale              finite and > 0
+ *   out           dev  rows [M, Hq, head_dim], aligned as q;   lse  dev [M, Hq] fp32, may be NULL
+ *   workspace     dev  256-byte aligned, at least atts_tree_attention_workspace_bytes(...) for the same sizes
+ * Values of slots below a sequence's length have to be finite unless the slot is padding: a masked product is 0 * v.
+ * Slots from a sequence's length on may hold anything.  Arithmetic: products accumulated in fp32, statistics and sums in
+ * fp32, probabilities rounded to the inputs' type before they multiply v.  Bit-reproducible for given sizes and bounds.
+ */
+int atts_tree_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,
+                                        int64_t max_tokens, int64_t max_len, size_t* bytes);
+int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
+                        const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre, const int32_t* end,
+                        int64_t M, int32_t Hq, int64_t max_tokens, int64_t max_len, float scale, void* out,
+                        int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Attention weight per cached slot, for eviction by accumulated weight:
+ *   weights_out[b, h, s] = weights_in[b, h, s] + sum over tokens i of b and the query heads g of key head h of
+ *                          exp(scale * q[i, g] . k_s - lse[i, g]),  over the slots that i sees
+ * and 0 for slots s from the sequence's length up to max_len.  lse as atts_tree_attention wrote it for the same batch.
+ *   weights_in    dev  [num_seqs, heads, weights_cols] fp32, NULL for zeros, may be weights_out (update in place)
+ *   weights_out   dev  the same shape; columns from max_len on are not written.  max_len <= weights_cols
+ * Other arguments as atts_tree_attention.  Every sum is made in one order: bit-reproducible.
+ */
+int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
+                       const float* lse, const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre,
+                       const int32_t* end, int64_t M, int32_t Hq, int64_t max_tokens, int64_t max_len, float scale,
+                       const float* weights_in, float* weights_out, int64_t weights_cols, void* cuda_stream);
+
+/*
+ * Eviction, first half: per sequence and head, the `budget` slots to keep, ascending: the first `sinks` and the last
+ * `recent` slots, then those of largest weight (ties: the lowest slot first; a NaN counts as less than any number).  A
+ * sequence of at most `budget` slots keeps all of them.
+ *   weights       dev  [num_seqs, heads, weights_cols] fp32
+ *   lens          dev  [num_seqs] int32, slots in use, 0 <= lens[b] <= weights_cols (else ATTS_DEV_SEQ_RANGE, cut)
+ *   budget, sinks, recent   budget >= 1, sinks + recent <= budget
+ *   kept          dev  [num_seqs, heads, budget] int32 out, -1 behind the last kept slot
+ *   counts        dev  [num_seqs] int32 out: min(lens[b], budget), the sequences' new lengths
+ */
+int atts_cache_select(const float* weights, int64_t weights_cols, const int32_t* lens, int64_t num_seqs, int32_t heads,
+                      int64_t budget, int64_t sinks, int64_t recent, int32_t* kept, int32_t* counts,
+                      void* cuda_stream);
+
+/*
+ * Eviction, second half (also: keeping the accepted line of a draft tree): slot c < counts[b] of sequence b, head h in
+ * `dst` gets the key and value of slot kept[b, h, c] of `src`.  The pages written must not be pages read.
+ *   kept          dev  [num_seqs, heads, kept_cols] int32, each in [0, pages of the sequence in src): a slot whose page is
+ *                      missing or out of range is skipped and ATTS_DEV_PAGE_RANGE recorded
+ *   counts        dev  [num_seqs] int32, cut at kept_cols
+ *   weights_in    dev  [num_seqs, heads, in_cols] fp32 or NULL; then weights_out [num_seqs, heads, kept_cols] gets the
+ *                      kept slots' weights and 0 behind them.  kept slots must be below in_cols (others: 0, flagged)
+ */
+int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kept_cols, const int32_t* counts,
+                      const atts_kv_cache* dst, const float* weights_in, int64_t in_cols, float* weights_out,
+                      void* cuda_stream);
 
 /*
  * Waits for `cuda_stream`, then returns in *bits (host out) the OR of the ATTS_DEV_* conditions

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_double, c_int, c_int32, c_int64, c_size_t, c_void_p, c_char_p, POINTER, c_uint32
+from ctypes import c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p, c_char_p, POINTER, c_uint32
 
 from . import build as _build
 
@@ -22,10 +22,13 @@ EXPORTS = (
     "atts_debug_score_plan", "atts_debug_score_unit", "atts_score_slice", "atts_score_combine",
     "atts_calib_index_bytes", "atts_calib_index_build", "atts_calib_update_indexed", "atts_rank_classify_indexed",
     "atts_takeover_ids_workspace_bytes", "atts_takeover_ids", "atts_debug_set_wait", "atts_debug_score_form",
+    "atts_tree_plan", "atts_rope_append", "atts_tree_attention_workspace_bytes", "atts_tree_attention",
+    "atts_cache_weights", "atts_cache_select", "atts_cache_gather",
 )
 
 STAGE_DRAFT, STAGE_ACCEPTED, STAGE_TARGET = 1, 2, 3
 DEV_TOKEN_ID_RANGE, DEV_WAIT_EXPIRED, DEV_GROUP_ID_RANGE, DEV_INDEX_STALE = 1, 2, 4, 8
+DEV_PAGE_RANGE, DEV_SEQ_RANGE = 16, 32
 
 _lib = None
 
@@ -88,6 +91,19 @@ def load(rebuild_if_stale: bool = True) -> ctypes.CDLL:
     lib.atts_takeover_ids.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.atts_debug_set_wait.argtypes = [c_int64, c_int32]
     lib.atts_debug_score_form.argtypes = [c_int64, c_int64, c_int64, POINTER(c_int32)]
+    lib.atts_tree_plan.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
+    rows = [c_void_p, c_int64, c_int64]
+    lib.atts_rope_append.argtypes = rows * 3 + [c_void_p, c_void_p, c_int32, c_float, c_int32, c_void_p, c_void_p, c_void_p,
+                                                c_int64, c_int32, c_int64] + rows + [c_void_p]
+    lib.atts_tree_attention_workspace_bytes.argtypes = [c_int64, c_int64, c_int32, c_int32, c_int32, c_int64, c_int64,
+                                                        POINTER(c_size_t)]
+    lib.atts_tree_attention.argtypes = rows + [c_void_p] * 5 + [c_int64, c_int32, c_int64, c_int64, c_float] + rows + [
+        c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.atts_cache_weights.argtypes = rows + [c_void_p] * 6 + [c_int64, c_int32, c_int64, c_int64, c_float, c_void_p, c_void_p,
+                                                                c_int64, c_void_p]
+    lib.atts_cache_select.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int64, c_int64, c_int64, c_void_p,
+                                      c_void_p, c_void_p]
+    lib.atts_cache_gather.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
     lib.atts_profile_begin.argtypes = [c_int]
     lib.atts_profile_end.argtypes = [POINTER(ctypes.c_float), c_int, POINTER(c_int)]
     for name in EXPORTS[2:]:
@@ -344,3 +360,189 @@ def debug_score_unit(M: int, d: int, V: int, workers: int, ctas: int, u: int) ->
     out = (c_int32 * 4)()
     _check(load().atts_debug_score_unit(M, d, V, workers, ctas, u, out), "atts_debug_score_unit")
     return tuple(out)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Attention of drafted tokens over a paged cache
+# ---------------------------------------------------------------------------------------------------------------------
+class _KvCache(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("block_table", c_void_p), ("num_seqs", c_int64), ("table_cols", c_int64),
+                ("table_stride", c_int64), ("num_pages", c_int64), ("page_size", c_int64), ("page_stride", c_int64),
+                ("slot_stride", c_int64), ("head_stride", c_int64), ("heads", c_int32), ("head_dim", c_int32),
+                ("dtype", c_int32), ("reserved", c_int32)]
+
+
+class PagedCache:
+    """Description of a paged key/value cache, made once and passed to every call (it holds pointers, not contents).
+
+    k, v: [num_pages, page_size, heads, head_dim] bf16 or fp16 (any strides that are multiples of 8 elements, the same for
+    both; head_dim contiguous; a head-major cache is passed as a transposed view); block_table: int32 [num_seqs, pages]."""
+
+    def __init__(self, k, v, block_table):
+        import torch
+        if k.dtype not in (torch.bfloat16, torch.float16) or v.dtype != k.dtype:
+            raise ValueError("k and v have to be bfloat16 or float16, both the same")
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or (k.numel() and k.stride(3) != 1):
+            raise ValueError("k and v: [num_pages, page_size, heads, head_dim] with equal strides, head_dim contiguous")
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+            raise ValueError("block_table: int32 [num_seqs, pages], rows contiguous")
+        if not (k.is_cuda and v.device == k.device and block_table.device == k.device):
+            raise ValueError("k, v and block_table have to be on one CUDA device")
+        self.k, self.v, self.block_table = k, v, block_table
+        self.num_pages, self.page_size, self.heads, self.head_dim = k.shape
+        self.num_seqs, self.dtype, self.device = block_table.shape[0], k.dtype, k.device
+        # a dimension of one entry has a stride that means nothing
+        ps, ss, hs = (k.stride(i) if k.shape[i] > 1 else 0 for i in range(3))
+        self._c = _KvCache(_ptr(k), _ptr(v), _ptr(block_table), self.num_seqs, block_table.shape[1],
+                           block_table.stride(0) if self.num_seqs > 1 else block_table.shape[1], self.num_pages,
+                           self.page_size, ps, ss, hs, self.heads, self.head_dim, 0 if k.dtype == torch.bfloat16 else 1, 0)
+        self._ref = ctypes.addressof(self._c)
+
+
+def _rows(t, name: str, M: int, heads, cache: PagedCache):
+    """(pointer, token stride, head stride) of a [M, heads, head_dim] tensor of the cache's type."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != M or (heads is not None and shape[1] != heads) or shape[2] != cache.head_dim:
+        raise ValueError(f"{name}: expected [{M}, {'heads' if heads is None else heads}, {cache.head_dim}], got {tuple(shape)}")
+    if t.dtype != cache.dtype or t.device != cache.device:
+        raise ValueError(f"{name}: has to be {cache.dtype} on {cache.device} like the cache")
+    if stride[2] != 1 and t.numel():
+        raise ValueError(f"{name}: head_dim has to be contiguous")
+    return t.data_ptr(), stride[0] if M > 1 else 0, stride[1] if shape[1] > 1 else 0
+
+
+def _vec(t, name: str, dtype, n: int, device):
+    """Pointer of a contiguous tensor of n entries."""
+    if t.dtype != dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: has to be a contiguous {dtype} tensor of {n} entries on {device}")
+    return t.data_ptr()
+
+
+def tree_plan(parent, cu_tokens):
+    """Preorder numbers of draft trees (host): parent [M] int32 per token (index within its sequence, -1: continues the
+    cache, -2: padding), cu_tokens [num_seqs + 1] int32, both CPU tensors or arrays -> (pre, end, depth) int32 CPU tensors:
+    token j is an ancestor of i, or i itself, iff pre[j] <= pre[i] < end[j]."""
+    import torch
+    parent = torch.as_tensor(parent, dtype=torch.int32).contiguous()
+    cu = torch.as_tensor(cu_tokens, dtype=torch.int32).contiguous()
+    if cu.numel() < 1 or int(cu[-1]) != parent.numel():
+        raise ValueError("cu_tokens has to end at the number of tokens")
+    pre, end, depth = (torch.empty_like(parent) for _ in range(3))
+    _check(load().atts_tree_plan(_ptr(parent), _ptr(cu), cu.numel() - 1, _ptr(pre), _ptr(end), _ptr(depth)), "atts_tree_plan")
+    return pre, end, depth
+
+
+def rope_freqs(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: int = 8192,
+               low: float = 1.0, high: float = 4.0, fast: float = 32.0, slow: float = 1.0):
+    """Rotations of rotary positions: (float64 CPU tensor [rotary_dim / 2] of radians per position, factor on cos and sin).
+
+    f_i = base ** (-2 i / rotary_dim), then for long contexts
+      "linear"  f / factor (positions stretched)
+      "bands"   pairs that turn more than `high` times over original_length keep f, those below `low` turns get f / factor,
+                a straight line in the number of turns in between
+      "ramp"    the same between the pairs that turn `fast` and `slow` times, a straight line in the pair's number, and
+                cosine and sine grow by 0.1 ln(factor) + 1"""
+    import math
+    import torch
+    if rotary_dim < 0 or rotary_dim % 2 or not base > 0 or not factor > 0 or original_length < 1:
+        raise ValueError("rotary_dim has to be even and >= 0, base, factor and original_length positive")
+    i = torch.arange(0, rotary_dim, 2, dtype=torch.float64)
+    f = base ** (-i / max(rotary_dim, 1))
+    if scaling == "none":
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "bands":
+        if not high > low:
+            raise ValueError("bands: high has to be above low")
+        keep = ((original_length * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        return f * keep + f / factor * (1 - keep), 1.0
+    if scaling == "ramp":
+        def pair(turns):   # where original_length positions make that many turns, in channels
+            return rotary_dim * math.log(original_length / (turns * 2 * math.pi)) / (2 * math.log(base))
+        first, last = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), max(rotary_dim - 1, 0))
+        ramp = ((torch.arange(rotary_dim // 2, dtype=torch.float64) - first) / max(last - first, 1e-3)).clamp(0.0, 1.0)
+        return f * (1 - ramp) + f / factor * ramp, (0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0)
+    raise ValueError(f"scaling: one of none, linear, bands, ramp, not {scaling!r}")
+
+
+def rope_append(q, k, v, positions, freqs, cache: PagedCache, ctx_lens, cu_tokens, max_tokens: int, q_out, interleaved: bool = False,
+                mscale: float = 1.0) -> None:
+    """Rotate q [M, Hq, D] into q_out (may be q) and k [M, heads, D] into the cache's slots ctx_lens[b] + t, copy v beside
+    it. positions int32 [M], freqs float64 [pairs] on the device (:func:`rope_freqs`). q and q_out None: append only."""
+    import torch
+    M, dev, B = k.shape[0], cache.device, cache.num_seqs
+    kr, vr = _rows(k, "k", M, cache.heads, cache), _rows(v, "v", M, cache.heads, cache)
+    Hq = 0 if q is None else q.shape[1]
+    qr, outr = ((0, 0, 0), (0, 0, 0)) if q is None else (_rows(q, "q", M, None, cache), _rows(q_out, "q_out", M, Hq, cache))
+    n = freqs.numel()
+    _check(load().atts_rope_append(*qr, *kr, *vr, _vec(positions, "positions", torch.int32, M, dev),
+                                   _vec(freqs, "freqs", torch.float64, n, dev), n, mscale, 1 if interleaved else 0, cache._ref,
+                                   _vec(ctx_lens, "ctx_lens", torch.int32, B, dev),
+                                   _vec(cu_tokens, "cu_tokens", torch.int32, B + 1, dev), M, Hq, max_tokens, *outr, _stream()),
+           "atts_rope_append")
+
+
+def tree_attention_workspace_bytes(num_seqs: int, M: int, Hq: int, heads: int, head_dim: int, max_tokens: int, max_len: int) -> int:
+    out = c_size_t(0)
+    _check(load().atts_tree_attention_workspace_bytes(num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, ctypes.byref(out)),
+           "atts_tree_attention_workspace_bytes")
+    return out.value
+
+
+def tree_attention(q, cache: PagedCache, ctx_lens, cu_tokens, pre, end, max_tokens: int, max_len: int, scale: float, out, lse,
+                   workspace) -> None:
+    """Attention of q [M, Hq, D] over each sequence's cached slots and its own drafted ancestors -> out [M, Hq, D],
+    lse [M, Hq] f32 (or None). pre, end int32 [M] (:func:`tree_plan`), both None: chains."""
+    import torch
+    M, Hq = q.shape[0], q.shape[1]
+    dev, B, i32 = cache.device, cache.num_seqs, torch.int32
+    _check(load().atts_tree_attention(*_rows(q, "q", M, Hq, cache), cache._ref, _vec(ctx_lens, "ctx_lens", i32, B, dev),
+                                      _vec(cu_tokens, "cu_tokens", i32, B + 1, dev), None if pre is None else _vec(pre, "pre", i32, M, dev),
+                                      None if end is None else _vec(end, "end", i32, M, dev), M, Hq, max_tokens, max_len, scale,
+                                      *_rows(out, "out", M, Hq, cache), None if lse is None else _vec(lse, "lse", torch.float32, M * Hq, dev),
+                                      _ptr(workspace), _nbytes(workspace), _stream()), "atts_tree_attention")
+
+
+def cache_weights(q, cache: PagedCache, lse, ctx_lens, cu_tokens, pre, end, max_tokens: int, max_len: int, scale: float, weights_in,
+                  weights_out) -> None:
+    """weights_out[b, h, s] = weights_in[b, h, s] (None: 0) + the attention that slot s of key head h receives in this batch
+    (lse as tree_attention wrote it); [num_seqs, heads, cols] f32 contiguous, weights_in may be weights_out."""
+    import torch
+    M, Hq = q.shape[0], q.shape[1]
+    dev, B, i32 = cache.device, cache.num_seqs, torch.int32
+    cols = weights_out.shape[-1]
+    n = B * cache.heads * cols
+    _check(load().atts_cache_weights(*_rows(q, "q", M, Hq, cache), cache._ref, _vec(lse, "lse", torch.float32, M * Hq, dev),
+                                     _vec(ctx_lens, "ctx_lens", i32, B, dev), _vec(cu_tokens, "cu_tokens", i32, B + 1, dev),
+                                     None if pre is None else _vec(pre, "pre", i32, M, dev), None if end is None else _vec(end, "end", i32, M, dev),
+                                     M, Hq, max_tokens, max_len, scale,
+                                     None if weights_in is None else _vec(weights_in, "weights_in", torch.float32, n, dev),
+                                     _vec(weights_out, "weights_out", torch.float32, n, dev), cols, _stream()), "atts_cache_weights")
+
+
+def cache_select(weights, lens, budget: int, sinks: int, recent: int, kept, counts) -> None:
+    """kept [num_seqs, heads, budget] i32: the slots to keep, ascending (the first `sinks`, the last `recent`, then the
+    largest of weights [num_seqs, heads, cols] f32; ties: the lowest), -1 behind; counts [num_seqs] i32 = min(lens, budget)."""
+    import torch
+    B, heads, cols = weights.shape
+    dev = weights.device
+    _check(load().atts_cache_select(_vec(weights, "weights", torch.float32, B * heads * cols, dev), cols,
+                                    _vec(lens, "lens", torch.int32, B, dev), B, heads, budget, sinks, recent,
+                                    _vec(kept, "kept", torch.int32, B * heads * budget, dev),
+                                    _vec(counts, "counts", torch.int32, B, dev), _stream()), "atts_cache_select")
+
+
+def cache_gather(src: PagedCache, kept, counts, dst: PagedCache, weights_in=None, weights_out=None) -> None:
+    """Slot c of every sequence and head in dst gets key and value of slot kept[b, h, c] of src (c < counts[b]; dst's pages
+    must not be src's), weights_out [num_seqs, heads, cols] the kept slots' weights."""
+    import torch
+    dev = src.device
+    cols = kept.shape[-1]
+    n = src.num_seqs * src.heads * cols
+    in_cols = 0 if weights_in is None else weights_in.shape[-1]
+    _check(load().atts_cache_gather(src._ref, _vec(kept, "kept", torch.int32, n, dev), cols,
+                                    _vec(counts, "counts", torch.int32, src.num_seqs, dev), dst._ref,
+                                    None if weights_in is None else _vec(weights_in, "weights_in", torch.float32, src.num_seqs * src.heads * in_cols, dev),
+                                    in_cols, None if weights_out is None else _vec(weights_out, "weights_out", torch.float32, n, dev),
+                                    _stream()), "atts_cache_gather")

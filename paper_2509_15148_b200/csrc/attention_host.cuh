@@ -1,0 +1,301 @@
+// C-ABI entry points of the attention side (declared in include/atts.h): argument checks and launch geometry.
+// Included by atts.cu behind its own helpers.
+#pragma once
+#include "rope_cache.cuh"
+#include "tree_attention.cuh"
+
+namespace atts {
+
+constexpr int64_t kMaxSlots = 1ll << 30;  // slots of one sequence, columns of a weight row
+
+static inline bool finite_pos(float x) { return x > 0.f && x <= 3.402823466e38f; }
+
+// Checks a cache handle's description and fills the kernels' view of it.
+static int cache_view(const atts_kv_cache* c, CacheView* out) {
+  if (!c) return ATTS_ERR_NULL;
+  if (c->dtype != ATTS_BF16 && c->dtype != ATTS_FP16) return ATTS_ERR_ARG;
+  if (c->reserved != 0) return ATTS_ERR_ARG;
+  if (c->num_seqs < 0 || c->num_seqs > 65535 || c->heads < 1 || c->heads > 1024) return ATTS_ERR_SHAPE;
+  if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 != 0) return ATTS_ERR_SHAPE;
+  if (c->page_size < 8 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0) return ATTS_ERR_SHAPE;
+  if (c->num_pages < 0 || c->num_pages > 0x7FFFFFFF || c->table_cols < 0 || c->table_cols > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  if (c->table_stride < c->table_cols && c->num_seqs > 1) return ATTS_ERR_SHAPE;
+  if (c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0 || c->page_stride % 8 || c->slot_stride % 8 ||
+      c->head_stride % 8)
+    return ATTS_ERR_SHAPE;
+  if ((c->num_pages > 0 && (!c->k || !c->v)) || (c->num_seqs > 0 && c->table_cols > 0 && !c->block_table)) return ATTS_ERR_NULL;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->block_table, 4)) return ATTS_ERR_ALIGN;
+  out->k = static_cast<char*>(c->k);
+  out->v = static_cast<char*>(c->v);
+  out->table = c->block_table;
+  out->table_stride = c->table_stride;
+  out->page_stride = c->page_stride;
+  out->slot_stride = c->slot_stride;
+  out->head_stride = c->head_stride;
+  out->table_cols = (int32_t)c->table_cols;
+  out->num_pages = (int32_t)c->num_pages;
+  out->heads = c->heads;
+  int lg = 0;
+  while ((1ll << lg) < c->page_size) ++lg;
+  out->page_log2 = lg;
+  return ATTS_OK;
+}
+
+// Checks shared by the two calls that read the cache against queries.
+static int check_queries(const void* q, int64_t q_ts, int64_t q_hs, const atts_kv_cache* c, const int32_t* ctx,
+                         const int32_t* cu, const int32_t* pre, const int32_t* end, int64_t M, int32_t Hq,
+                         int64_t max_tokens, int64_t max_len, float scale) {
+  if (c->head_dim != 64 && c->head_dim != 128) return ATTS_ERR_SHAPE;
+  if (M < 0 || M > (1ll << 30) || Hq < 1 || Hq % c->heads != 0 || Hq / c->heads > 128) return ATTS_ERR_SHAPE;
+  if (max_tokens < 0 || max_len < 0 || max_len > kMaxSlots || max_tokens > max_len) return ATTS_ERR_SHAPE;
+  if (q_ts < 0 || q_hs < 0 || q_ts % 8 || q_hs % 8) return ATTS_ERR_SHAPE;
+  if (!finite_pos(scale)) return ATTS_ERR_ARG;
+  if ((M > 0 && !q) || (c->num_seqs > 0 && (!ctx || !cu)) || ((pre == nullptr) != (end == nullptr))) return ATTS_ERR_NULL;
+  if (!aligned(q, 16) || !aligned(ctx, 4) || !aligned(cu, 4) || !aligned(pre, 4) || !aligned(end, 4)) return ATTS_ERR_ALIGN;
+  return ATTS_OK;
+}
+
+}  // namespace atts
+
+using namespace atts;
+
+extern "C" {
+
+int atts_tree_plan(const int32_t* parent, const int32_t* cu_tokens, int64_t num_seqs, int32_t* pre, int32_t* end,
+                   int32_t* depth) {
+  if (num_seqs < 0 || num_seqs >= (1ll << 31)) return ATTS_ERR_SHAPE;
+  if (num_seqs == 0) return ATTS_OK;
+  if (!cu_tokens) return ATTS_ERR_NULL;
+  if (cu_tokens[0] != 0) return ATTS_ERR_ARG;
+  for (int64_t b = 0; b < num_seqs; ++b)
+    if (cu_tokens[b + 1] < cu_tokens[b]) return ATTS_ERR_ARG;
+  if (cu_tokens[num_seqs] > 0 && (!parent || !pre || !end)) return ATTS_ERR_NULL;
+  for (int64_t b = 0; b < num_seqs; ++b) {
+    const int32_t n = cu_tokens[b + 1] - cu_tokens[b];
+    const int32_t* par = parent + cu_tokens[b];
+    int32_t *p = pre + cu_tokens[b], *e = end + cu_tokens[b];
+    for (int32_t i = 0; i < n; ++i) {
+      if (par[i] < -2 || par[i] >= i || (par[i] >= 0 && par[par[i]] == -2)) return ATTS_ERR_ARG;
+      e[i] = 1;
+    }
+    // sizes of the subtrees (children come after their parents), kept in end
+    for (int32_t i = n - 1; i >= 0; --i)
+      if (par[i] >= 0) e[par[i]] += e[i];
+    // A token's place follows its parent's and the subtrees of the siblings before it.  While a token still has
+    // children to come, its subtree's unplaced part ends at pre + size: the first child takes the last piece.
+    int32_t top = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      if (par[i] == -2) {
+        p[i] = e[i] = -1;
+        continue;
+      }
+      const int32_t size = e[i];
+      if (par[i] == -1) {
+        p[i] = top;
+        top += size;
+      } else {
+        e[par[i]] -= size;        // end of the parent's part that is not placed yet
+        p[i] = e[par[i]];
+      }
+      e[i] = p[i] + size;
+    }
+    // restore the ends: after the pass above end[i] = pre[i] + 1 for every token; the true end is the largest among
+    // its descendants'
+    for (int32_t i = n - 1; i >= 0; --i)
+      if (par[i] >= 0 && e[par[i]] < e[i]) e[par[i]] = e[i];
+    if (depth) {
+      int32_t* d = depth + cu_tokens[b];
+      for (int32_t i = 0; i < n; ++i) d[i] = par[i] >= 0 ? d[par[i]] + 1 : 0;
+    }
+  }
+  return ATTS_OK;
+}
+
+int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                     int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                     const int32_t* positions, const double* freqs, int32_t rotary_pairs, float mscale,
+                     int32_t interleaved, const atts_kv_cache* cache, const int32_t* ctx_lens, const int32_t* cu_tokens,
+                     int64_t M, int32_t Hq, int64_t max_tokens, void* q_out, int64_t out_token_stride,
+                     int64_t out_head_stride, void* cuda_stream) {
+  RopeArgs a;
+  int st = cache_view(cache, &a.cache);
+  if (st != ATTS_OK) return st;
+  const int D = cache->head_dim;
+  if (M < 0 || M > (1ll << 30) || Hq < 0 || Hq > (1 << 20) || max_tokens < 0 || max_tokens > kMaxSlots) return ATTS_ERR_SHAPE;
+  if (rotary_pairs < 0 || 2 * (int64_t)rotary_pairs > D) return ATTS_ERR_SHAPE;
+  if (q_token_stride < 0 || q_head_stride < 0 || k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 ||
+      v_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0)
+    return ATTS_ERR_SHAPE;
+  if (interleaved != 0 && interleaved != 1) return ATTS_ERR_ARG;
+  if (!(mscale >= -3.402823466e38f && mscale <= 3.402823466e38f)) return ATTS_ERR_ARG;
+  if (cache->num_seqs > 0 && (!ctx_lens || !cu_tokens)) return ATTS_ERR_NULL;
+  if (M > 0 && (!k || !v || (Hq > 0 && (!q || !q_out)) || (rotary_pairs > 0 && (!positions || !freqs)))) return ATTS_ERR_NULL;
+  if (!aligned(q, 2) || !aligned(k, 2) || !aligned(v, 2) || !aligned(q_out, 2) || !aligned(positions, 4) || !aligned(freqs, 8) ||
+      !aligned(ctx_lens, 4) || !aligned(cu_tokens, 4))
+    return ATTS_ERR_ALIGN;
+  const DeviceInfo* di;
+  st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  if (M == 0 || cache->num_seqs == 0 || max_tokens == 0) return ATTS_OK;
+  a.q = static_cast<const char*>(q);
+  a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v);
+  a.q_out = static_cast<char*>(q_out);
+  a.q_ts = q_token_stride; a.q_hs = q_head_stride;
+  a.k_ts = k_token_stride; a.k_hs = k_head_stride;
+  a.v_ts = v_token_stride; a.v_hs = v_head_stride;
+  a.o_ts = out_token_stride; a.o_hs = out_head_stride;
+  a.positions = positions; a.ctx = ctx_lens; a.cu = cu_tokens; a.freqs = freqs;
+  a.pairs = rotary_pairs; a.D = D; a.Hq = Hq; a.M = (int)M; a.max_tokens = (int)max_tokens; a.mscale = mscale;
+  const int64_t bits = (Hq > 0 ? q_token_stride | q_head_stride | out_token_stride | out_head_stride : 0) | k_token_stride |
+                       k_head_stride | v_token_stride | v_head_stride;
+  const bool wide = bits % 8 == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(q_out, 16) &&
+                    rotary_pairs % (interleaved ? 4 : 8) == 0;
+  a.tpb = M >= 4 * 8 * (int64_t)di->sm_count ? 4 : 1;
+  const int64_t gx = (max_tokens + a.tpb - 1) / a.tpb;
+  if (gx > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  const dim3 grid((unsigned)gx, (unsigned)cache->num_seqs);
+  const size_t smem = sizeof(float2) * a.tpb * (size_t)rotary_pairs;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+#define ATTS_ROPE(T, I, W) rope_append_kernel<T, I, W><<<grid, kRopeThreads, smem, stream>>>(a, di->dev_status)
+#define ATTS_ROPE_T(T)                                                                        \
+  do {                                                                                        \
+    if (interleaved) { if (wide) ATTS_ROPE(T, true, true); else ATTS_ROPE(T, true, false); }  \
+    else { if (wide) ATTS_ROPE(T, false, true); else ATTS_ROPE(T, false, false); }            \
+  } while (0)
+  if (cache->dtype == ATTS_BF16) ATTS_ROPE_T(__nv_bfloat16);
+  else ATTS_ROPE_T(__half);
+#undef ATTS_ROPE_T
+#undef ATTS_ROPE
+  return launch_status();
+}
+
+int atts_tree_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,
+                                        int64_t max_tokens, int64_t max_len, size_t* bytes) {
+  if (!bytes) return ATTS_ERR_NULL;
+  if (num_seqs < 0 || num_seqs > 65535 || M < 0 || M > (1ll << 30) || heads < 1 || heads > 1024 || Hq < 1 || Hq % heads != 0 ||
+      Hq / heads > 128 || (head_dim != 64 && head_dim != 128) || max_tokens < 0 || max_len < max_tokens || max_len > kMaxSlots)
+    return ATTS_ERR_SHAPE;
+  *bytes = 256;
+  return ATTS_OK;
+}
+
+int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
+                        const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre, const int32_t* end,
+                        int64_t M, int32_t Hq, int64_t max_tokens, int64_t max_len, float scale, void* out,
+                        int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
+                        size_t workspace_bytes, void* cuda_stream) {
+  AttnArgs a;
+  int st = cache_view(cache, &a.cache);
+  if (st != ATTS_OK) return st;
+  st = check_queries(q, q_token_stride, q_head_stride, cache, ctx_lens, cu_tokens, pre, end, M, Hq, max_tokens, max_len, scale);
+  if (st != ATTS_OK) return st;
+  if (out_token_stride < 0 || out_head_stride < 0 || out_token_stride % 8 || out_head_stride % 8) return ATTS_ERR_SHAPE;
+  if ((M > 0 && !out) || !workspace) return ATTS_ERR_NULL;
+  if (!aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, 256)) return ATTS_ERR_ALIGN;
+  size_t need = 0;
+  st = atts_tree_attention_workspace_bytes(cache->num_seqs, M, Hq, cache->heads, cache->head_dim, max_tokens, max_len, &need);
+  if (st != ATTS_OK) return st;
+  if (workspace_bytes < need) return ATTS_ERR_WORKSPACE;
+  const DeviceInfo* di;
+  st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  if (M == 0 || cache->num_seqs == 0 || max_tokens == 0) return ATTS_OK;
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.q_ts = q_token_stride; a.q_hs = q_head_stride; a.o_ts = out_token_stride; a.o_hs = out_head_stride;
+  a.ctx = ctx_lens; a.cu = cu_tokens; a.pre = pre; a.end = end;
+  a.M = (int)M; a.Hq = Hq; a.G = Hq / cache->heads; a.max_tokens = (int)max_tokens; a.max_len = (int)max_len;
+  a.scale = scale;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const dim3 grid((unsigned)((max_tokens + 7) / 8), (unsigned)Hq, (unsigned)cache->num_seqs);
+  const bool bf = cache->dtype == ATTS_BF16;
+  if (cache->head_dim == 128) {
+    if (bf) tree_attention_simple_kernel<__nv_bfloat16, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
+    else tree_attention_simple_kernel<__half, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
+  } else {
+    if (bf) tree_attention_simple_kernel<__nv_bfloat16, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
+    else tree_attention_simple_kernel<__half, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
+  }
+  return launch_status();
+}
+
+int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
+                       const float* lse, const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre,
+                       const int32_t* end, int64_t M, int32_t Hq, int64_t max_tokens, int64_t max_len, float scale,
+                       const float* weights_in, float* weights_out, int64_t weights_cols, void* cuda_stream) {
+  WeightArgs a;
+  int st = cache_view(cache, &a.cache);
+  if (st != ATTS_OK) return st;
+  st = check_queries(q, q_token_stride, q_head_stride, cache, ctx_lens, cu_tokens, pre, end, M, Hq, max_tokens, max_len, scale);
+  if (st != ATTS_OK) return st;
+  if (weights_cols < max_len || weights_cols > kMaxSlots) return ATTS_ERR_SHAPE;
+  if ((M > 0 && !lse) || (cache->num_seqs > 0 && max_len > 0 && !weights_out)) return ATTS_ERR_NULL;
+  if (!aligned(lse, 4) || !aligned(weights_in, 4) || !aligned(weights_out, 4)) return ATTS_ERR_ALIGN;
+  const DeviceInfo* di;
+  st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  if (cache->num_seqs == 0 || max_len == 0) return ATTS_OK;
+  a.q = static_cast<const char*>(q);
+  a.lse = lse;
+  a.q_ts = q_token_stride; a.q_hs = q_head_stride;
+  a.ctx = ctx_lens; a.cu = cu_tokens; a.pre = pre; a.end = end;
+  a.M = (int)M; a.Hq = Hq; a.G = Hq / cache->heads; a.max_tokens = (int)max_tokens; a.max_len = (int)max_len;
+  a.scale = scale;
+  a.win = weights_in; a.wout = weights_out; a.wcols = weights_cols;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const dim3 grid((unsigned)((max_len + 7) / 8), (unsigned)cache->heads, (unsigned)cache->num_seqs);
+  const bool bf = cache->dtype == ATTS_BF16;
+  if (cache->head_dim == 128) {
+    if (bf) cache_weights_simple_kernel<__nv_bfloat16, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
+    else cache_weights_simple_kernel<__half, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
+  } else {
+    if (bf) cache_weights_simple_kernel<__nv_bfloat16, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
+    else cache_weights_simple_kernel<__half, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
+  }
+  return launch_status();
+}
+
+int atts_cache_select(const float* weights, int64_t weights_cols, const int32_t* lens, int64_t num_seqs, int32_t heads,
+                      int64_t budget, int64_t sinks, int64_t recent, int32_t* kept, int32_t* counts, void* cuda_stream) {
+  if (num_seqs < 0 || num_seqs > 65535 || heads < 1 || heads > 1024 || weights_cols < 0 || weights_cols > kMaxSlots)
+    return ATTS_ERR_SHAPE;
+  if (budget < 1 || budget > kMaxSlots || sinks < 0 || recent < 0 || sinks > budget || recent > budget || sinks + recent > budget)
+    return ATTS_ERR_SHAPE;
+  if (num_seqs > 0 && (!lens || !kept || !counts || (weights_cols > 0 && !weights))) return ATTS_ERR_NULL;
+  if (!aligned(weights, 4) || !aligned(lens, 4) || !aligned(kept, 4) || !aligned(counts, 4)) return ATTS_ERR_ALIGN;
+  const DeviceInfo* di;
+  int st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  if (num_seqs == 0) return ATTS_OK;
+  cache_select_kernel<<<(unsigned)(num_seqs * heads), kSelectThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+      weights, weights_cols, lens, heads, (int)budget, (int)sinks, (int)recent, kept, counts, di->dev_status);
+  return launch_status();
+}
+
+int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kept_cols, const int32_t* counts,
+                      const atts_kv_cache* dst, const float* weights_in, int64_t in_cols, float* weights_out,
+                      void* cuda_stream) {
+  CacheView s, d;
+  int st = cache_view(src, &s);
+  if (st != ATTS_OK) return st;
+  if ((st = cache_view(dst, &d)) != ATTS_OK) return st;
+  if (src->dtype != dst->dtype) return ATTS_ERR_ARG;
+  if (src->heads != dst->heads || src->head_dim != dst->head_dim || src->num_seqs != dst->num_seqs) return ATTS_ERR_SHAPE;
+  if (kept_cols < 0 || kept_cols > kMaxSlots || in_cols < 0 || in_cols > kMaxSlots) return ATTS_ERR_SHAPE;
+  if (src->num_seqs > 0 && ((kept_cols > 0 && !kept) || !counts)) return ATTS_ERR_NULL;
+  if ((weights_in == nullptr) != (weights_out == nullptr)) return ATTS_ERR_NULL;
+  if (!aligned(kept, 4) || !aligned(counts, 4) || !aligned(weights_in, 4) || !aligned(weights_out, 4)) return ATTS_ERR_ALIGN;
+  const DeviceInfo* di;
+  st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  if (src->num_seqs == 0 || kept_cols == 0) return ATTS_OK;
+  const int64_t gx = (kept_cols * (src->head_dim / 8) + 255) / 256;
+  const dim3 grid((unsigned)gx, (unsigned)src->heads, (unsigned)src->num_seqs);
+  cache_gather_kernel<<<grid, 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(s, d, src->head_dim, kept, kept_cols, counts,
+                                                                                weights_in, in_cols, weights_out, di->dev_status);
+  return launch_status();
+}
+
+}  // extern "C"

@@ -1,5 +1,6 @@
 // C-ABI entry points of libatts (declared in include/atts.h): argument checks, launch geometry,
-// tensor-map encoding.  All device work is in the kernels of conformal.cuh and lmhead_lse.cuh.
+// tensor-map encoding.  All device work is in the kernels of conformal.cuh and lmhead_lse.cuh; the entry points of the
+// attention side are in attention_host.cuh.
 #include "atts.h"
 
 #include <cuda.h>
@@ -997,3 +998,5 @@ int atts_profile_end(float* ms, int cap, int* count) {
 }
 
 }  // extern "C"
+
+#include "attention_host.cuh"
