@@ -49,10 +49,91 @@ static int check_queries(const void* q, int64_t q_ts, int64_t q_hs, const atts_k
   if (M < 0 || M > (1ll << 30) || Hq < 1 || Hq % c->heads != 0 || Hq / c->heads > 128) return ATTS_ERR_SHAPE;
   if (max_tokens < 0 || max_len < 0 || max_len > kMaxSlots || max_tokens > max_len) return ATTS_ERR_SHAPE;
   if (q_ts < 0 || q_hs < 0 || q_ts % 8 || q_hs % 8) return ATTS_ERR_SHAPE;
+  // rows of their own: a stride of 0 (a broadcast) is refused where there is more than one entry
+  if ((M > 1 && q_ts == 0) || (Hq > 1 && q_hs == 0) || c->num_pages < 1 || (c->num_pages > 1 && c->page_stride == 0) ||
+      c->slot_stride == 0 || (c->heads > 1 && c->head_stride == 0))
+    return ATTS_ERR_SHAPE;
   if (!finite_pos(scale)) return ATTS_ERR_ARG;
   if ((M > 0 && !q) || (c->num_seqs > 0 && (!ctx || !cu)) || ((pre == nullptr) != (end == nullptr))) return ATTS_ERR_NULL;
   if (!aligned(q, 16) || !aligned(ctx, 4) || !aligned(cu, 4) || !aligned(pre, 4) || !aligned(end, 4)) return ATTS_ERR_ALIGN;
   return ATTS_OK;
+}
+
+// Tensor maps.  Queries: (channel, head, token) with boxes of 64 channels, the heads of a group and the tokens of a row
+// tile.  Cache: (channel, slot of a page, head, page) with boxes of 64 channels and the slots of a page (128 at most).
+static int encode_rows(const DeviceInfo* di, CUtensorMap* map, bool bf16, const void* base, int rank, const int64_t* dims,
+                       const int64_t* strides_elems, const int* box) {
+  cuuint64_t d[4], st[3];
+  cuuint32_t b[4], e[4];
+  for (int i = 0; i < rank; ++i) {
+    d[i] = (cuuint64_t)dims[i];
+    b[i] = (cuuint32_t)box[i];
+    e[i] = 1;
+    // a dimension of one entry has no stride of its own
+    if (i > 0) st[i - 1] = dims[i] > 1 ? (cuuint64_t)strides_elems[i - 1] * 2 : (cuuint64_t)dims[0] * 2;
+  }
+  const CUresult r = di->encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
+                                const_cast<void*>(base), d, st, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? ATTS_OK : ATTS_ERR_CUDA;
+}
+static int encode_queries(const DeviceInfo* di, CUtensorMap* map, const atts_kv_cache* c, const void* q, int64_t q_ts, int64_t q_hs,
+                          int64_t M, int32_t Hq, int tokens) {
+  const int64_t dims[3] = {c->head_dim, Hq, M}, st[2] = {q_hs, q_ts};
+  const int box[3] = {64, Hq / c->heads, tokens};
+  return encode_rows(di, map, c->dtype == ATTS_BF16, q, 3, dims, st, box);
+}
+static int encode_cache(const DeviceInfo* di, CUtensorMap* map, const atts_kv_cache* c, const void* base) {
+  const int64_t dims[4] = {c->head_dim, c->page_size, c->heads, c->num_pages}, st[3] = {c->slot_stride, c->head_stride, c->page_stride};
+  const int box[4] = {64, (int)(c->page_size < 128 ? c->page_size : 128), 1, 1};
+  return encode_rows(di, map, c->dtype == ATTS_BF16, base, 4, dims, st, box);
+}
+
+// How an attention call is cut up.  Row tiles: as many whole tokens as fit 128 rows; two of them to a CTA if the longest
+// sequence has more than one.  Chunks: the number that makes the launch shortest when a slot tile takes one unit of time,
+// a CTA's start and end 2.5 and joining the chunks 2 (a unit is about 1.4 us: 64 KB per SM at the device's bandwidth).
+struct AttnShape {
+  bool two;
+  AttnPlan p;
+};
+static AttnShape attn_shape(int sms, int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int64_t max_tokens, int64_t max_len) {
+  AttnShape r{};
+  const int G = Hq / heads;
+  r.p.tpt = kAttnTile / G;
+  r.two = max_tokens > r.p.tpt;
+  const int64_t per = r.p.tpt * (r.two ? 2 : 1);
+  r.p.nq = (int)((max_tokens + per - 1) / per);
+  const int64_t tiles = (max_len + kAttnTile - 1) / kAttnTile;
+  const int64_t base = num_seqs * heads * r.p.nq;
+  double best = 0.0;
+  int64_t best_n = 1;
+  for (int64_t n = 1; n <= tiles && n <= 256 && (n == 1 || base * n <= 64 * (int64_t)sms); ++n) {
+    const int64_t ct = (tiles + n - 1) / n;
+    if ((tiles + ct - 1) / ct != n) continue;   // the same chunk length with fewer chunks was looked at
+    const double cost = (double)((base * n + sms - 1) / sms) * (2.5 + (double)ct) + (n > 1 ? 2.0 : 0.0);
+    if (n == 1 || cost < best) {
+      best = cost;
+      best_n = n;
+    }
+  }
+  r.p.chunk = (int)(tiles > 0 ? (tiles + best_n - 1) / best_n : 1);
+  r.p.chunks = (int)(tiles > 0 ? (tiles + r.p.chunk - 1) / r.p.chunk : 1);
+  return r;
+}
+static size_t attn_workspace(const AttnShape& s, int64_t M, int32_t Hq, int32_t head_dim) {
+  if (s.p.chunks <= 1) return 256;
+  const size_t rows = (size_t)M * Hq * s.p.chunks;
+  return round_up(rows * 4, 256) + round_up(rows * head_dim * 4, 256);
+}
+
+template <typename T, int D, bool TWO>
+static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, const AttnPlan& p,
+                            dim3 grid, unsigned* status, cudaStream_t stream) {
+  tree_attention_kernel<T, D, TWO><<<grid, kAttnThreads, AttnCfg<D, TWO>::kSmemBytes, stream>>>(mq, mk, mv, a, p, status);
+  int st = launch_status();
+  if (st != ATTS_OK || p.chunks <= 1) return st;
+  const int64_t rows = (int64_t)a.max_tokens * a.Hq;
+  return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
 }
 
 }  // namespace atts
@@ -176,7 +257,10 @@ int atts_tree_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq,
   if (num_seqs < 0 || num_seqs > 65535 || M < 0 || M > (1ll << 30) || heads < 1 || heads > 1024 || Hq < 1 || Hq % heads != 0 ||
       Hq / heads > 128 || (head_dim != 64 && head_dim != 128) || max_tokens < 0 || max_len < max_tokens || max_len > kMaxSlots)
     return ATTS_ERR_SHAPE;
-  *bytes = 256;
+  const DeviceInfo* di;
+  const int st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  *bytes = attn_workspace(attn_shape(di->sm_count, num_seqs, M, Hq, heads, max_tokens, max_len), M, Hq, head_dim);
   return ATTS_OK;
 }
 
@@ -193,13 +277,11 @@ int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
   if (out_token_stride < 0 || out_head_stride < 0 || out_token_stride % 8 || out_head_stride % 8) return ATTS_ERR_SHAPE;
   if ((M > 0 && !out) || !workspace) return ATTS_ERR_NULL;
   if (!aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, 256)) return ATTS_ERR_ALIGN;
-  size_t need = 0;
-  st = atts_tree_attention_workspace_bytes(cache->num_seqs, M, Hq, cache->heads, cache->head_dim, max_tokens, max_len, &need);
-  if (st != ATTS_OK) return st;
-  if (workspace_bytes < need) return ATTS_ERR_WORKSPACE;
   const DeviceInfo* di;
   st = device_info(&di);
   if (st != ATTS_OK) return st;
+  AttnShape sh = attn_shape(di->sm_count, cache->num_seqs, M, Hq, cache->heads, max_tokens, max_len);
+  if (workspace_bytes < attn_workspace(sh, M, Hq, cache->head_dim)) return ATTS_ERR_WORKSPACE;
   if (M == 0 || cache->num_seqs == 0 || max_tokens == 0) return ATTS_OK;
   a.q = static_cast<const char*>(q);
   a.out = static_cast<char*>(out);
@@ -208,17 +290,25 @@ int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
   a.ctx = ctx_lens; a.cu = cu_tokens; a.pre = pre; a.end = end;
   a.M = (int)M; a.Hq = Hq; a.G = Hq / cache->heads; a.max_tokens = (int)max_tokens; a.max_len = (int)max_len;
   a.scale = scale;
+  sh.p.part_lse = static_cast<float*>(workspace);
+  sh.p.part_o = sh.p.part_lse + round_up((size_t)M * Hq * sh.p.chunks * 4, 256) / 4;
+  sh.p.wait_limit = wait_limit();
+  sh.p.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
+  const int64_t gx = (int64_t)sh.p.nq * sh.p.chunks;
+  if (gx > 0x7FFFFFFF || (int64_t)max_tokens * Hq > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  CUtensorMap mq, mk, mv;
+  if (encode_queries(di, &mq, cache, q, q_token_stride, q_head_stride, M, Hq, sh.p.tpt) != ATTS_OK ||
+      encode_cache(di, &mk, cache, cache->k) != ATTS_OK || encode_cache(di, &mv, cache, cache->v) != ATTS_OK)
+    return ATTS_ERR_CUDA;
+  const dim3 grid((unsigned)gx, (unsigned)cache->heads, (unsigned)cache->num_seqs);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const dim3 grid((unsigned)((max_tokens + 7) / 8), (unsigned)Hq, (unsigned)cache->num_seqs);
   const bool bf = cache->dtype == ATTS_BF16;
-  if (cache->head_dim == 128) {
-    if (bf) tree_attention_simple_kernel<__nv_bfloat16, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
-    else tree_attention_simple_kernel<__half, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
-  } else {
-    if (bf) tree_attention_simple_kernel<__nv_bfloat16, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
-    else tree_attention_simple_kernel<__half, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
-  }
-  return launch_status();
+#define ATTS_ATTEND(D, TWO)                                                                                       \
+  (bf ? launch_attention<__nv_bfloat16, D, TWO>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream)                \
+      : launch_attention<__half, D, TWO>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream))
+  if (cache->head_dim == 128) return sh.two ? ATTS_ATTEND(128, true) : ATTS_ATTEND(128, false);
+  return sh.two ? ATTS_ATTEND(64, true) : ATTS_ATTEND(64, false);
+#undef ATTS_ATTEND
 }
 
 int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,

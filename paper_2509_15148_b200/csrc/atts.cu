@@ -13,6 +13,7 @@
 
 #include "conformal.cuh"
 #include "lmhead_lse.cuh"
+#include "tree_attention.cuh"
 
 namespace atts {
 
@@ -123,6 +124,7 @@ static int device_info(const DeviceInfo** out) {
       ok = ok && cudaFuncSetAttribute(takeover_ids_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kIdsSmemBytes) == cudaSuccess;
       ok = ok && cudaFuncSetAttribute(merge_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, merge_smem) == cudaSuccess;
       ok = ok && cudaFuncSetAttribute(merge_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, merge_smem) == cudaSuccess;
+      ok = ok && attention_attributes() == cudaSuccess;
       if (!ok) {
         cudaGetLastError();
         di.status = ATTS_ERR_CUDA;

@@ -2,6 +2,8 @@
 #pragma once
 #include <math.h>
 
+#include "conformal.cuh"
+#include "lmhead_lse.cuh"
 #include "rope_cache.cuh"
 
 namespace atts {
@@ -32,49 +34,652 @@ __device__ __forceinline__ bool seq_view(const int32_t* cu, const int32_t* ctx, 
   return ok;
 }
 
-// One warp per (token, query head); lanes share the channels.
-template <typename T, int D>
-__global__ void __launch_bounds__(256)
-tree_attention_simple_kernel(const AttnArgs a, unsigned* __restrict__ dev_status) {
-  const int seq = blockIdx.z;
-  SeqView s;
-  if (!seq_view(a.cu, a.ctx, seq, a.M, a.max_tokens, a.max_len, s, dev_status, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0)) return;
-  const int t = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, h = blockIdx.y;
-  if (t >= s.n) return;
-  const int64_t token = s.first + t;
-  const int mine = a.pre ? a.pre[token] : t;
-  constexpr int E = D / 32;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
-  for (int e = 0; e < E; ++e) {
-    q[e] = Pack<T>::get(reinterpret_cast<const T*>(a.q)[token * a.q_ts + h * a.q_hs + lane * E + e]);
-    o[e] = 0.f;
+// ------------------------------------------------------------------------------------------------------------------
+// PTX wrappers beyond those of lmhead_lse.cuh
+// ------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem], the A operand packed two 16-bit values to a tensor-memory column.
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Descriptor of an operand whose M/N dimension is contiguous: blocks of 64 elements (128 bytes, 128-byte swizzle) `lbo`
+// bytes apart, groups of eight K rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t umma_smem_desc_mn(uint32_t smem_addr, uint32_t lbo) {
+  return (umma_smem_desc(smem_addr) & ~(0x3FFFull << 16)) | ((uint64_t)(lbo >> 4) << 16);
+}
+#define ATTS_TMEM_ST_16(taddr, v)                                                                                          \
+  asm volatile(                                                                                                            \
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "                                                                      \
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),                              \
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),         \
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])                                                \
+      : "memory")
+#define ATTS_TMEM_ST_32(taddr, v)                                                                                          \
+  do {                                                                                                                     \
+    ATTS_TMEM_ST_16(taddr, v);                                                                                             \
+    ATTS_TMEM_ST_16((taddr) + 16u, (&v[16]));                                                                              \
+  } while (0)
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ------------------------------------------------------------------------------------------------------------------
+// Tree attention.  A CTA takes tiles of 128 rows (the query heads of one key head for 128 / G tokens: grouped heads share
+// the keys and values that are read) against the slots of its sequence, 128 at a time:
+//   S = Q K^T (tcgen05, fp32 in tensor memory) -> one thread per row: running maximum, p = 2^(c s - c m), sum
+//   -> p rounded to the inputs' type, back into tensor memory over S -> O += P V (A operand from tensor memory).
+// Two streams of this alternate on the tensor pipe, so that one's products hide the other's exponentials:
+//   TWO: two row tiles against the same slots;  otherwise: one row tile, even and odd slot tiles, joined at the end.
+// The running maximum that p refers to only moves when a row exceeds it by 2^8: p <= 256 and sums stay exact in fp32, and
+// O is rescaled (a pass over tensor memory) in a few tiles instead of in every one.
+// The slots may be cut into chunks of `chunk` tiles over CTAs (few rows, long caches); the parts are then joined by
+// attention_join_kernel.
+//
+// Warps: 0 loads (TMA, one box per page and 64 channels), 1 issues the products, 2 clears the values of slots that hold
+// nothing (whatever lies there, 0 * NaN must not reach O), 4-7 and 8-11 the two streams' rows.
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kAttnThreads = 384;
+constexpr int kAttnTile = 128;          // rows of a tile, slots of a tile
+constexpr int kAttnTreeTiles = 1024;    // tiles behind the cached part whose visibility is looked up ahead
+
+template <int D, bool TWO>
+struct AttnCfg {
+  static constexpr int kTileBytes = kAttnTile * D * 2;
+  static constexpr int kQBytes = (TWO ? 2 : 1) * kTileBytes;
+  static constexpr int kStages = D == 128 ? (TWO ? 4 : 5) : 8;
+  static constexpr int kRing = kQBytes;                              // byte offsets in (aligned) shared memory
+  static constexpr int kMask = kRing + kStages * kTileBytes;         // [2 streams][2][128] int2
+  static constexpr int kFlags = kMask + 4 * kAttnTile * 8;
+  static constexpr int kStats = kFlags + kAttnTreeTiles;             // [128] float2: maximum and sum of the odd stream
+  static constexpr int kBars = kStats + kAttnTile * 8;
+  static constexpr int kSmemBytes = kBars + 256 + 1024;
+  static constexpr int kLead = TWO ? 1 : 2;                          // key tiles loaded ahead of the first value tile
+  static_assert(kSmemBytes <= 232448, "shared memory of one SM");
+  static_assert(kStages * kTileBytes >= kAttnTile * (D + 4) * 4, "the odd stream's sums are joined through the ring");
+};
+
+enum : uint32_t { kTileMasked = 1, kTileFull = 2, kTileDead = 4 };  // some / all pairs visible; some slots hold nothing
+
+struct AttnPlan {
+  int chunk;        // slot tiles per CTA
+  int nq, chunks;   // row tiles (or pairs of them) and chunks of the longest sequence
+  int tpt;          // tokens per row tile
+  float* part_o;    // [M * Hq][chunks][D]
+  float* part_lse;  // [M * Hq][chunks], base 2
+  long long wait_limit;
+  int withhold_loads;
+};
+
+template <typename T>
+struct AttnType;
+template <>
+struct AttnType<__nv_bfloat16> { static constexpr uint32_t fmt = 1; static constexpr float shift = 0.f; };
+// fp16 probabilities are carried 2^6 larger (they stay below 2^14): those under 2^-14 would lose digits otherwise.
+template <>
+struct AttnType<__half> { static constexpr uint32_t fmt = 0; static constexpr float shift = 6.f; };
+
+// What slots of a tile hold, as the interval of preorder places that see them: mine is in it iff
+// (unsigned)(mine - x) < (unsigned)y.
+__device__ __forceinline__ int2 slot_interval(const AttnArgs& a, const SeqView& s, int slot) {
+  if (slot < s.ctx && slot < s.len) return make_int2(0, 0x7FFFFFFF);
+  if (slot >= s.len) return make_int2(0, 0);
+  const int j = slot - s.ctx;
+  if (!a.pre) return make_int2(j, 0x7FFFFFFF);
+  const int lo = a.pre[s.first + j], hi = a.end[s.first + j];
+  return (lo < 0 || hi <= lo) ? make_int2(0, 0) : make_int2(lo, hi - lo);
+}
+
+// Visibility of one tile behind the cached part for rows whose places span [qmin, qmax] (whole warp).
+__device__ __forceinline__ uint32_t tile_flags(const AttnArgs& a, const SeqView& s, int tile, int qmin, int qmax, int lane) {
+  bool any = false, all = true, dead = false;
+#pragma unroll
+  for (int e = 0; e < kAttnTile / 32; ++e) {
+    const int2 v = slot_interval(a, s, tile * kAttnTile + e * 32 + lane);
+    const unsigned last = (unsigned)v.x + (unsigned)v.y;    // one past the interval
+    const bool none = v.y == 0;
+    any |= !none && v.x <= qmax && (unsigned)qmin < last;
+    all &= !none && v.x <= qmin && (unsigned)qmax < last;
+    dead |= none;
   }
-  for (int slot = 0; slot < s.len && mine >= 0; ++slot) {
-    if (slot >= s.ctx) {
-      const int j = slot - s.ctx;
-      const bool see = a.pre ? (a.pre[s.first + j] >= 0 && a.pre[s.first + j] <= mine && mine < a.end[s.first + j]) : j <= t;
-      if (!see) continue;
+  any = __any_sync(0xFFFFFFFFu, any);
+  all = __all_sync(0xFFFFFFFFu, all);
+  dead = __any_sync(0xFFFFFFFFu, dead);
+  return !any ? 0u : (all ? kTileFull : kTileMasked) | (dead ? kTileDead : 0u);
+}
+
+// Loads one row tile's 32 columns, scales by the row's factor, stores them back.
+template <int D>
+__device__ __forceinline__ void rescale_o(uint32_t taddr, float f) {
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) {
+    uint32_t v[32];
+    ATTS_TMEM_LD_32(taddr + 32u * j, v);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+    ATTS_TMEM_ST_32(taddr + 32u * j, v);
+  }
+  tmem_st_wait();
+}
+
+template <typename T, int D, bool TWO>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a,
+                      const __grid_constant__ AttnPlan plan, unsigned* __restrict__ dev_status) {
+  using Cfg = AttnCfg<D, TWO>;
+  constexpr int kStages = Cfg::kStages;
+  constexpr int kLead = Cfg::kLead;
+  extern __shared__ uint8_t smem_raw[];
+  const int seq = blockIdx.z, hk = blockIdx.y;
+  const int qt = plan.nq - 1 - (int)(blockIdx.x % plan.nq), chunk = blockIdx.x / plan.nq;   // late rows see most: first
+
+  // ---- what this CTA works on: nothing at all, or rows [tok0, tok0 + ntok) and slot tiles [tile0, tile1) ----
+  SeqView s;
+  if (!seq_view(a.cu, a.ctx, seq, a.M, a.max_tokens, a.max_len, s, dev_status, threadIdx.x == 0 && blockIdx.x == 0 && hk == 0)) return;
+  const int per = plan.tpt * (TWO ? 2 : 1);
+  const int tok0 = qt * per;
+  if (tok0 >= s.n) return;
+  const int ntok = min(per, s.n - tok0);
+  const int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
+  const int tile0 = chunk * plan.chunk, tile1 = min(ntiles, tile0 + plan.chunk);
+  if (chunk > 0 && tile0 >= ntiles) return;
+  const bool two = TWO && ntok > plan.tpt;
+  const int tree0 = min(s.ctx / kAttnTile, ntiles);   // first tile that is not all cached slots
+
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
+  int2* mask = reinterpret_cast<int2*>(smem + Cfg::kMask);
+  uint8_t* flags = smem + Cfg::kFlags;
+  float2* stats = reinterpret_cast<float2*>(smem + Cfg::kStats);
+  const uint32_t bar0 = smem_base + Cfg::kBars;
+  auto full_bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+  auto empty_bar = [&](int i) { return bar0 + 8u * (uint32_t)(kStages + i); };
+  const uint32_t q_bar = bar0 + 8u * (2 * kStages), clean_bar = q_bar + 8u;
+  auto s_bar = [&](int i) { return clean_bar + 8u + 8u * (uint32_t)i; };
+  auto p_bar = [&](int i) { return clean_bar + 24u + 8u * (uint32_t)i; };
+  auto o_bar = [&](int i) { return clean_bar + 40u + 8u * (uint32_t)i; };
+  auto m_bar = [&](int i) { return clean_bar + 56u + 8u * (uint32_t)i; };
+  const uint32_t join_bar = clean_bar + 72u, dirty_bar = clean_bar + 80u;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kBars + 8 * (2 * kStages + 12));
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  volatile int* range = reinterpret_cast<volatile int*>(tmem_slot + 2);   // smallest and largest place of the rows
+  volatile int* clear_stage = range + 2;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&map_q);
+    prefetch_tmap(&map_k);
+    prefetch_tmap(&map_v);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(full_bar(i), 1);
+      mbar_init(empty_bar(i), 1);
     }
-    const int page = cache_page(a.cache, seq, slot, dev_status);
-    float x = 0.f, v[E];
-    for (int e = 0; e < E; ++e) v[e] = 0.f;
-    if (page >= 0) {
-      const int64_t at = cache_offset(a.cache, page, slot) + (h / a.G) * a.cache.head_stride + lane * E;
-      for (int e = 0; e < E; ++e) {
-        x += q[e] * Pack<T>::get(reinterpret_cast<const T*>(a.cache.k)[at + e]);
-        v[e] = Pack<T>::get(reinterpret_cast<const T*>(a.cache.v)[at + e]);
+    mbar_init(q_bar, 1);
+    mbar_init(clean_bar, 1);
+    mbar_init(dirty_bar, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_bar(i), 1);
+      mbar_init(p_bar(i), 4);
+      mbar_init(o_bar(i), 1);
+      mbar_init(m_bar(i), 4);
+    }
+    mbar_init(join_bar, 4);
+    *abort_flag = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"((uint32_t)kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp == 2) {
+    int lo = 0x7FFFFFFF, hi = -1;
+    for (int t = lane; t < ntok; t += 32) {
+      const int p = a.pre ? a.pre[s.first + tok0 + t] : tok0 + t;
+      if (p >= 0) lo = min(lo, p);
+      hi = max(hi, p);
+    }
+    lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+    hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+    if (lane == 0) {
+      range[0] = lo;
+      range[1] = hi;
+    }
+  }
+  __syncthreads();
+  {
+    // all rows padding: qmax is -1 and no tile is visible
+    const int qmin = range[0], qmax = range[1];
+    const int t0 = max(tile0, tree0), t1 = min(tile1, tree0 + kAttnTreeTiles);
+    for (int t = t0 + warp; t < t1; t += kAttnThreads / 32) {
+      const uint32_t f = qmax < 0 ? 0u : tile_flags(a, s, t, qmin, qmax, lane);
+      if (lane == 0) flags[t - tree0] = (uint8_t)f;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const bool rows_live = range[1] >= 0;
+  auto flags_of = [&](int t) -> uint32_t {
+    if (t < tree0) return rows_live ? kTileFull : 0u;
+    return t - tree0 < kAttnTreeTiles ? flags[t - tree0] : rows_live ? (uint32_t)(kTileMasked | kTileDead) : 0u;
+  };
+  int ntile = 0;  // visible tiles
+  for (int t = tile0; t < tile1; ++t) {
+    if (t < tree0) {
+      const int e = min(tile1, tree0);
+      ntile += rows_live ? e - t : 0;
+      t = e - 1;
+    } else {
+      ntile += flags_of(t) != 0u;
+    }
+  }
+  auto next_tile = [&](int t) {  // the first visible tile from t on
+    while (t < tile1 && flags_of(t) == 0u) ++t;
+    return t;
+  };
+  const long long limit = plan.wait_limit;
+  auto wait_one = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, limit, 0u); };
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait_one(bar, parity)) != 0; };
+
+  if (warp == 0) {
+    // ---------------- loads, in the order in which they are used: K_0 .. K_{lead-1}, then V_i, K_{i+lead} ----------------
+    const int pl = a.cache.page_log2;
+    const int rows = min(1 << pl, kAttnTile);                 // slots of a box
+    const int boxes = (kAttnTile / rows) * (D / 64);          // <= 32
+    const int bslot = (lane / (D / 64)) * rows, bcol = (lane % (D / 64)) * 64;
+    const uint32_t bdst = (uint32_t)(bcol / 64) * (kAttnTile * 128) + (uint32_t)bslot * 128u;
+    auto page_of = [&](int t) -> int {
+      if (lane >= boxes || t >= tile1) return 0;
+      const int slot = t * kAttnTile + bslot;
+      if (slot >= s.len) return a.cache.num_pages;            // out of the map: filled with zeros
+      const int page = cache_page(a.cache, seq, slot, dev_status);
+      return page < 0 ? a.cache.num_pages : page;
+    };
+    if (!plan.withhold_loads && ntile > 0) {
+      if (lane == 0) {
+        mbar_expect_tx(q_bar, (uint32_t)((two ? 2 : 1) * a.G * plan.tpt * D * 2));
+        for (int i = 0; i < (two ? 2 : 1); ++i)
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_3d(smem_base + (uint32_t)i * Cfg::kTileBytes + (uint32_t)c * (kAttnTile * 128), &map_q, q_bar, c * 64, hk * a.G,
+                        s.first + tok0 + i * plan.tpt);
+      }
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      auto load = [&](const CUtensorMap* map, int t, int page) {
+        ok = wait_warp(empty_bar(stage), phase ^ 1u);
+        if (!ok) return;
+        if (lane == 0) mbar_expect_tx(full_bar(stage), Cfg::kTileBytes);
+        __syncwarp();
+        if (lane < boxes)
+          tma_load_4d(smem_base + Cfg::kRing + (uint32_t)stage * Cfg::kTileBytes + bdst, map, full_bar(stage), bcol,
+                      (t * kAttnTile + bslot) & ((1 << pl) - 1), hk, page);
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      };
+      int tk = next_tile(tile0), tv = tk;
+      int pk = page_of(tk), pv = pk;
+      for (int i = 0; i < kLead && tk < tile1 && ok; ++i) {
+        const int nt = next_tile(tk + 1), np = page_of(nt);
+        load(&map_k, tk, pk);
+        tk = nt; pk = np;
+      }
+      while (tv < tile1 && ok) {
+        const int nv = next_tile(tv + 1), npv = page_of(nv);
+        load(&map_v, tv, pv);
+        tv = nv; pv = npv;
+        if (tk < tile1 && ok) {
+          const int nt = next_tile(tk + 1), np = page_of(nt);
+          load(&map_k, tk, pk);
+          tk = nt; pk = np;
+        }
       }
     }
-    for (int i = 16; i > 0; i >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, i);
-    x *= a.scale;
-    const float mn = fmaxf(m, x), keep = expf(m - mn), p = expf(x - mn);
-    l = l * keep + p;
-    for (int e = 0; e < E; ++e) o[e] = o[e] * keep + p * v[e];
-    m = mn;
+  } else if (warp == 1) {
+    // ---------------- products ----------------
+    if (lane == 0 && ntile > 0) {
+      constexpr uint32_t kFmt = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24);
+      constexpr uint32_t kIdescS = kFmt | ((uint32_t)(kAttnTile >> 3) << 17);
+      constexpr uint32_t kIdescO = kFmt | (1u << 16) | ((uint32_t)(D >> 3) << 17);   // B with its N dimension contiguous
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = wait_one(q_bar, 0);
+      uint32_t p_phase[2] = {0, 0}, clean_phase = 0;
+      auto advance = [&]() {
+        umma_commit(empty_bar(stage));
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      };
+      auto qk = [&](int i) {   // S_i = Q (of stream i if TWO) K^T of the ring's present tile
+        const uint32_t sa = smem_base + (TWO ? (uint32_t)i * Cfg::kTileBytes : 0u);
+        const uint32_t sb = smem_base + Cfg::kRing + (uint32_t)stage * Cfg::kTileBytes;
+        const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sb);
+#pragma unroll
+        for (int k = 0; k < D / kUmmaK; ++k) {
+          const uint64_t at = (uint64_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2);
+          umma_bf16(tmem_base + (uint32_t)i * kAttnTile, da + at, db + at, kIdescS, (uint32_t)(k != 0));
+        }
+        umma_commit(s_bar(i));
+      };
+      auto next_k = [&]() {    // products of the next key tile, for the streams that use it
+        ok = ok && wait_one(full_bar(stage), phase);
+        if (!ok) return;
+        tc_fence_after();
+      };
+      int tv = next_tile(tile0);
+      int lead = min(kLead, ntile), ik = 0;
+      for (; ik < lead && ok; ++ik) {
+        next_k();
+        if (!ok) break;
+        if (TWO) {
+          qk(0);
+          if (two) qk(1);
+        } else {
+          qk(ik & 1);
+        }
+        advance();
+      }
+      for (int i = 0; i < ntile && ok; ++i) {
+        ok = wait_one(full_bar(stage), phase);
+        if (ok && (flags_of(tv) & kTileDead)) {   // hand the stage to warp 2 and wait until it has been cleared
+          *clear_stage = stage;
+          mbar_arrive(dirty_bar);
+          ok = wait_one(clean_bar, clean_phase);
+          clean_phase ^= 1u;
+        }
+        if (!ok) break;
+        tc_fence_after();
+        const int vstage = stage;
+        const bool more = ik < ntile;
+        const int kstage = stage + 1 == kStages ? 0 : stage + 1;
+        const uint32_t kphase = stage + 1 == kStages ? phase ^ 1u : phase;
+        const int streams = TWO ? (two ? 2 : 1) : 1;
+        for (int u = 0; u < streams && ok; ++u) {
+          const int st = TWO ? u : i & 1;
+          ok = wait_one(p_bar(st), p_phase[st]);
+          if (!ok) break;
+          p_phase[st] ^= 1u;
+          tc_fence_after();
+          const uint64_t db = umma_smem_desc_mn(smem_base + Cfg::kRing + (uint32_t)vstage * Cfg::kTileBytes, kAttnTile * 128);
+          const bool first = TWO ? i == 0 : i < 2;
+#pragma unroll
+          for (int k = 0; k < kAttnTile / kUmmaK; ++k)
+            umma_ts(tmem_base + 256u + (uint32_t)st * D, tmem_base + (uint32_t)st * kAttnTile + 8u * k, db + (uint64_t)(k * (kUmmaK * 128 / 16)),
+                    kIdescO, (uint32_t)(!first || k != 0));
+          umma_commit(o_bar(st));
+          if (u + 1 == streams) umma_commit(empty_bar(vstage));
+          if (more) {
+            if (u == 0) {
+              ok = wait_one(full_bar(kstage), kphase);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            const int keep = stage;
+            stage = kstage;
+            qk(st);
+            stage = keep;
+            if (u + 1 == streams) umma_commit(empty_bar(kstage));
+          }
+        }
+        if (!ok) break;
+        for (int u = 0; u < (more ? 2 : 1); ++u)
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        ik += more ? 1 : 0;
+        tv = next_tile(tv + 1);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // ---------------- values of slots that hold nothing ----------------
+    int t = next_tile(tile0);
+    uint32_t dirty_phase = 0;
+    for (int i = 0; i < ntile; ++i, t = next_tile(t + 1)) {
+      if (!(flags_of(t) & kTileDead)) continue;
+      if (!wait_warp(dirty_bar, dirty_phase)) break;
+      dirty_phase ^= 1u;
+      uint8_t* v = smem + Cfg::kRing + *clear_stage * Cfg::kTileBytes;
+      for (int e = 0; e < kAttnTile / 32; ++e) {
+        const int row = e * 32 + lane;
+        if (slot_interval(a, s, t * kAttnTile + row).y != 0) continue;
+        for (int c = 0; c < D / 64; ++c)
+          for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(v + c * (kAttnTile * 128) + row * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(clean_bar);
+    }
+  } else if (warp >= 4) {
+    // ---------------- rows ----------------
+    const int st = (warp - 4) >> 2;                    // stream
+    const int quarter = warp & 3;
+    const int row = quarter * 32 + lane;
+    const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_s = tmem_base + lane_base + (uint32_t)st * kAttnTile, t_o = tmem_base + lane_base + 256u + (uint32_t)st * D;
+    const int tok = (TWO ? st * plan.tpt : 0) + row / a.G;           // within the CTA's tokens
+    const bool in = row < plan.tpt * a.G && tok < ntok;
+    const bool warp_in = __any_sync(0xFFFFFFFFu, in);
+    const int64_t token = (int64_t)s.first + tok0 + tok;
+    const int head = hk * a.G + row % a.G;
+    const int mine = !in ? -1 : a.pre ? a.pre[token] : tok0 + tok;
+    const float c = a.scale * 1.4426950408889634f;
+    float m = -INFINITY, l = 0.f;
+    int done = 0;                                      // tiles of this stream so far
+    uint32_t masked = 0;
+    bool ok = true;
+    const bool active = TWO ? (st == 0 || two) : true;
+    int t = next_tile(tile0);
+    for (int i = 0; i < ntile && ok && active; ++i, t = next_tile(t + 1)) {
+      if (!TWO && (i & 1) != st) continue;
+      const uint32_t f = flags_of(t);
+      int2* mk = mask + (st * 2 + (masked & 1u)) * kAttnTile;
+      if (f & kTileMasked) {
+        mk[row] = slot_interval(a, s, t * kAttnTile + row);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(m_bar(st));
+      }
+      ok = wait_warp(s_bar(st), (uint32_t)done & 1u);
+      if (ok && (f & kTileMasked)) {
+        ok = wait_warp(m_bar(st), masked & 1u);
+        ++masked;
+      }
+      if (!ok) break;
+      tc_fence_after();
+      if (warp_in) {
+        uint32_t v[128];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ATTS_TMEM_LD_32(t_s + 32u * j, (&v[32 * j]));
+        tmem_ld_wait();
+        if (f & kTileMasked) {
+#pragma unroll
+          for (int j = 0; j < 128; j += 2) {
+            const int4 w = *reinterpret_cast<const int4*>(mk + j);
+            if ((unsigned)(mine - w.x) >= (unsigned)w.y) v[j] = 0xFF800000u;
+            if ((unsigned)(mine - w.z) >= (unsigned)w.w) v[j + 1] = 0xFF800000u;
+          }
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 128; j += 4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], __uint_as_float(v[j + e]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        // the reference moves when a row's maximum passes it by more than 8 (base 2), and for the first visible slot
+        float keep = 1.f;
+        if ((top - m) * c > 8.f) {
+          keep = ex2_approx((m - top) * c);     // 0 for m = -inf
+          m = top;
+          l *= keep;
+        }
+        if (done > 0 && __any_sync(0xFFFFFFFFu, keep != 1.f)) {
+          ok = wait_warp(o_bar(st), (uint32_t)(done - 1) & 1u);
+          if (!ok) break;
+          tc_fence_after();
+          rescale_o<D>(t_o, keep);
+        }
+        const float off = (m == -INFINITY ? 0.f : -m * c) + AttnType<T>::shift;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 128; j += 32) {
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float p0 = ex2_approx(fmaf(__uint_as_float(v[j + e]), c, off));
+            const float p1 = ex2_approx(fmaf(__uint_as_float(v[j + e + 1]), c, off));
+            sum[e & 2] += p0;
+            sum[(e & 2) + 1] += p1;
+            w[e / 2] = Pack<T>::pack(p0, p1);
+          }
+          ATTS_TMEM_ST_16(t_s + (uint32_t)(j / 2), w);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_st_wait();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_bar(st));
+      ++done;
+    }
+    if (active && ok && done > 0) ok = wait_warp(o_bar(st), (uint32_t)(done - 1) & 1u);
+    tc_fence_after();
+    // ---- join of the two streams (one row tile): the odd one hands its sums over through the ring, which is free ----
+    float2 other = make_float2(-INFINITY, 0.f);
+    const bool joined = !TWO && ntile > 1;
+    float* pass = reinterpret_cast<float*>(smem + Cfg::kRing);
+    if (joined && st == 1) {
+      // the ring is free once every product has finished: this stream's last one has, the other's has when it gets here
+      if (ok && ntile > 0) ok = wait_warp(o_bar(0), (uint32_t)((ntile + 1) / 2 - 1) & 1u);
+      if (ok && warp_in) {
+        stats[row] = make_float2(m, l);
+#pragma unroll 1
+        for (int j = 0; j < D / 32; ++j) {
+          uint32_t v[32];
+          ATTS_TMEM_LD_32(t_o + 32u * j, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            *reinterpret_cast<uint4*>(pass + row * (D + 4) + 32 * j + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(join_bar);
+    }
+    if (joined && st == 0 && ok) {
+      ok = wait_warp(join_bar, 0);
+      if (ok && warp_in) other = stats[row];
+    }
+    if (ok && active && warp_in && (TWO || st == 0)) {
+      // o = (O_0 f0 + O_1 f1) / (l_0 f0 + l_1 f1), fk = 2^(c (m_k - max))
+      const float mm = fmaxf(m, other.x);
+      const float f0 = m == -INFINITY ? 0.f : ex2_approx((m - mm) * c), f1 = other.x == -INFINITY ? 0.f : ex2_approx((other.x - mm) * c);
+      const float sum = l * f0 + other.y * f1;
+      const bool empty = mine < 0 || !(sum > 0.f);
+      const float g0 = empty ? 0.f : f0 / sum, g1 = empty ? 0.f : f1 / sum;
+      const float lse2 = empty ? -INFINITY : mm * c - AttnType<T>::shift + log2f(sum);
+      const int parts = (ntiles + plan.chunk - 1) / plan.chunk;
+      const int64_t r = token * a.Hq + head;
+      T* out = reinterpret_cast<T*>(a.out) + token * a.o_ts + (int64_t)head * a.o_hs;
+      float* part = plan.part_o + (r * plan.chunks + chunk) * D;
+      if (in) {
+        if (parts > 1) plan.part_lse[r * plan.chunks + chunk] = lse2;
+        else if (a.lse) a.lse[r] = lse2 * 0.6931471805599453f;
+      }
+#pragma unroll 1
+      for (int j = 0; j < D / 32; ++j) {
+        uint32_t v[32];
+        if (done > 0) {
+          ATTS_TMEM_LD_32(t_o + 32u * j, v);
+          tmem_ld_wait();
+        }
+        float o[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = empty || done == 0 ? 0.f : __uint_as_float(v[i]) * g0;
+        if (joined && !empty) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(pass + row * (D + 4) + 32 * j + i);
+            o[i] += x.x * g1; o[i + 1] += x.y * g1; o[i + 2] += x.z * g1; o[i + 3] += x.w * g1;
+          }
+        }
+        if (in) {
+          if (parts > 1) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + 32 * j + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+              *reinterpret_cast<uint4*>(out + 32 * j + i) = make_uint4(Pack<T>::pack(o[i], o[i + 1]), Pack<T>::pack(o[i + 2], o[i + 3]),
+                                                                      Pack<T>::pack(o[i + 4], o[i + 5]), Pack<T>::pack(o[i + 6], o[i + 7]));
+          }
+        }
+      }
+    }
   }
-  for (int e = 0; e < E; ++e)
-    reinterpret_cast<T*>(a.out)[token * a.o_ts + h * a.o_hs + lane * E + e] = Pack<T>::put(l > 0.f ? o[e] / l : 0.f);
-  if (a.lse && lane == 0) a.lse[token * a.Hq + h] = l > 0.f ? m + logf(l) : -INFINITY;
+
+  // ---------------- teardown ----------------
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    // A wait expired.  Record it, give copies and products still in flight time to land, then free tensor memory.
+    if (threadIdx.x == 0) atomicOr(dev_status, 2u);
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)kTmemCols) : "memory");
+  }
+}
+
+// Joins the chunks of a row: o = sum_c o_c 2^(lse_c - max) / sum_c 2^(lse_c - max), one warp per row, chunks in order.
+template <typename T, int D>
+__global__ void __launch_bounds__(256)
+attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnPlan plan) {
+  pdl_wait();
+  const int seq = blockIdx.y;
+  SeqView s;
+  unsigned none;
+  if (!seq_view(a.cu, a.ctx, seq, a.M, a.max_tokens, a.max_len, s, &none, false)) return;
+  const int64_t r = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (r >= (int64_t)s.n * a.Hq) return;
+  const int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
+  const int parts = (ntiles + plan.chunk - 1) / plan.chunk;
+  if (parts <= 1) return;
+  const int64_t row = (int64_t)s.first * a.Hq + r;
+  const float* lse = plan.part_lse + row * plan.chunks;
+  float top = -INFINITY;
+  for (int i = lane; i < parts; i += 32) top = fmaxf(top, lse[i]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  constexpr int E = D / 32;
+  float o[E], sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int i = 0; i < parts; ++i) {
+    const float w = lse[i] == -INFINITY ? 0.f : ex2_approx(lse[i] - top);
+    if (w == 0.f) continue;
+    sum += w;
+    const float* p = plan.part_o + (row * plan.chunks + i) * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += w * p[e];
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const int64_t token = row / a.Hq;
+  const int head = (int)(row - token * a.Hq);
+  uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + token * a.o_ts + (int64_t)head * a.o_hs + lane * E);
+#pragma unroll
+  for (int e = 0; e < E; e += 2) out[e / 2] = Pack<T>::pack(o[e] * inv, o[e + 1] * inv);
+  if (a.lse && lane == 0) a.lse[row] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
 struct WeightArgs {
@@ -126,6 +731,22 @@ cache_weights_simple_kernel(const WeightArgs a, unsigned* __restrict__ dev_statu
     }
   }
   if (lane == 0) a.wout[at_w] = (a.win ? a.win[at_w] : 0.f) + sum;
+}
+
+// Opt-in shared memory of the kernels above (once per device).
+template <typename T, int D>
+static cudaError_t attention_attributes_of() {
+  cudaError_t e = cudaFuncSetAttribute(tree_attention_kernel<T, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, true>::kSmemBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(tree_attention_kernel<T, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, false>::kSmemBytes);
+  return e;
+}
+static cudaError_t attention_attributes() {
+  cudaError_t e = attention_attributes_of<__nv_bfloat16, 128>();
+  if (e == cudaSuccess) e = attention_attributes_of<__nv_bfloat16, 64>();
+  if (e == cudaSuccess) e = attention_attributes_of<__half, 128>();
+  if (e == cudaSuccess) e = attention_attributes_of<__half, 64>();
+  return e;
 }
 
 }  // namespace atts
