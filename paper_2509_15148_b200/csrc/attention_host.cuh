@@ -136,6 +136,27 @@ static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const 
   return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
 }
 
+template <typename T, int D>
+static int launch_weights(const CUtensorMap& mq, const CUtensorMap& mk, const WeightArgs& a, dim3 grid, unsigned* status, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kWeightThreads);
+  cfg.dynamicSmemBytes = WeightCfg<D>::kSmemBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)a.cluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.cluster > 1 ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, cache_weights_kernel<T, D>, mq, mk, a, status) != cudaSuccess) {
+    cudaGetLastError();
+    return ATTS_ERR_CUDA;
+  }
+  return ATTS_OK;
+}
+
 }  // namespace atts
 
 using namespace atts;
@@ -316,7 +337,7 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
                        const int32_t* end, int64_t M, int32_t Hq, int64_t max_tokens, int64_t max_len, float scale,
                        const float* weights_in, float* weights_out, int64_t weights_cols, void* cuda_stream) {
   WeightArgs a;
-  int st = cache_view(cache, &a.cache);
+  int st = cache_view(cache, &a.q.cache);
   if (st != ATTS_OK) return st;
   st = check_queries(q, q_token_stride, q_head_stride, cache, ctx_lens, cu_tokens, pre, end, M, Hq, max_tokens, max_len, scale);
   if (st != ATTS_OK) return st;
@@ -327,24 +348,34 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
   st = device_info(&di);
   if (st != ATTS_OK) return st;
   if (cache->num_seqs == 0 || max_len == 0) return ATTS_OK;
-  a.q = static_cast<const char*>(q);
+  const int G = Hq / cache->heads;
+  a.q.q = static_cast<const char*>(q);
+  a.q.out = nullptr;
+  a.q.lse = nullptr;
+  a.q.q_ts = q_token_stride; a.q.q_hs = q_head_stride; a.q.o_ts = 0; a.q.o_hs = 0;
+  a.q.ctx = ctx_lens; a.q.cu = cu_tokens; a.q.pre = pre; a.q.end = end;
+  a.q.M = (int)M; a.q.Hq = Hq; a.q.G = G; a.q.max_tokens = (int)max_tokens; a.q.max_len = (int)max_len;
+  a.q.scale = scale;
   a.lse = lse;
-  a.q_ts = q_token_stride; a.q_hs = q_head_stride;
-  a.ctx = ctx_lens; a.cu = cu_tokens; a.pre = pre; a.end = end;
-  a.M = (int)M; a.Hq = Hq; a.G = Hq / cache->heads; a.max_tokens = (int)max_tokens; a.max_len = (int)max_len;
-  a.scale = scale;
   a.win = weights_in; a.wout = weights_out; a.wcols = weights_cols;
+  a.tpt = kAttnTile / G;
+  a.wait_limit = wait_limit();
+  a.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
+  // a cluster's CTAs take at least two row tiles each
+  const int64_t nq = (max_tokens + a.tpt - 1) / a.tpt;
+  a.cluster = 1;
+  while (a.cluster < kWeightMaxCluster && nq >= 4 * a.cluster) a.cluster *= 2;
+  const int64_t gx = (max_len + kAttnTile - 1) / kAttnTile * a.cluster;
+  const dim3 grid((unsigned)gx, (unsigned)cache->heads, (unsigned)cache->num_seqs);
+  CUtensorMap mq, mk;
+  // without queries (M == 0) the kernel only writes; the map then describes the cache's keys and is not used
+  if (encode_queries(di, &mq, cache, M > 0 ? q : cache->k, q_token_stride, q_head_stride, M > 0 ? M : 1, M > 0 ? Hq : cache->heads, a.tpt) != ATTS_OK ||
+      encode_cache(di, &mk, cache, cache->k) != ATTS_OK)
+    return ATTS_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const dim3 grid((unsigned)((max_len + 7) / 8), (unsigned)cache->heads, (unsigned)cache->num_seqs);
   const bool bf = cache->dtype == ATTS_BF16;
-  if (cache->head_dim == 128) {
-    if (bf) cache_weights_simple_kernel<__nv_bfloat16, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
-    else cache_weights_simple_kernel<__half, 128><<<grid, 256, 0, stream>>>(a, di->dev_status);
-  } else {
-    if (bf) cache_weights_simple_kernel<__nv_bfloat16, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
-    else cache_weights_simple_kernel<__half, 64><<<grid, 256, 0, stream>>>(a, di->dev_status);
-  }
-  return launch_status();
+  if (cache->head_dim == 128) return bf ? launch_weights<__nv_bfloat16, 128>(mq, mk, a, grid, di->dev_status, stream) : launch_weights<__half, 128>(mq, mk, a, grid, di->dev_status, stream);
+  return bf ? launch_weights<__nv_bfloat16, 64>(mq, mk, a, grid, di->dev_status, stream) : launch_weights<__half, 64>(mq, mk, a, grid, di->dev_status, stream);
 }
 
 int atts_cache_select(const float* weights, int64_t weights_cols, const int32_t* lens, int64_t num_seqs, int32_t heads,

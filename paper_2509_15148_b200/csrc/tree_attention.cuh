@@ -683,54 +683,298 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
 }
 
 struct WeightArgs {
-  const char* q;
+  AttnArgs q;              // out and lse unused
   const float* lse;
-  int64_t q_ts, q_hs;
-  const int32_t *ctx, *cu, *pre, *end;
-  int M, Hq, G, max_tokens, max_len;
-  float scale;
   const float* win;
   float* wout;
   int64_t wcols;
-  CacheView cache;
+  int tpt, cluster;        // tokens per row tile, CTAs that share a slot tile's queries
+  long long wait_limit;
+  int withhold_loads;
 };
 
-// One warp per (slot, key head).
+// ------------------------------------------------------------------------------------------------------------------
+// Attention weight per slot.  A CTA takes one tile of 128 slots of one key head and goes over row tiles of queries:
+//   S^T = K Q^T (tcgen05, fp32 in tensor memory), a thread per slot, and each thread adds 2^(c s - lse2) over the columns
+// of its own row: no sum crosses threads, so the order is fixed and nothing is stored but one number per slot.  Even and
+// odd row tiles go to two groups of four warps with an accumulator each, and two CTAs share an SM: the exponentials (one
+// per visible pair, 16 a clock and SM) are what the time goes to.  Long query lists are dealt to the CTAs of a cluster,
+// whose first one adds up their sums in order through the cluster's shared memory.
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kWeightThreads = 320;     // warp 0 loads, warp 1 products, 2-5 and 6-9 slots
+constexpr int kWeightTiles = 512;       // row tiles of a CTA whose visibility is looked up ahead
+constexpr int kWeightMaxCluster = 8;
+
+template <int D>
+struct WeightCfg {
+  static constexpr int kTileBytes = kAttnTile * D * 2;
+  static constexpr int kQ = kTileBytes;                            // two stages
+  static constexpr int kCols = kQ + 2 * kTileBytes;                // [2 streams][2][128] lse2, then places
+  static constexpr int kFlags = kCols + 2 * 4 * kAttnTile * 4;
+  static constexpr int kSums = kFlags + kWeightTiles;              // [cluster][128] sums, [128] of the odd stream
+  static constexpr int kBars = kSums + (kWeightMaxCluster + 1) * kAttnTile * 4;
+  static constexpr int kSmemBytes = kBars + 128 + 1024;
+};
+
 template <typename T, int D>
-__global__ void __launch_bounds__(256)
-cache_weights_simple_kernel(const WeightArgs a, unsigned* __restrict__ dev_status) {
-  const int seq = blockIdx.z;
+__global__ void __launch_bounds__(kWeightThreads, 2)
+cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                     const __grid_constant__ WeightArgs a, unsigned* __restrict__ dev_status) {
+  using Cfg = WeightCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const int ranks = a.cluster, rank = blockIdx.x % ranks, tile = blockIdx.x / ranks, hk = blockIdx.y, seq = blockIdx.z;
   SeqView s;
-  const bool ok = seq_view(a.cu, a.ctx, seq, a.M, a.max_tokens, a.max_len, s, dev_status, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0);
-  const int slot = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31, hk = blockIdx.y;
-  if (slot >= a.max_len) return;
-  const int64_t at_w = ((int64_t)seq * a.cache.heads + hk) * a.wcols + slot;
-  if (!ok || slot >= s.len) {
-    if (lane == 0) a.wout[at_w] = 0.f;
+  const bool ok_seq = seq_view(a.q.cu, a.q.ctx, seq, a.q.M, a.q.max_tokens, a.q.max_len, s, dev_status,
+                               threadIdx.x == 0 && blockIdx.x == 0 && hk == 0);
+  const int slot0 = tile * kAttnTile;
+  float* wout = a.wout + ((int64_t)seq * a.q.cache.heads + hk) * a.wcols;
+  const float* win = a.win ? a.win + ((int64_t)seq * a.q.cache.heads + hk) * a.wcols : nullptr;
+  if (!ok_seq || slot0 >= s.len || s.n == 0) {   // the same for every CTA of a cluster
+    const int slot = slot0 + threadIdx.x;
+    if (rank == 0 && threadIdx.x < kAttnTile && slot < a.q.max_len) wout[slot] = ok_seq && slot < s.len && win ? win[slot] : 0.f;
     return;
   }
-  constexpr int E = D / 32;
-  const int page = cache_page(a.cache, seq, slot, dev_status);
-  float k[E], sum = 0.f;
-  for (int e = 0; e < E; ++e) k[e] = 0.f;
-  if (page >= 0) {
-    const int64_t at = cache_offset(a.cache, page, slot) + hk * a.cache.head_stride + lane * E;
-    for (int e = 0; e < E; ++e) k[e] = Pack<T>::get(reinterpret_cast<const T*>(a.cache.k)[at + e]);
+  const int tpt = a.tpt, nq = (s.n + tpt - 1) / tpt;                 // row tiles; this CTA's are rank, rank + ranks, ...
+  const int mine_n = nq > rank ? (nq - rank + ranks - 1) / ranks : 0;
+  const int ncols = (tpt * a.q.G + 31) & ~31;
+  const bool cached = slot0 + kAttnTile <= s.ctx;
+
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
+  float* col_lse = reinterpret_cast<float*>(smem + Cfg::kCols);
+  int* col_place = reinterpret_cast<int*>(smem + Cfg::kCols + 4 * kAttnTile * 4);
+  uint8_t* flags = smem + Cfg::kFlags;
+  float* sums = reinterpret_cast<float*>(smem + Cfg::kSums);
+  const uint32_t bar0 = smem_base + Cfg::kBars;
+  const uint32_t k_bar = bar0;
+  auto q_full = [&](int i) { return bar0 + 8u + 8u * (uint32_t)i; };
+  auto q_empty = [&](int i) { return bar0 + 24u + 8u * (uint32_t)i; };
+  auto s_full = [&](int i) { return bar0 + 40u + 8u * (uint32_t)i; };
+  auto s_empty = [&](int i) { return bar0 + 56u + 8u * (uint32_t)i; };
+  auto c_bar = [&](int i) { return bar0 + 72u + 8u * (uint32_t)i; };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kBars + 88);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&map_q);
+    prefetch_tmap(&map_k);
+    mbar_init(k_bar, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(q_full(i), 1);
+      mbar_init(q_empty(i), 1);
+      mbar_init(s_full(i), 1);
+      mbar_init(s_empty(i), 4);
+      mbar_init(c_bar(i), 4);
+    }
+    *abort_flag = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  const int j = slot - s.ctx;
-  const int lo = j < 0 ? 0 : a.pre ? a.pre[s.first + j] : j, hi = j < 0 ? 0x7FFFFFFF : a.pre ? a.end[s.first + j] : 0x7FFFFFFF;
-  for (int t = 0; t < s.n; ++t) {
-    const int64_t token = s.first + t;
-    const int mine = a.pre ? a.pre[token] : t;
-    if (mine < 0 || lo < 0 || mine < lo || mine >= hi) continue;
-    for (int g = hk * a.G; g < (hk + 1) * a.G; ++g) {
-      float x = 0.f;
-      for (int e = 0; e < E; ++e) x += k[e] * Pack<T>::get(reinterpret_cast<const T*>(a.q)[token * a.q_ts + g * a.q_hs + lane * E + e]);
-      for (int i = 16; i > 0; i >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, i);
-      sum += expf(x * a.scale - a.lse[token * a.Hq + g]);
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"(256u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // rows of a query tile that no token fills stay zero (a box never writes them)
+  for (int i = threadIdx.x; i < 2 * (D / 64) * (kAttnTile - tpt * a.q.G) * 8; i += kWeightThreads) {
+    const int x = i & 7, r = (i >> 3) % (kAttnTile - tpt * a.q.G), blk = (i >> 3) / (kAttnTile - tpt * a.q.G);
+    *reinterpret_cast<uint4*>(smem + Cfg::kQ + blk * (kAttnTile * 128) + (tpt * a.q.G + r) * 128 + x * 16) = make_uint4(0, 0, 0, 0);
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  // which row tiles see any of these slots, and which see all of them from all rows
+  {
+    int2 v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = slot_interval(a.q, s, slot0 + e * 32 + lane);
+    const int live = s.len - slot0;
+    for (int i = warp; i < min(mine_n, kWeightTiles); i += kWeightThreads / 32) {
+      const int t0 = (rank + i * ranks) * tpt, nt = min(tpt, s.n - t0);
+      int qmin = 0x7FFFFFFF, qmax = -1;
+      bool whole = nt == tpt;
+      for (int t = lane; t < nt; t += 32) {
+        const int p = a.q.pre ? a.q.pre[s.first + t0 + t] : t0 + t;
+        if (p >= 0) qmin = min(qmin, p);
+        else whole = false;
+        qmax = max(qmax, p);
+      }
+      qmin = __reduce_min_sync(0xFFFFFFFFu, qmin);
+      qmax = __reduce_max_sync(0xFFFFFFFFu, qmax);
+      whole = __all_sync(0xFFFFFFFFu, whole);
+      bool any = false, all = true;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const unsigned last = (unsigned)v[e].x + (unsigned)v[e].y;
+        any |= v[e].y != 0 && v[e].x <= qmax && (unsigned)qmin < last;
+        all &= e * 32 + lane >= live || (v[e].y != 0 && v[e].x <= qmin && (unsigned)qmax < last);
+      }
+      any = __any_sync(0xFFFFFFFFu, any) && qmax >= 0;
+      all = __all_sync(0xFFFFFFFFu, all) && whole;
+      if (lane == 0) flags[i] = !any ? 0u : all ? (uint8_t)kTileFull : (uint8_t)kTileMasked;
     }
   }
-  if (lane == 0) a.wout[at_w] = (a.win ? a.win[at_w] : 0.f) + sum;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  auto flags_of = [&](int i) -> uint32_t { return i < kWeightTiles ? flags[i] : (uint32_t)kTileMasked; };
+  auto next_tile = [&](int i) {
+    while (i < mine_n && flags_of(i) == 0u) ++i;
+    return i;
+  };
+  const long long limit = a.wait_limit;
+  auto wait_one = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, limit, 0u); };
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait_one(bar, parity)) != 0; };
+  const bool work = next_tile(0) < mine_n;
+  float total = 0.f;
+  // another CTA's shared memory may be written once that CTA runs: awaited below
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+
+  if (warp == 0) {
+    if (!a.withhold_loads && work) {
+      const int pl = a.q.cache.page_log2;
+      const int rows = min(1 << pl, kAttnTile);
+      const int boxes = (kAttnTile / rows) * (D / 64);
+      const int bslot = (lane / (D / 64)) * rows, bcol = (lane % (D / 64)) * 64;
+      if (lane == 0) mbar_expect_tx(k_bar, Cfg::kTileBytes);
+      __syncwarp();
+      if (lane < boxes) {
+        const int slot = slot0 + bslot;
+        int page = a.q.cache.num_pages;
+        if (slot < s.len) {
+          const int p = cache_page(a.q.cache, seq, slot, dev_status);
+          if (p >= 0) page = p;
+        }
+        tma_load_4d(smem_base + (uint32_t)(bcol / 64) * (kAttnTile * 128) + (uint32_t)bslot * 128u, &map_k, k_bar, bcol,
+                    slot & ((1 << pl) - 1), hk, page);
+      }
+      if (lane == 0) {
+        uint32_t phase = 0;
+        int stage = 0;
+        for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1)) {
+          if (!wait_one(q_empty(stage), phase ^ 1u)) break;
+          mbar_expect_tx(q_full(stage), (uint32_t)(a.q.G * tpt * D * 2));
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_3d(smem_base + Cfg::kQ + (uint32_t)stage * Cfg::kTileBytes + (uint32_t)c * (kAttnTile * 128), &map_q, q_full(stage),
+                        c * 64, hk * a.q.G, s.first + (rank + i * ranks) * tpt);
+          stage ^= 1;
+          phase ^= (uint32_t)(stage == 0);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && work && wait_one(k_bar, 0)) {
+      const uint32_t idesc = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24) |
+                             ((uint32_t)(ncols >> 3) << 17);
+      uint32_t phase = 0;
+      int stage = 0;   // stage, accumulator and stream at once
+      for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1)) {
+        if (!wait_one(q_full(stage), phase) || !wait_one(s_empty(stage), phase ^ 1u)) break;
+        tc_fence_after();
+        const uint64_t da = umma_smem_desc(smem_base), db = umma_smem_desc(smem_base + Cfg::kQ + (uint32_t)stage * Cfg::kTileBytes);
+#pragma unroll
+        for (int k = 0; k < D / kUmmaK; ++k) {
+          const uint64_t at = (uint64_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2);
+          umma_bf16(tmem_base + (uint32_t)stage * kAttnTile, da + at, db + at, idesc, (uint32_t)(k != 0));
+        }
+        umma_commit(q_empty(stage));
+        umma_commit(s_full(stage));
+        stage ^= 1;
+        phase ^= (uint32_t)(stage == 0);
+      }
+    }
+    __syncwarp();
+  } else {
+    const int st = (warp - 2) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t t_s = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)st * kAttnTile;
+    const int slot = slot0 + row;
+    const int2 iv = slot_interval(a.q, s, slot);
+    const bool warp_in = slot0 + quarter * 32 < s.len;
+    const float c = a.q.scale * 1.4426950408889634f;
+    // column `row` of a tile: which token and head it stands for
+    const int ct = row / a.q.G, ch = hk * a.q.G + row % a.q.G;
+    int n = 0, k = 0;   // tiles of all streams, of this one
+    for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1), ++n) {
+      if ((n & 1) != st) continue;
+      float* lse = col_lse + (st * 2 + (k & 1)) * kAttnTile;
+      int* place = col_place + (st * 2 + (k & 1)) * kAttnTile;
+      const int t = (rank + i * ranks) * tpt + ct;
+      float l2 = INFINITY;
+      int p = -1;
+      if (ct < tpt && t < s.n) {
+        const int64_t token = s.first + t;
+        p = a.q.pre ? a.q.pre[token] : t;
+        const float x = a.lse[token * a.q.Hq + ch];
+        if (x != -INFINITY) l2 = x * 1.4426950408889634f;
+      }
+      lse[row] = l2;
+      place[row] = p;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(c_bar(st));
+      if (!wait_warp(c_bar(st), (uint32_t)k & 1u) || !wait_warp(s_full(st), (uint32_t)k & 1u)) break;
+      tc_fence_after();
+      if (warp_in) {
+        const bool masked = (flags_of(i) & kTileMasked) != 0u;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < ncols; j += 32) {
+          uint32_t v[32];
+          ATTS_TMEM_LD_32(t_s + (uint32_t)j, v);
+          tmem_ld_wait();
+          if (masked) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const int4 w = *reinterpret_cast<const int4*>(place + j + e);
+              if ((unsigned)(w.x - iv.x) >= (unsigned)iv.y) v[e] = 0xFF800000u;
+              if ((unsigned)(w.y - iv.x) >= (unsigned)iv.y) v[e + 1] = 0xFF800000u;
+              if ((unsigned)(w.z - iv.x) >= (unsigned)iv.y) v[e + 2] = 0xFF800000u;
+              if ((unsigned)(w.w - iv.x) >= (unsigned)iv.y) v[e + 3] = 0xFF800000u;
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            const float4 w = *reinterpret_cast<const float4*>(lse + j + e);
+            sum[0] += ex2_approx(fmaf(__uint_as_float(v[e]), c, -w.x));
+            sum[1] += ex2_approx(fmaf(__uint_as_float(v[e + 1]), c, -w.y));
+            sum[2] += ex2_approx(fmaf(__uint_as_float(v[e + 2]), c, -w.z));
+            sum[3] += ex2_approx(fmaf(__uint_as_float(v[e + 3]), c, -w.w));
+          }
+        }
+        total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_empty(st));
+      ++k;
+    }
+    if (st == 1) sums[kWeightMaxCluster * kAttnTile + row] = total;
+  }
+
+  // ---------------- sums of the two streams, then of the cluster's CTAs in order ----------------
+  tc_fence_before();
+  __syncthreads();
+  if (ranks > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  if (warp >= 2 && warp < 6) {
+    const int row = (warp & 3) * 32 + lane;
+    total += sums[kWeightMaxCluster * kAttnTile + row];
+    if (rank == 0) sums[row] = total;
+    else
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(smem_u32(sums + rank * kAttnTile + row), 0)), "f"(total) : "memory");
+  }
+  if (ranks > 1) cluster_sync_all();
+  if (rank == 0 && warp >= 2 && warp < 6) {
+    const int row = (warp & 3) * 32 + lane, slot = slot0 + row;
+    float w = 0.f;
+    for (int i = 0; i < ranks; ++i) w += sums[i * kAttnTile + row];
+    if (slot < a.q.max_len) wout[slot] = slot < s.len ? (win ? win[slot] : 0.f) + w : 0.f;
+  }
+  if (*abort_flag) {
+    if (threadIdx.x == 0) atomicOr(dev_status, 2u);
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
+  }
 }
 
 // Opt-in shared memory of the kernels above (once per device).
@@ -739,6 +983,8 @@ static cudaError_t attention_attributes_of() {
   cudaError_t e = cudaFuncSetAttribute(tree_attention_kernel<T, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, true>::kSmemBytes);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(tree_attention_kernel<T, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, false>::kSmemBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(cache_weights_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightCfg<D>::kSmemBytes);
   return e;
 }
 static cudaError_t attention_attributes() {
