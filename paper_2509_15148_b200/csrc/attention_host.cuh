@@ -90,13 +90,14 @@ static int encode_cache(const DeviceInfo* di, CUtensorMap* map, const atts_kv_ca
 }
 
 // How an attention call is cut up.  Row tiles: as many whole tokens as fit 128 rows; two of them to a CTA if the longest
-// sequence has more than one.  Chunks: the number that makes the launch shortest when a slot tile takes one unit of time,
-// a CTA's start and end 2.5 and joining the chunks 2 (a unit is about 1.4 us: 64 KB per SM at the device's bandwidth).
+// sequence has more than one.  Chunks: the number that makes the launch shortest when a slot tile takes one unit of time
+// (about 1.4 us: 64 KB per SM at the device's bandwidth), a CTA's start and end 2.5, writing and reading back its rows'
+// sums one per 64 KB, and the second launch 3.
 struct AttnShape {
   bool two;
   AttnPlan p;
 };
-static AttnShape attn_shape(int sms, int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int64_t max_tokens, int64_t max_len) {
+static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens, int64_t max_len) {
   AttnShape r{};
   const int G = Hq / heads;
   r.p.tpt = kAttnTile / G;
@@ -105,12 +106,13 @@ static AttnShape attn_shape(int sms, int64_t num_seqs, int64_t M, int32_t Hq, in
   r.p.nq = (int)((max_tokens + per - 1) / per);
   const int64_t tiles = (max_len + kAttnTile - 1) / kAttnTile;
   const int64_t base = num_seqs * heads * r.p.nq;
+  const double part = (double)((max_tokens < per ? max_tokens : per) * G) * head_dim * 8 / 65536;
   double best = 0.0;
   int64_t best_n = 1;
   for (int64_t n = 1; n <= tiles && n <= 256 && (n == 1 || base * n <= 64 * (int64_t)sms); ++n) {
     const int64_t ct = (tiles + n - 1) / n;
     if ((tiles + ct - 1) / ct != n) continue;   // the same chunk length with fewer chunks was looked at
-    const double cost = (double)((base * n + sms - 1) / sms) * (2.5 + (double)ct) + (n > 1 ? 2.0 : 0.0);
+    const double cost = (double)((base * n + sms - 1) / sms) * (2.5 + (double)ct + (n > 1 ? part : 0.0)) + (n > 1 ? 3.0 : 0.0);
     if (n == 1 || cost < best) {
       best = cost;
       best_n = n;
@@ -281,7 +283,7 @@ int atts_tree_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq,
   const DeviceInfo* di;
   const int st = device_info(&di);
   if (st != ATTS_OK) return st;
-  *bytes = attn_workspace(attn_shape(di->sm_count, num_seqs, M, Hq, heads, max_tokens, max_len), M, Hq, head_dim);
+  *bytes = attn_workspace(attn_shape(di->sm_count, num_seqs, Hq, heads, head_dim, max_tokens, max_len), M, Hq, head_dim);
   return ATTS_OK;
 }
 
@@ -301,7 +303,7 @@ int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
   const DeviceInfo* di;
   st = device_info(&di);
   if (st != ATTS_OK) return st;
-  AttnShape sh = attn_shape(di->sm_count, cache->num_seqs, M, Hq, cache->heads, max_tokens, max_len);
+  AttnShape sh = attn_shape(di->sm_count, cache->num_seqs, Hq, cache->heads, cache->head_dim, max_tokens, max_len);
   if (workspace_bytes < attn_workspace(sh, M, Hq, cache->head_dim)) return ATTS_ERR_WORKSPACE;
   if (M == 0 || cache->num_seqs == 0 || max_tokens == 0) return ATTS_OK;
   a.q = static_cast<const char*>(q);

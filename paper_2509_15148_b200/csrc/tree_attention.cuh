@@ -45,19 +45,33 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
-// D[tmem] (+)= A[tmem] * B[smem], the A operand packed two 16-bit values to a tensor-memory column.
-__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+// Descriptors here are kept as their low word (address and leading offset); the high word is a constant and the step along
+// K an immediate, added inside the instruction's block: whole descriptors, one per step and tile, would be kept in more
+// registers than the issuing thread has, and every spilled one costs the tensor pipe a trip to L2.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);   // groups of eight rows 1024 bytes apart, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_low(uint32_t smem_addr, uint32_t lbo) { return (smem_addr >> 4) | ((lbo >> 4) << 16); }
+// D[tmem] (+)= A[smem] * B[smem]^T, both at `step` 16-byte units from their descriptors.
+__device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint32_t a_low, uint32_t b_low, uint32_t step, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b32 x, y;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "add.u32 x, %1, %3;\n\tadd.u32 y, %2, %3;\n\t"
+      "mov.b64 da, {x, %6};\n\tmov.b64 db, {y, %6};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}"
+      ::"r"(tmem_d), "r"(a_low), "r"(b_low), "r"(step), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
       : "memory");
 }
-// Descriptor of an operand whose M/N dimension is contiguous: blocks of 64 elements (128 bytes, 128-byte swizzle) `lbo`
-// bytes apart, groups of eight K rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t umma_smem_desc_mn(uint32_t smem_addr, uint32_t lbo) {
-  return (umma_smem_desc(smem_addr) & ~(0x3FFFull << 16)) | ((uint64_t)(lbo >> 4) << 16);
+// D[tmem] (+)= A[tmem] * B[smem], the A operand packed two 16-bit values to a tensor-memory column.
+__device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_low, uint32_t step_a, uint32_t step_b, uint32_t idesc,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b32 x, y;\n\t.reg .b64 db;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "add.u32 x, %1, %3;\n\tadd.u32 y, %2, %4;\n\t"
+      "mov.b64 db, {y, %7};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %5, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "r"(b_low), "r"(step_a), "r"(step_b), "r"(idesc), "r"(accumulate), "r"(kDescHigh)
+      : "memory");
 }
 #define ATTS_TMEM_ST_16(taddr, v)                                                                                          \
   asm volatile(                                                                                                            \
@@ -66,11 +80,14 @@ __device__ __forceinline__ uint64_t umma_smem_desc_mn(uint32_t smem_addr, uint32
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),         \
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])                                                \
       : "memory")
-#define ATTS_TMEM_ST_32(taddr, v)                                                                                          \
-  do {                                                                                                                     \
-    ATTS_TMEM_ST_16(taddr, v);                                                                                             \
-    ATTS_TMEM_ST_16((taddr) + 16u, (&v[16]));                                                                              \
-  } while (0)
+#define ATTS_TMEM_LD_16(taddr, v)                                                                                          \
+  asm volatile(                                                                                                            \
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "                                                                            \
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"                                     \
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),         \
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])                            \
+      : "r"(taddr)                                                                                                         \
+      : "memory")
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -160,14 +177,14 @@ __device__ __forceinline__ uint32_t tile_flags(const AttnArgs& a, const SeqView&
 // Loads one row tile's 32 columns, scales by the row's factor, stores them back.
 template <int D>
 __device__ __forceinline__ void rescale_o(uint32_t taddr, float f) {
-#pragma unroll
-  for (int j = 0; j < D / 32; ++j) {
-    uint32_t v[32];
-    ATTS_TMEM_LD_32(taddr + 32u * j, v);
+#pragma unroll 1
+  for (int j = 0; j < D / 16; ++j) {   // few columns at a time: the row's scores are in registers meanwhile
+    uint32_t v[16];
+    ATTS_TMEM_LD_16(taddr + 16u * j, v);
     tmem_ld_wait();
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-    ATTS_TMEM_ST_32(taddr + 32u * j, v);
+    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+    ATTS_TMEM_ST_16(taddr + 16u * j, v);
   }
   tmem_st_wait();
 }
@@ -293,6 +310,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   auto wait_one = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, limit, 0u); };
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait_one(bar, parity)) != 0; };
 
+  // A row's 128 scores stay in registers: 224 for the rows' warps and 56 for the others, 384 x 168 in all as launched.
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 0) {
     // ---------------- loads, in the order in which they are used: K_0 .. K_{lead-1}, then V_i, K_{i+lead} ----------------
     const int pl = a.cache.page_log2;
@@ -355,7 +375,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       int stage = 0;
       uint32_t phase = 0;
       bool ok = wait_one(q_bar, 0);
-      uint32_t p_phase[2] = {0, 0}, clean_phase = 0;
+      uint32_t p_phase = 0, clean_phase = 0;   // a bit per stream
       auto advance = [&]() {
         umma_commit(empty_bar(stage));
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -363,12 +383,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       auto qk = [&](int i) {   // S_i = Q (of stream i if TWO) K^T of the ring's present tile
         const uint32_t sa = smem_base + (TWO ? (uint32_t)i * Cfg::kTileBytes : 0u);
         const uint32_t sb = smem_base + Cfg::kRing + (uint32_t)stage * Cfg::kTileBytes;
-        const uint64_t da = umma_smem_desc(sa), db = umma_smem_desc(sb);
+        const uint32_t da = desc_low(sa, 16), db = desc_low(sb, 16);   // K contiguous: the leading offset is unused
 #pragma unroll
-        for (int k = 0; k < D / kUmmaK; ++k) {
-          const uint64_t at = (uint64_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2);
-          umma_bf16(tmem_base + (uint32_t)i * kAttnTile, da + at, db + at, kIdescS, (uint32_t)(k != 0));
-        }
+        for (int k = 0; k < D / kUmmaK; ++k)
+          umma_ss(tmem_base + (uint32_t)i * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), kIdescS, (uint32_t)(k != 0));
         umma_commit(s_bar(i));
       };
       auto next_k = [&]() {    // products of the next key tile, for the streams that use it
@@ -406,15 +424,16 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const int streams = TWO ? (two ? 2 : 1) : 1;
         for (int u = 0; u < streams && ok; ++u) {
           const int st = TWO ? u : i & 1;
-          ok = wait_one(p_bar(st), p_phase[st]);
+          ok = wait_one(p_bar(st), (p_phase >> st) & 1u);
           if (!ok) break;
-          p_phase[st] ^= 1u;
+          p_phase ^= 1u << st;
           tc_fence_after();
-          const uint64_t db = umma_smem_desc_mn(smem_base + Cfg::kRing + (uint32_t)vstage * Cfg::kTileBytes, kAttnTile * 128);
+          // channels contiguous: blocks of 64 channels kAttnTile * 128 bytes apart, 16 slots are two groups of eight rows
+          const uint32_t db = desc_low(smem_base + Cfg::kRing + (uint32_t)vstage * Cfg::kTileBytes, kAttnTile * 128);
           const bool first = TWO ? i == 0 : i < 2;
 #pragma unroll
           for (int k = 0; k < kAttnTile / kUmmaK; ++k)
-            umma_ts(tmem_base + 256u + (uint32_t)st * D, tmem_base + (uint32_t)st * kAttnTile + 8u * k, db + (uint64_t)(k * (kUmmaK * 128 / 16)),
+            umma_ts(tmem_base + 256u + (uint32_t)st * D, tmem_base + (uint32_t)st * kAttnTile, db, 8u * k, (uint32_t)(k * (kUmmaK * 128 / 16)),
                     kIdescO, (uint32_t)(!first || k != 0));
           umma_commit(o_bar(st));
           if (u + 1 == streams) umma_commit(empty_bar(vstage));
@@ -458,8 +477,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       __syncwarp();
       if (lane == 0) mbar_arrive(clean_bar);
     }
-  } else if (warp >= 4) {
+  }
+  } else {
     // ---------------- rows ----------------
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const int st = (warp - 4) >> 2;                    // stream
     const int quarter = warp & 3;
     const int row = quarter * 32 + lane;
@@ -870,12 +891,10 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1)) {
         if (!wait_one(q_full(stage), phase) || !wait_one(s_empty(stage), phase ^ 1u)) break;
         tc_fence_after();
-        const uint64_t da = umma_smem_desc(smem_base), db = umma_smem_desc(smem_base + Cfg::kQ + (uint32_t)stage * Cfg::kTileBytes);
+        const uint32_t da = desc_low(smem_base, 16), db = desc_low(smem_base + Cfg::kQ + (uint32_t)stage * Cfg::kTileBytes, 16);
 #pragma unroll
-        for (int k = 0; k < D / kUmmaK; ++k) {
-          const uint64_t at = (uint64_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2);
-          umma_bf16(tmem_base + (uint32_t)stage * kAttnTile, da + at, db + at, idesc, (uint32_t)(k != 0));
-        }
+        for (int k = 0; k < D / kUmmaK; ++k)
+          umma_ss(tmem_base + (uint32_t)stage * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), idesc, (uint32_t)(k != 0));
         umma_commit(q_empty(stage));
         umma_commit(s_full(stage));
         stage ^= 1;
