@@ -88,6 +88,29 @@ __device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32
         "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])                            \
       : "r"(taddr)                                                                                                         \
       : "memory")
+// Two fp32 values in one 64-bit register pair: one instruction for two multiply-adds or additions.
+__device__ __forceinline__ uint64_t pair2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float low2(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float high2(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -102,12 +125,18 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // The slots may be cut into chunks of `chunk` tiles over CTAs (few rows, long caches); the parts are then joined by
 // attention_join_kernel.
 //
-// Warps: 0 loads (TMA, one box per page and 64 channels), 1 issues the products, 2 clears the values of slots that hold
-// nothing (whatever lies there, 0 * NaN must not reach O), 4-7 and 8-11 the two streams' rows.
+// Which of the tiles behind the cached part a CTA needs, and in which groups of 32 slots pairs have to be looked at one by
+// one, is listed while the cached tiles are already on their way: the rows' warps look at a tile each, warp 3 makes the
+// list; whoever comes to the end of the cached tiles waits for it.
+//
+// Warps: 0 and 2 load (TMA, one box per page and 64 channels), 1 issues the products, 3 makes the list, lays out the intervals
+// of the tiles that need them and clears the values of slots that hold nothing (whatever lies there, 0 * NaN must not reach
+// O), 4-7 and 8-11 are the two streams' rows.
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kAttnThreads = 384;
 constexpr int kAttnTile = 128;          // rows of a tile, slots of a tile
-constexpr int kAttnTreeTiles = 1024;    // tiles behind the cached part whose visibility is looked up ahead
+constexpr int kAttnTreeTiles = 1024;    // tiles behind the cached part that are listed; further ones are all looked at
+constexpr int kMaskRing = 4;
 
 template <int D, bool TWO>
 struct AttnCfg {
@@ -115,17 +144,23 @@ struct AttnCfg {
   static constexpr int kQBytes = (TWO ? 2 : 1) * kTileBytes;
   static constexpr int kStages = D == 128 ? (TWO ? 4 : 5) : 8;
   static constexpr int kRing = kQBytes;                              // byte offsets in (aligned) shared memory
-  static constexpr int kMask = kRing + kStages * kTileBytes;         // [2 streams][2][128] int2
-  static constexpr int kFlags = kMask + 4 * kAttnTile * 8;
-  static constexpr int kStats = kFlags + kAttnTreeTiles;             // [128] float2: maximum and sum of the odd stream
+  static constexpr int kMask = kRing + kStages * kTileBytes;         // [kMaskRing][128] int2
+  static constexpr int kList = kMask + kMaskRing * kAttnTile * 8;    // [kAttnTreeTiles] uint32
+  static constexpr int kStats = kList + kAttnTreeTiles * 4;          // [128] float2: maximum and sum of the odd stream
   static constexpr int kBars = kStats + kAttnTile * 8;
-  static constexpr int kSmemBytes = kBars + 256 + 1024;
+  static constexpr int kSmemBytes = kBars + 512 + 1024;
   static constexpr int kLead = TWO ? 1 : 2;                          // key tiles loaded ahead of the first value tile
   static_assert(kSmemBytes <= 232448, "shared memory of one SM");
   static_assert(kStages * kTileBytes >= kAttnTile * (D + 4) * 4, "the odd stream's sums are joined through the ring");
 };
 
-enum : uint32_t { kTileMasked = 1, kTileFull = 2, kTileDead = 4 };  // some / all pairs visible; some slots hold nothing
+// A tile's flags: two bits for each group of 32 slots (0 nobody sees any, 1 pairs differ, 2 everybody sees all), then
+enum : uint32_t {
+  kTileDead = 1u << 8,      // some slots hold nothing
+  kTileMasked = 1u << 9,    // some group is neither empty nor full
+  kTileFull = 0xAAu,
+  kTileUnknown = 0x55u | kTileDead | kTileMasked
+};
 
 struct AttnPlan {
   int chunk;        // slot tiles per CTA
@@ -156,23 +191,65 @@ __device__ __forceinline__ int2 slot_interval(const AttnArgs& a, const SeqView& 
   return (lo < 0 || hi <= lo) ? make_int2(0, 0) : make_int2(lo, hi - lo);
 }
 
-// Visibility of one tile behind the cached part for rows whose places span [qmin, qmax] (whole warp).
+// The same for a whole tile by one warp, slots e * 32 + lane, all loads under way at once.
+__device__ __forceinline__ void tile_intervals(const AttnArgs& a, const SeqView& s, int tile, int lane, int2 (&v)[kAttnTile / 32]) {
+  constexpr int E = kAttnTile / 32;
+  int lo[E], hi[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int j = tile * kAttnTile + e * 32 + lane - s.ctx;
+    lo[e] = hi[e] = 0;
+    if (a.pre && j >= 0 && j < s.n) {
+      lo[e] = a.pre[s.first + j];
+      hi[e] = a.end[s.first + j];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int slot = tile * kAttnTile + e * 32 + lane;
+    if (slot >= s.len) v[e] = make_int2(0, 0);
+    else if (slot < s.ctx) v[e] = make_int2(0, 0x7FFFFFFF);
+    else if (!a.pre) v[e] = make_int2(slot - s.ctx, 0x7FFFFFFF);
+    else v[e] = (lo[e] < 0 || hi[e] <= lo[e]) ? make_int2(0, 0) : make_int2(lo[e], hi[e] - lo[e]);
+  }
+}
+
+// Flags of one tile for rows whose places span [qmin, qmax] (whole warp); 0: nobody sees anything of it.
 __device__ __forceinline__ uint32_t tile_flags(const AttnArgs& a, const SeqView& s, int tile, int qmin, int qmax, int lane) {
-  bool any = false, all = true, dead = false;
+  uint32_t f = 0;
+  int2 v[kAttnTile / 32];
+  tile_intervals(a, s, tile, lane, v);
 #pragma unroll
   for (int e = 0; e < kAttnTile / 32; ++e) {
-    const int2 v = slot_interval(a, s, tile * kAttnTile + e * 32 + lane);
-    const unsigned last = (unsigned)v.x + (unsigned)v.y;    // one past the interval
-    const bool none = v.y == 0;
-    any |= !none && v.x <= qmax && (unsigned)qmin < last;
-    all &= !none && v.x <= qmin && (unsigned)qmax < last;
-    dead |= none;
+    const unsigned last = (unsigned)v[e].x + (unsigned)v[e].y;    // one past the interval
+    const bool none = v[e].y == 0;
+    const bool any = __any_sync(0xFFFFFFFFu, !none && v[e].x <= qmax && (unsigned)qmin < last);
+    const bool all = __all_sync(0xFFFFFFFFu, !none && v[e].x <= qmin && (unsigned)qmax < last);
+    if (any) f |= all ? 2u << (2 * e) : (1u << (2 * e)) | kTileMasked;
+    if (__any_sync(0xFFFFFFFFu, none)) f |= kTileDead;
   }
-  any = __any_sync(0xFFFFFFFFu, any);
-  all = __all_sync(0xFFFFFFFFu, all);
-  dead = __any_sync(0xFFFFFFFFu, dead);
-  return !any ? 0u : (all ? kTileFull : kTileMasked) | (dead ? kTileDead : 0u);
+  return (f & 0xFFu) ? f : 0u;
 }
+
+// Loads a tile of slots, a lane per box (one page, 64 channels).  A TMA instruction costs its warp about 117 cycles when one
+// lane issues one after the other and 56 when lanes issue side by side, whatever its size, and warps do not disturb one
+// another (measured, boxes of 8 to 128 rows): so small pages are issued by many lanes, keys and values by two warps.
+template <int D>
+struct TileBoxes {
+  static constexpr int kHalves = D / 64;
+  int page_log2, rows, boxes, slot;   // slots of a box, boxes of a tile (<= 32), this lane's first slot in the tile
+  __device__ __forceinline__ TileBoxes(int page_log2_, int lane) : page_log2(page_log2_) {
+    rows = min(1 << page_log2, kAttnTile);
+    boxes = (kAttnTile / rows) * kHalves;
+    slot = (lane / kHalves) * rows;
+  }
+  __device__ __forceinline__ void issue(uint32_t dst, const CUtensorMap* map, uint32_t bar, int tile, int hk, int page, int lane) const {
+    if (lane < boxes)
+      tma_load_4d(dst + (uint32_t)(lane % kHalves) * (kAttnTile * 128) + (uint32_t)slot * 128u, map, bar, (lane % kHalves) * 64,
+                  (tile * kAttnTile + slot) & ((1 << page_log2) - 1), hk, page);
+    __syncwarp();
+  }
+};
 
 // Loads one row tile's 32 columns, scales by the row's factor, stores them back.
 template <int D>
@@ -217,21 +294,23 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
   int2* mask = reinterpret_cast<int2*>(smem + Cfg::kMask);
-  uint8_t* flags = smem + Cfg::kFlags;
+  volatile uint32_t* list = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kList);
   float2* stats = reinterpret_cast<float2*>(smem + Cfg::kStats);
   const uint32_t bar0 = smem_base + Cfg::kBars;
   auto full_bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   auto empty_bar = [&](int i) { return bar0 + 8u * (uint32_t)(kStages + i); };
-  const uint32_t q_bar = bar0 + 8u * (2 * kStages), clean_bar = q_bar + 8u;
-  auto s_bar = [&](int i) { return clean_bar + 8u + 8u * (uint32_t)i; };
-  auto p_bar = [&](int i) { return clean_bar + 24u + 8u * (uint32_t)i; };
-  auto o_bar = [&](int i) { return clean_bar + 40u + 8u * (uint32_t)i; };
-  auto m_bar = [&](int i) { return clean_bar + 56u + 8u * (uint32_t)i; };
-  const uint32_t join_bar = clean_bar + 72u, dirty_bar = clean_bar + 80u;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kBars + 8 * (2 * kStages + 12));
+  const uint32_t q_bar = bar0 + 8u * (2 * kStages), clean_bar = q_bar + 8u, join_bar = q_bar + 16u, flag_bar = q_bar + 24u, list_bar = q_bar + 32u;
+  auto s_bar = [&](int i) { return q_bar + 40u + 8u * (uint32_t)i; };
+  auto p_bar = [&](int i) { return q_bar + 56u + 8u * (uint32_t)i; };
+  auto o_bar = [&](int i) { return q_bar + 72u + 8u * (uint32_t)i; };
+  auto m_full = [&](int i) { return q_bar + 88u + 8u * (uint32_t)i; };
+  auto m_empty = [&](int i) { return q_bar + 88u + 8u * (uint32_t)(kMaskRing + i); };
+  constexpr int kBarCount = 2 * kStages + 11 + 2 * kMaskRing;
+  static_assert(8 * kBarCount + 32 <= 512, "room for the barriers");
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kBars + 8 * kBarCount);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   volatile int* range = reinterpret_cast<volatile int*>(tmem_slot + 2);   // smallest and largest place of the rows
-  volatile int* clear_stage = range + 2;
+  volatile int* listed = range + 2;                                       // entries of the list
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -240,18 +319,22 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     prefetch_tmap(&map_v);
     for (int i = 0; i < kStages; ++i) {
       mbar_init(full_bar(i), 1);
-      mbar_init(empty_bar(i), 1);
+      mbar_init(empty_bar(i), 2);     // the products that read the stage, and warp 3
     }
     mbar_init(q_bar, 1);
     mbar_init(clean_bar, 1);
-    mbar_init(dirty_bar, 1);
+    mbar_init(join_bar, 4);
+    mbar_init(flag_bar, 8);
+    mbar_init(list_bar, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_bar(i), 1);
       mbar_init(p_bar(i), 4);
       mbar_init(o_bar(i), 1);
-      mbar_init(m_bar(i), 4);
     }
-    mbar_init(join_bar, 4);
+    for (int i = 0; i < kMaskRing; ++i) {
+      mbar_init(m_full(i), 1);
+      mbar_init(m_empty(i), TWO && two ? 8 : 4);   // the warps that read it
+    }
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -273,214 +356,244 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       range[1] = hi;
     }
   }
-  __syncthreads();
-  {
-    // all rows padding: qmax is -1 and no tile is visible
-    const int qmin = range[0], qmax = range[1];
-    const int t0 = max(tile0, tree0), t1 = min(tile1, tree0 + kAttnTreeTiles);
-    for (int t = t0 + warp; t < t1; t += kAttnThreads / 32) {
-      const uint32_t f = qmax < 0 ? 0u : tile_flags(a, s, t, qmin, qmax, lane);
-      if (lane == 0) flags[t - tree0] = (uint8_t)f;
-    }
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const bool rows_live = range[1] >= 0;
-  auto flags_of = [&](int t) -> uint32_t {
-    if (t < tree0) return rows_live ? kTileFull : 0u;
-    return t - tree0 < kAttnTreeTiles ? flags[t - tree0] : rows_live ? (uint32_t)(kTileMasked | kTileDead) : 0u;
-  };
-  int ntile = 0;  // visible tiles
-  for (int t = tile0; t < tile1; ++t) {
-    if (t < tree0) {
-      const int e = min(tile1, tree0);
-      ntile += rows_live ? e - t : 0;
-      t = e - 1;
-    } else {
-      ntile += flags_of(t) != 0u;
-    }
-  }
-  auto next_tile = [&](int t) {  // the first visible tile from t on
-    while (t < tile1 && flags_of(t) == 0u) ++t;
-    return t;
-  };
   const long long limit = plan.wait_limit;
   auto wait_one = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, limit, 0u); };
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait_one(bar, parity)) != 0; };
 
+  // The CTA's visible tiles: number i is tile0 + i among the cached ones (none if every row is padding), then the listed
+  // ones of [t0, t0 + kAttnTreeTiles), then all further ones.
+  const bool rows_live = range[1] >= 0;
+  const int t0 = max(tile0, tree0), t_far = min(tile1, t0 + kAttnTreeTiles);
+  const int npre = rows_live ? max(0, min(tile1, tree0) - tile0) : 0;
+  int nlist = -1, ntile = npre;           // known once the list has been waited for
+  auto has = [&](int i, bool one_thread) -> bool {
+    if (i < npre) return true;
+    if (nlist < 0) {
+      if (!(one_thread ? wait_one(list_bar, 0) : wait_warp(list_bar, 0))) return false;   // gave up: every other wait does too
+      nlist = *listed;
+      ntile = npre + nlist + (rows_live ? max(0, tile1 - t0 - kAttnTreeTiles) : 0);
+    }
+    return i < ntile;
+  };
+  auto tile_of = [&](int i, uint32_t& f) -> int {
+    f = kTileFull;
+    if (i < npre) return tile0 + i;
+    if (i - npre < nlist) {
+      const uint32_t e = list[i - npre];
+      f = e & 0xFFFFu;
+      return t0 + (int)(e >> 16);
+    }
+    f = kTileUnknown;
+    return t0 + kAttnTreeTiles + (i - npre - nlist);
+  };
+
   // A row's 128 scores stay in registers: 224 for the rows' warps and 56 for the others, 384 x 168 in all as launched.
   if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-  if (warp == 0) {
-    // ---------------- loads, in the order in which they are used: K_0 .. K_{lead-1}, then V_i, K_{i+lead} ----------------
-    const int pl = a.cache.page_log2;
-    const int rows = min(1 << pl, kAttnTile);                 // slots of a box
-    const int boxes = (kAttnTile / rows) * (D / 64);          // <= 32
-    const int bslot = (lane / (D / 64)) * rows, bcol = (lane % (D / 64)) * 64;
-    const uint32_t bdst = (uint32_t)(bcol / 64) * (kAttnTile * 128) + (uint32_t)bslot * 128u;
-    auto page_of = [&](int t) -> int {
-      if (lane >= boxes || t >= tile1) return 0;
-      const int slot = t * kAttnTile + bslot;
-      if (slot >= s.len) return a.cache.num_pages;            // out of the map: filled with zeros
-      const int page = cache_page(a.cache, seq, slot, dev_status);
-      return page < 0 ? a.cache.num_pages : page;
-    };
-    if (!plan.withhold_loads && ntile > 0) {
-      if (lane == 0) {
-        mbar_expect_tx(q_bar, (uint32_t)((two ? 2 : 1) * a.G * plan.tpt * D * 2));
-        for (int i = 0; i < (two ? 2 : 1); ++i)
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_3d(smem_base + (uint32_t)i * Cfg::kTileBytes + (uint32_t)c * (kAttnTile * 128), &map_q, q_bar, c * 64, hk * a.G,
-                        s.first + tok0 + i * plan.tpt);
-      }
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      auto load = [&](const CUtensorMap* map, int t, int page) {
-        ok = wait_warp(empty_bar(stage), phase ^ 1u);
-        if (!ok) return;
-        if (lane == 0) mbar_expect_tx(full_bar(stage), Cfg::kTileBytes);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0 || warp == 2) {
+      // ---------------- loads: keys (and the queries) by warp 0, values by warp 2.  The ring's order is that of use:
+      // K_0 .. K_{lead-1}, then V_i, K_{i+lead} ----------------
+      const TileBoxes<D> bx(a.cache.page_log2, lane);
+      constexpr int kNoSlot = -2;                               // behind the sequence: no page, filled with zeros
+      auto look_up = [&](int i) -> int {                        // the table's entry for this lane's box, not looked at yet
+        if (!has(i, false)) return kNoSlot;
+        uint32_t f;
+        const int slot = tile_of(i, f) * kAttnTile + bx.slot;
+        if (lane >= bx.boxes || slot >= s.len) return kNoSlot;
+        const int col = slot >> bx.page_log2;
+        return col < a.cache.table_cols ? a.cache.table[(int64_t)seq * a.cache.table_stride + col] : -1;
+      };
+      auto page_of = [&](int entry) -> int {
+        if (entry >= 0 && entry < a.cache.num_pages) return entry;
+        if (entry != kNoSlot) atomicOr(dev_status, kDevPageRange);
+        return a.cache.num_pages;                               // out of the map: filled with zeros
+      };
+      if (!plan.withhold_loads) {
+        const bool value = warp == 2;
+        int e0 = look_up(0);                                    // entries of the next two tiles
+        if (!value && lane == 0 && has(0, true)) {              // nothing is loaded that nothing waits for
+          mbar_expect_tx(q_bar, (uint32_t)((two ? 2 : 1) * a.G * plan.tpt * D * 2));
+          for (int i = 0; i < (two ? 2 : 1); ++i)
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_3d(smem_base + (uint32_t)i * Cfg::kTileBytes + (uint32_t)c * (kAttnTile * 128), &map_q, q_bar, c * 64, hk * a.G,
+                          s.first + tok0 + i * plan.tpt);
+        }
         __syncwarp();
-        if (lane < boxes)
-          tma_load_4d(smem_base + Cfg::kRing + (uint32_t)stage * Cfg::kTileBytes + bdst, map, full_bar(stage), bcol,
-                      (t * kAttnTile + bslot) & ((1 << pl) - 1), hk, page);
-        if (++stage == kStages) { stage = 0; phase ^= 1u; }
-      };
-      int tk = next_tile(tile0), tv = tk;
-      int pk = page_of(tk), pv = pk;
-      for (int i = 0; i < kLead && tk < tile1 && ok; ++i) {
-        const int nt = next_tile(tk + 1), np = page_of(nt);
-        load(&map_k, tk, pk);
-        tk = nt; pk = np;
-      }
-      while (tv < tile1 && ok) {
-        const int nv = next_tile(tv + 1), npv = page_of(nv);
-        load(&map_v, tv, pv);
-        tv = nv; pv = npv;
-        if (tk < tile1 && ok) {
-          const int nt = next_tile(tk + 1), np = page_of(nt);
-          load(&map_k, tk, pk);
-          tk = nt; pk = np;
-        }
-      }
-    }
-  } else if (warp == 1) {
-    // ---------------- products ----------------
-    if (lane == 0 && ntile > 0) {
-      constexpr uint32_t kFmt = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24);
-      constexpr uint32_t kIdescS = kFmt | ((uint32_t)(kAttnTile >> 3) << 17);
-      constexpr uint32_t kIdescO = kFmt | (1u << 16) | ((uint32_t)(D >> 3) << 17);   // B with its N dimension contiguous
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = wait_one(q_bar, 0);
-      uint32_t p_phase = 0, clean_phase = 0;   // a bit per stream
-      auto advance = [&]() {
-        umma_commit(empty_bar(stage));
-        if (++stage == kStages) { stage = 0; phase ^= 1u; }
-      };
-      auto qk = [&](int i) {   // S_i = Q (of stream i if TWO) K^T of the ring's present tile
-        const uint32_t sa = smem_base + (TWO ? (uint32_t)i * Cfg::kTileBytes : 0u);
-        const uint32_t sb = smem_base + Cfg::kRing + (uint32_t)stage * Cfg::kTileBytes;
-        const uint32_t da = desc_low(sa, 16), db = desc_low(sb, 16);   // K contiguous: the leading offset is unused
-#pragma unroll
-        for (int k = 0; k < D / kUmmaK; ++k)
-          umma_ss(tmem_base + (uint32_t)i * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), kIdescS, (uint32_t)(k != 0));
-        umma_commit(s_bar(i));
-      };
-      auto next_k = [&]() {    // products of the next key tile, for the streams that use it
-        ok = ok && wait_one(full_bar(stage), phase);
-        if (!ok) return;
-        tc_fence_after();
-      };
-      int tv = next_tile(tile0);
-      int lead = min(kLead, ntile), ik = 0;
-      for (; ik < lead && ok; ++ik) {
-        next_k();
-        if (!ok) break;
-        if (TWO) {
-          qk(0);
-          if (two) qk(1);
-        } else {
-          qk(ik & 1);
-        }
-        advance();
-      }
-      for (int i = 0; i < ntile && ok; ++i) {
-        ok = wait_one(full_bar(stage), phase);
-        if (ok && (flags_of(tv) & kTileDead)) {   // hand the stage to warp 2 and wait until it has been cleared
-          *clear_stage = stage;
-          mbar_arrive(dirty_bar);
-          ok = wait_one(clean_bar, clean_phase);
-          clean_phase ^= 1u;
-        }
-        if (!ok) break;
-        tc_fence_after();
-        const int vstage = stage;
-        const bool more = ik < ntile;
-        const int kstage = stage + 1 == kStages ? 0 : stage + 1;
-        const uint32_t kphase = stage + 1 == kStages ? phase ^ 1u : phase;
-        const int streams = TWO ? (two ? 2 : 1) : 1;
-        for (int u = 0; u < streams && ok; ++u) {
-          const int st = TWO ? u : i & 1;
-          ok = wait_one(p_bar(st), (p_phase >> st) & 1u);
+        int e1 = look_up(1);
+        bool ok = true;
+        for (int i = 0; ok && has(i, false); ++i) {
+          const int page = page_of(e0);
+          e0 = e1;
+          e1 = look_up(i + 2);
+          // place in the ring's order: before V_i come i values and min(lead + i, ntile) keys
+          const int pos = value ? (has(kLead + i - 1, false) ? kLead + 2 * i : ntile + i) : i < kLead ? i : 2 * i - kLead + 1;
+          const int stage = pos % kStages;
+          ok = wait_warp(empty_bar(stage), ((uint32_t)(pos / kStages) & 1u) ^ 1u);
           if (!ok) break;
-          p_phase ^= 1u << st;
-          tc_fence_after();
-          // channels contiguous: blocks of 64 channels kAttnTile * 128 bytes apart, 16 slots are two groups of eight rows
-          const uint32_t db = desc_low(smem_base + Cfg::kRing + (uint32_t)vstage * Cfg::kTileBytes, kAttnTile * 128);
-          const bool first = TWO ? i == 0 : i < 2;
-#pragma unroll
-          for (int k = 0; k < kAttnTile / kUmmaK; ++k)
-            umma_ts(tmem_base + 256u + (uint32_t)st * D, tmem_base + (uint32_t)st * kAttnTile, db, 8u * k, (uint32_t)(k * (kUmmaK * 128 / 16)),
-                    kIdescO, (uint32_t)(!first || k != 0));
-          umma_commit(o_bar(st));
-          if (u + 1 == streams) umma_commit(empty_bar(vstage));
-          if (more) {
-            if (u == 0) {
-              ok = wait_one(full_bar(kstage), kphase);
-              if (!ok) break;
-              tc_fence_after();
-            }
-            const int keep = stage;
-            stage = kstage;
-            qk(st);
-            stage = keep;
-            if (u + 1 == streams) umma_commit(empty_bar(kstage));
-          }
+          if (lane == 0) mbar_expect_tx(full_bar(stage), Cfg::kTileBytes);
+          __syncwarp();
+          uint32_t f;
+          bx.issue(smem_base + Cfg::kRing + (uint32_t)stage * Cfg::kTileBytes, value ? &map_v : &map_k, full_bar(stage), tile_of(i, f), hk, page, lane);
         }
-        if (!ok) break;
-        for (int u = 0; u < (more ? 2 : 1); ++u)
+      }
+    } else if (warp == 1) {
+      // ---------------- products ----------------
+      if (lane == 0 && has(0, true)) {
+        constexpr uint32_t kFmt = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24);
+        constexpr uint32_t kIdescS = kFmt | ((uint32_t)(kAttnTile >> 3) << 17);
+        constexpr uint32_t kIdescO = kFmt | (1u << 16) | ((uint32_t)(D >> 3) << 17);   // B with its N dimension contiguous
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = wait_one(q_bar, 0);
+        uint32_t p_phase = 0, clean_phase = 0;   // a bit per stream
+        auto qk = [&](int i, int at) {   // S_i = Q (of stream i if TWO) K^T of the stage's tile
+          const uint32_t sa = smem_base + (TWO ? (uint32_t)i * Cfg::kTileBytes : 0u);
+          const uint32_t sb = smem_base + Cfg::kRing + (uint32_t)at * Cfg::kTileBytes;
+          const uint32_t da = desc_low(sa, 16), db = desc_low(sb, 16);   // K contiguous: the leading offset is unused
+#pragma unroll
+          for (int k = 0; k < D / kUmmaK; ++k)
+            umma_ss(tmem_base + (uint32_t)i * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), kIdescS, (uint32_t)(k != 0));
+          umma_commit(s_bar(i));
+        };
+        const int streams = TWO ? (two ? 2 : 1) : 1;   // that use each tile
+        for (int ik = 0; ik < kLead && ok && has(ik, true); ++ik) {
+          ok = wait_one(full_bar(stage), phase);
+          if (!ok) break;
+          tc_fence_after();
+          for (int u = 0; u < streams; ++u) qk(TWO ? u : ik & 1, stage);
+          umma_commit(empty_bar(stage));
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        ik += more ? 1 : 0;
-        tv = next_tile(tv + 1);
+        }
+        for (int i = 0; ok && has(i, true); ++i) {
+          uint32_t f;
+          tile_of(i, f);
+          ok = wait_one(full_bar(stage), phase);
+          if (ok && (f & kTileDead)) {
+            ok = wait_one(clean_bar, clean_phase);
+            clean_phase ^= 1u;
+          }
+          const bool more = ok && has(i + kLead, true);
+          if (!ok) break;
+          tc_fence_after();
+          const int vstage = stage;
+          const int kstage = stage + 1 == kStages ? 0 : stage + 1;
+          const uint32_t kphase = stage + 1 == kStages ? phase ^ 1u : phase;
+          for (int u = 0; u < streams && ok; ++u) {
+            const int st = TWO ? u : i & 1;
+            ok = wait_one(p_bar(st), (p_phase >> st) & 1u);
+            if (!ok) break;
+            p_phase ^= 1u << st;
+            tc_fence_after();
+            // channels contiguous: blocks of 64 channels kAttnTile * 128 bytes apart, 16 slots are two groups of eight rows
+            const uint32_t db = desc_low(smem_base + Cfg::kRing + (uint32_t)vstage * Cfg::kTileBytes, kAttnTile * 128);
+            const bool first = TWO ? i == 0 : i < 2;
+#pragma unroll
+            for (int k = 0; k < kAttnTile / kUmmaK; ++k)
+              umma_ts(tmem_base + 256u + (uint32_t)st * D, tmem_base + (uint32_t)st * kAttnTile, db, 8u * k, (uint32_t)(k * (kUmmaK * 128 / 16)),
+                      kIdescO, (uint32_t)(!first || k != 0));
+            umma_commit(o_bar(st));
+            if (u + 1 == streams) umma_commit(empty_bar(vstage));
+            if (more) {
+              if (u == 0) {
+                ok = wait_one(full_bar(kstage), kphase);
+                if (!ok) break;
+                tc_fence_after();
+              }
+              qk(st, kstage);
+              if (u + 1 == streams) umma_commit(empty_bar(kstage));
+            }
+          }
+          if (!ok) break;
+          for (int u = 0; u < (more ? 2 : 1); ++u)
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        }
       }
-    }
-    __syncwarp();
-  } else if (warp == 2) {
-    // ---------------- values of slots that hold nothing ----------------
-    int t = next_tile(tile0);
-    uint32_t dirty_phase = 0;
-    for (int i = 0; i < ntile; ++i, t = next_tile(t + 1)) {
-      if (!(flags_of(t) & kTileDead)) continue;
-      if (!wait_warp(dirty_bar, dirty_phase)) break;
-      dirty_phase ^= 1u;
-      uint8_t* v = smem + Cfg::kRing + *clear_stage * Cfg::kTileBytes;
-      for (int e = 0; e < kAttnTile / 32; ++e) {
-        const int row = e * 32 + lane;
-        if (slot_interval(a, s, t * kAttnTile + row).y != 0) continue;
-        for (int c = 0; c < D / 64; ++c)
-          for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(v + c * (kAttnTile * 128) + row * 128 + x * 16) = make_uint4(0, 0, 0, 0);
-      }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(clean_bar);
+    } else {
+      // ---------------- the list of visible tiles behind the cached part; then, along the ring, the intervals of tiles that
+      // need them, and zeros over the values of slots that hold nothing ----------------
+      bool ok = wait_warp(flag_bar, 0);
+      int n = 0;
+      for (int base = t0; ok && base < t_far; base += 32) {
+        const uint32_t f = base + lane < t_far ? list[base - t0 + lane] : 0u;
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, f != 0u);
+        __syncwarp();
+        if (f) list[n + __popc(some & ((1u << lane) - 1u))] = f | ((uint32_t)(base - t0 + lane) << 16);
+        n += __popc(some);
+      }
+      if (lane == 0) *listed = n;
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(list_bar);
+      int stage = 0, masked = 0;
+      uint32_t phase = 0;
+      auto intervals = [&](int i) {
+        uint32_t f;
+        const int t = tile_of(i, f);
+        if (!(f & kTileMasked)) return;
+        const int b = masked % kMaskRing;
+        ok = wait_warp(m_empty(b), ((uint32_t)(masked / kMaskRing) & 1u) ^ 1u);
+        if (!ok) return;
+        int2 v[kAttnTile / 32];
+        tile_intervals(a, s, t, lane, v);
+#pragma unroll
+        for (int e = 0; e < kAttnTile / 32; ++e) mask[b * kAttnTile + e * 32 + lane] = v[e];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(m_full(b));
+        ++masked;
+      };
+      auto release = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty_bar(stage));
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      };
+      int ik = 0;
+      auto pass_key = [&]() {
+        intervals(ik++);
+        ok = ok && wait_warp(full_bar(stage), phase);
+        if (ok) release();
+      };
+      while (ik < kLead && ok && has(ik, false)) pass_key();
+      for (int i = 0; ok && has(i, false); ++i) {
+        ok = wait_warp(full_bar(stage), phase);
+        if (!ok) break;
+        uint32_t f;
+        const int t = tile_of(i, f);
+        if (f & kTileDead) {
+          uint8_t* v = smem + Cfg::kRing + stage * Cfg::kTileBytes;
+          int2 iv[kAttnTile / 32];
+          tile_intervals(a, s, t, lane, iv);
+#pragma unroll 1
+          for (int e = 0; e < kAttnTile / 32; ++e) {
+            if (iv[e].y != 0) continue;
+            uint8_t* at = v + (e * 32 + lane) * 128;
+            for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+              for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(at + c * (kAttnTile * 128) + x * 16) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(clean_bar);
+        }
+        release();
+        if (has(ik, false)) pass_key();
+      }
     }
-  }
   } else {
     // ---------------- rows ----------------
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    {
+      const int qmin = range[0], qmax = range[1];    // all rows padding: qmax is -1 and no tile is visible
+      for (int t = t0 + warp - 4; t < t_far; t += 8) {
+        const uint32_t f = qmax < 0 ? 0u : tile_flags(a, s, t, qmin, qmax, lane);
+        if (lane == 0) list[t - t0] = f;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(flag_bar);
+    }
     const int st = (warp - 4) >> 2;                    // stream
     const int quarter = warp & 3;
     const int row = quarter * 32 + lane;
@@ -495,24 +608,18 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     const float c = a.scale * 1.4426950408889634f;
     float m = -INFINITY, l = 0.f;
     int done = 0;                                      // tiles of this stream so far
-    uint32_t masked = 0;
+    int masked = 0;                                    // tiles with intervals so far, of both streams
     bool ok = true;
     const bool active = TWO ? (st == 0 || two) : true;
-    int t = next_tile(tile0);
-    for (int i = 0; i < ntile && ok && active; ++i, t = next_tile(t + 1)) {
-      if (!TWO && (i & 1) != st) continue;
-      const uint32_t f = flags_of(t);
-      int2* mk = mask + (st * 2 + (masked & 1u)) * kAttnTile;
-      if (f & kTileMasked) {
-        mk[row] = slot_interval(a, s, t * kAttnTile + row);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(m_bar(st));
+    for (int i = 0; ok && active && has(i, false); ++i) {
+      uint32_t f;
+      tile_of(i, f);
+      if (!TWO && (i & 1) != st) {
+        masked += (f & kTileMasked) ? 1 : 0;
+        continue;
       }
       ok = wait_warp(s_bar(st), (uint32_t)done & 1u);
-      if (ok && (f & kTileMasked)) {
-        ok = wait_warp(m_bar(st), masked & 1u);
-        ++masked;
-      }
+      if (ok && (f & kTileMasked)) ok = wait_warp(m_full(masked % kMaskRing), (uint32_t)(masked / kMaskRing) & 1u);
       if (!ok) break;
       tc_fence_after();
       if (warp_in) {
@@ -520,19 +627,29 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 #pragma unroll
         for (int j = 0; j < 4; ++j) ATTS_TMEM_LD_32(t_s + 32u * j, (&v[32 * j]));
         tmem_ld_wait();
-        if (f & kTileMasked) {
+        if ((f & 0xFFu) != kTileFull) {
+          const int2* mk = mask + (masked % kMaskRing) * kAttnTile;
 #pragma unroll
-          for (int j = 0; j < 128; j += 2) {
-            const int4 w = *reinterpret_cast<const int4*>(mk + j);
-            if ((unsigned)(mine - w.x) >= (unsigned)w.y) v[j] = 0xFF800000u;
-            if ((unsigned)(mine - w.z) >= (unsigned)w.w) v[j + 1] = 0xFF800000u;
+          for (int g = 0; g < 4; ++g) {
+            const uint32_t kind = (f >> (2 * g)) & 3u;
+            if (kind == 0u) {
+#pragma unroll
+              for (int j = 32 * g; j < 32 * g + 32; ++j) v[j] = 0xFF800000u;
+            } else if (kind == 1u) {
+#pragma unroll
+              for (int j = 32 * g; j < 32 * g + 32; j += 2) {
+                const int4 w = *reinterpret_cast<const int4*>(mk + j);
+                if ((unsigned)(mine - w.x) >= (unsigned)w.y) v[j] = 0xFF800000u;
+                if ((unsigned)(mine - w.z) >= (unsigned)w.w) v[j + 1] = 0xFF800000u;
+              }
+            }
           }
         }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < 128; j += 4)
+        for (int j = 0; j < 128; j += 8)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], __uint_as_float(v[j + e]));
+          for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], __uint_as_float(v[j + e]), __uint_as_float(v[j + 4 + e]));
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         // the reference moves when a row's maximum passes it by more than 8 (base 2), and for the first visible slot
         float keep = 1.f;
@@ -548,47 +665,51 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
           rescale_o<D>(t_o, keep);
         }
         const float off = (m == -INFINITY ? 0.f : -m * c) + AttnType<T>::shift;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
+        uint64_t sum2[2] = {0, 0};
 #pragma unroll
         for (int j = 0; j < 128; j += 32) {
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const float p0 = ex2_approx(fmaf(__uint_as_float(v[j + e]), c, off));
-            const float p1 = ex2_approx(fmaf(__uint_as_float(v[j + e + 1]), c, off));
-            sum[e & 2] += p0;
-            sum[(e & 2) + 1] += p1;
+            const uint64_t x = fma2(pair2(__uint_as_float(v[j + e]), __uint_as_float(v[j + e + 1])), c2, off2);
+            const float p0 = ex2_approx(low2(x)), p1 = ex2_approx(high2(x));
+            sum2[(e >> 1) & 1] = add2(sum2[(e >> 1) & 1], pair2(p0, p1));
             w[e / 2] = Pack<T>::pack(p0, p1);
           }
           ATTS_TMEM_ST_16(t_s + (uint32_t)(j / 2), w);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        const uint64_t sum = add2(sum2[0], sum2[1]);
+        l += low2(sum) + high2(sum);
         tmem_st_wait();
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(p_bar(st));
+      if (lane == 0) {
+        mbar_arrive(p_bar(st));
+        if (f & kTileMasked) mbar_arrive(m_empty(masked % kMaskRing));
+      }
+      masked += (f & kTileMasked) ? 1 : 0;
       ++done;
     }
     if (active && ok && done > 0) ok = wait_warp(o_bar(st), (uint32_t)(done - 1) & 1u);
     tc_fence_after();
-    // ---- join of the two streams (one row tile): the odd one hands its sums over through the ring, which is free ----
+    // ---- join of the two streams (one row tile): the odd one hands its sums over through the ring, which is free once
+    // every product has finished: this stream's last one has; the other's last but one has, and its last is waited for ----
     float2 other = make_float2(-INFINITY, 0.f);
     const bool joined = !TWO && ntile > 1;
     float* pass = reinterpret_cast<float*>(smem + Cfg::kRing);
     if (joined && st == 1) {
-      // the ring is free once every product has finished: this stream's last one has, the other's has when it gets here
-      if (ok && ntile > 0) ok = wait_warp(o_bar(0), (uint32_t)((ntile + 1) / 2 - 1) & 1u);
+      if (ok) ok = wait_warp(o_bar(0), (uint32_t)((ntile + 1) / 2 - 1) & 1u);
       if (ok && warp_in) {
         stats[row] = make_float2(m, l);
 #pragma unroll 1
-        for (int j = 0; j < D / 32; ++j) {
+        for (int j = 0; j < D; j += 32) {   // run once: short code costs less to fetch than unrolled code saves
           uint32_t v[32];
-          ATTS_TMEM_LD_32(t_o + 32u * j, v);
+          ATTS_TMEM_LD_32(t_o + (uint32_t)j, v);
           tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            *reinterpret_cast<uint4*>(pass + row * (D + 4) + 32 * j + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+          for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(pass + row * (D + 4) + j + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
         }
       }
       __syncwarp();
@@ -615,31 +736,31 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         else if (a.lse) a.lse[r] = lse2 * 0.6931471805599453f;
       }
 #pragma unroll 1
-      for (int j = 0; j < D / 32; ++j) {
-        uint32_t v[32];
+      for (int j = 0; j < D; j += 16) {
+        uint32_t v[16];
         if (done > 0) {
-          ATTS_TMEM_LD_32(t_o + 32u * j, v);
+          ATTS_TMEM_LD_16(t_o + (uint32_t)j, v);
           tmem_ld_wait();
         }
-        float o[32];
+        float o[16];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = empty || done == 0 ? 0.f : __uint_as_float(v[i]) * g0;
+        for (int e = 0; e < 16; ++e) o[e] = empty || done == 0 ? 0.f : __uint_as_float(v[e]) * g0;
         if (joined && !empty) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float4 x = *reinterpret_cast<const float4*>(pass + row * (D + 4) + 32 * j + i);
-            o[i] += x.x * g1; o[i + 1] += x.y * g1; o[i + 2] += x.z * g1; o[i + 3] += x.w * g1;
+          for (int e = 0; e < 16; e += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(pass + row * (D + 4) + j + e);
+            o[e] += x.x * g1; o[e + 1] += x.y * g1; o[e + 2] += x.z * g1; o[e + 3] += x.w * g1;
           }
         }
         if (in) {
           if (parts > 1) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + 32 * j + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + j + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           } else {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              *reinterpret_cast<uint4*>(out + 32 * j + i) = make_uint4(Pack<T>::pack(o[i], o[i + 1]), Pack<T>::pack(o[i + 2], o[i + 3]),
-                                                                      Pack<T>::pack(o[i + 4], o[i + 5]), Pack<T>::pack(o[i + 6], o[i + 7]));
+            for (int e = 0; e < 16; e += 8)
+              *reinterpret_cast<uint4*>(out + j + e) = make_uint4(Pack<T>::pack(o[e], o[e + 1]), Pack<T>::pack(o[e + 2], o[e + 3]),
+                                                                 Pack<T>::pack(o[e + 4], o[e + 5]), Pack<T>::pack(o[e + 6], o[e + 7]));
           }
         }
       }
@@ -758,7 +879,6 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   const int tpt = a.tpt, nq = (s.n + tpt - 1) / tpt;                 // row tiles; this CTA's are rank, rank + ranks, ...
   const int mine_n = nq > rank ? (nq - rank + ranks - 1) / ranks : 0;
   const int ncols = (tpt * a.q.G + 31) & ~31;
-  const bool cached = slot0 + kAttnTile <= s.ctx;
 
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -829,14 +949,14 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       }
       any = __any_sync(0xFFFFFFFFu, any) && qmax >= 0;
       all = __all_sync(0xFFFFFFFFu, all) && whole;
-      if (lane == 0) flags[i] = !any ? 0u : all ? (uint8_t)kTileFull : (uint8_t)kTileMasked;
+      if (lane == 0) flags[i] = !any ? 0u : all ? 2u : 1u;   // as a group of slots: 1 pairs differ, 2 all
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  auto flags_of = [&](int i) -> uint32_t { return i < kWeightTiles ? flags[i] : (uint32_t)kTileMasked; };
+  auto flags_of = [&](int i) -> uint32_t { return i < kWeightTiles ? flags[i] : 1u; };
   auto next_tile = [&](int i) {
     while (i < mine_n && flags_of(i) == 0u) ++i;
     return i;
@@ -851,22 +971,15 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 
   if (warp == 0) {
     if (!a.withhold_loads && work) {
-      const int pl = a.q.cache.page_log2;
-      const int rows = min(1 << pl, kAttnTile);
-      const int boxes = (kAttnTile / rows) * (D / 64);
-      const int bslot = (lane / (D / 64)) * rows, bcol = (lane % (D / 64)) * 64;
+      const TileBoxes<D> bx(a.q.cache.page_log2, lane);
+      int page = a.q.cache.num_pages;                           // out of the map: filled with zeros
+      if (lane < bx.boxes && slot0 + bx.slot < s.len) {
+        const int p = cache_page(a.q.cache, seq, slot0 + bx.slot, dev_status);
+        if (p >= 0) page = p;
+      }
       if (lane == 0) mbar_expect_tx(k_bar, Cfg::kTileBytes);
       __syncwarp();
-      if (lane < boxes) {
-        const int slot = slot0 + bslot;
-        int page = a.q.cache.num_pages;
-        if (slot < s.len) {
-          const int p = cache_page(a.q.cache, seq, slot, dev_status);
-          if (p >= 0) page = p;
-        }
-        tma_load_4d(smem_base + (uint32_t)(bcol / 64) * (kAttnTile * 128) + (uint32_t)bslot * 128u, &map_k, k_bar, bcol,
-                    slot & ((1 << pl) - 1), hk, page);
-      }
+      bx.issue(smem_base, &map_k, k_bar, tile, hk, page, lane);
       if (lane == 0) {
         uint32_t phase = 0;
         int stage = 0;
@@ -932,7 +1045,7 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       if (!wait_warp(c_bar(st), (uint32_t)k & 1u) || !wait_warp(s_full(st), (uint32_t)k & 1u)) break;
       tc_fence_after();
       if (warp_in) {
-        const bool masked = (flags_of(i) & kTileMasked) != 0u;
+        const bool masked = flags_of(i) == 1u;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
         for (int j = 0; j < ncols; j += 32) {
           uint32_t v[32];
