@@ -50,6 +50,15 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
 // registers than the issuing thread has, and every spilled one costs the tensor pipe a trip to L2.
 constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);   // groups of eight rows 1024 bytes apart, 128-byte swizzle
 __device__ __forceinline__ uint32_t desc_low(uint32_t smem_addr, uint32_t lbo) { return (smem_addr >> 4) | ((lbo >> 4) << 16); }
+// One lane of a converged warp, always the same one.  A whole warp runs the issuing loops and one lane is elected around the
+// products themselves: their operands then stay in the warp's uniform registers.  Issued from a loop that one lane runs by itself
+// every operand is moved there first: about 110 cycles a product instead of the 64 that it takes the tensor pipe.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0u;
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 // D[tmem] (+)= A[smem] * B[smem]^T, both at `step` 16-byte units from their descriptors.
 __device__ __forceinline__ void umma_ss(uint32_t tmem_d, uint32_t a_low, uint32_t b_low, uint32_t step, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -442,77 +451,81 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       }
     } else if (warp == 1) {
       // ---------------- products ----------------
-      if (lane == 0 && has(0, true)) {
-        constexpr uint32_t kFmt = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24);
-        constexpr uint32_t kIdescS = kFmt | ((uint32_t)(kAttnTile >> 3) << 17);
-        constexpr uint32_t kIdescO = kFmt | (1u << 16) | ((uint32_t)(D >> 3) << 17);   // B with its N dimension contiguous
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = wait_one(q_bar, 0);
-        uint32_t p_phase = 0, clean_phase = 0;   // a bit per stream
-        auto qk = [&](int i, int at) {   // S_i = Q (of stream i if TWO) K^T of the stage's tile
-          const uint32_t sa = smem_base + (TWO ? (uint32_t)i * Cfg::kTileBytes : 0u);
-          const uint32_t sb = smem_base + Cfg::kRing + (uint32_t)at * Cfg::kTileBytes;
-          const uint32_t da = desc_low(sa, 16), db = desc_low(sb, 16);   // K contiguous: the leading offset is unused
+      constexpr uint32_t kFmt = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24);
+      constexpr uint32_t kIdescS = kFmt | ((uint32_t)(kAttnTile >> 3) << 17);
+      constexpr uint32_t kIdescO = kFmt | (1u << 16) | ((uint32_t)(D >> 3) << 17);   // B with its N dimension contiguous
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = has(0, false) && wait_warp(q_bar, 0);
+      uint32_t p_phase = 0, clean_phase = 0;   // a bit per stream
+      const int streams = TWO ? (two ? 2 : 1) : 1;   // that use each tile
+      const uint32_t tm = uniform(tmem_base), base = uniform(smem_base);
+      // S_st = Q (of stream st if TWO) K^T of the tile in stage `at`; `last`: nothing else reads the stage
+      auto qk = [&](int st, int at, bool last) {
+        const uint32_t u = uniform((uint32_t)st), ring = uniform((uint32_t)at);
+        const uint32_t da = desc_low(base + (TWO ? u * Cfg::kTileBytes : 0u), 16);   // K contiguous: the leading offset is unused
+        const uint32_t db = desc_low(base + Cfg::kRing + ring * Cfg::kTileBytes, 16);
+        if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / kUmmaK; ++k)
-            umma_ss(tmem_base + (uint32_t)i * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), kIdescS, (uint32_t)(k != 0));
-          umma_commit(s_bar(i));
-        };
-        const int streams = TWO ? (two ? 2 : 1) : 1;   // that use each tile
-        for (int ik = 0; ik < kLead && ok && has(ik, true); ++ik) {
-          ok = wait_one(full_bar(stage), phase);
-          if (!ok) break;
-          tc_fence_after();
-          for (int u = 0; u < streams; ++u) qk(TWO ? u : ik & 1, stage);
-          umma_commit(empty_bar(stage));
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            umma_ss(tm + u * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), kIdescS, (uint32_t)(k != 0));
+          umma_commit(s_bar(0) + 8u * u);
+          if (last) umma_commit(empty_bar(0) + 8u * ring);
         }
-        for (int i = 0; ok && has(i, true); ++i) {
-          uint32_t f;
-          tile_of(i, f);
-          ok = wait_one(full_bar(stage), phase);
-          if (ok && (f & kTileDead)) {
-            ok = wait_one(clean_bar, clean_phase);
-            clean_phase ^= 1u;
-          }
-          const bool more = ok && has(i + kLead, true);
-          if (!ok) break;
-          tc_fence_after();
-          const int vstage = stage;
-          const int kstage = stage + 1 == kStages ? 0 : stage + 1;
-          const uint32_t kphase = stage + 1 == kStages ? phase ^ 1u : phase;
-          for (int u = 0; u < streams && ok; ++u) {
-            const int st = TWO ? u : i & 1;
-            ok = wait_one(p_bar(st), (p_phase >> st) & 1u);
-            if (!ok) break;
-            p_phase ^= 1u << st;
-            tc_fence_after();
-            // channels contiguous: blocks of 64 channels kAttnTile * 128 bytes apart, 16 slots are two groups of eight rows
-            const uint32_t db = desc_low(smem_base + Cfg::kRing + (uint32_t)vstage * Cfg::kTileBytes, kAttnTile * 128);
-            const bool first = TWO ? i == 0 : i < 2;
-#pragma unroll
-            for (int k = 0; k < kAttnTile / kUmmaK; ++k)
-              umma_ts(tmem_base + 256u + (uint32_t)st * D, tmem_base + (uint32_t)st * kAttnTile, db, 8u * k, (uint32_t)(k * (kUmmaK * 128 / 16)),
-                      kIdescO, (uint32_t)(!first || k != 0));
-            umma_commit(o_bar(st));
-            if (u + 1 == streams) umma_commit(empty_bar(vstage));
-            if (more) {
-              if (u == 0) {
-                ok = wait_one(full_bar(kstage), kphase);
-                if (!ok) break;
-                tc_fence_after();
-              }
-              qk(st, kstage);
-              if (u + 1 == streams) umma_commit(empty_bar(kstage));
-            }
-          }
-          if (!ok) break;
-          for (int u = 0; u < (more ? 2 : 1); ++u)
-            if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        }
+        __syncwarp();
+      };
+      for (int ik = 0; ik < kLead && ok && has(ik, false); ++ik) {
+        ok = wait_warp(full_bar(stage), phase);
+        if (!ok) break;
+        tc_fence_after();
+        for (int u = 0; u < streams; ++u) qk(TWO ? u : ik & 1, stage, u + 1 == streams);
+        if (++stage == kStages) { stage = 0; phase ^= 1u; }
       }
-      __syncwarp();
+      for (int i = 0; ok && has(i, false); ++i) {
+        uint32_t f;
+        tile_of(i, f);
+        ok = wait_warp(full_bar(stage), phase);
+        if (ok && (f & kTileDead)) {
+          ok = wait_warp(clean_bar, clean_phase);
+          clean_phase ^= 1u;
+        }
+        const bool more = ok && has(i + kLead, false);
+        if (!ok) break;
+        const int vstage = stage;
+        const int kstage = stage + 1 == kStages ? 0 : stage + 1;
+        const uint32_t kphase = stage + 1 == kStages ? phase ^ 1u : phase;
+        for (int w = 0; w < streams && ok; ++w) {
+          const int st = TWO ? w : i & 1;
+          ok = wait_warp(p_bar(st), (p_phase >> st) & 1u);
+          if (!ok) break;
+          p_phase ^= 1u << st;
+          tc_fence_after();
+          {
+            const uint32_t u = uniform((uint32_t)st), ring = uniform((uint32_t)vstage), more_o = uniform((uint32_t)(TWO ? i > 0 : i > 1));
+            // channels contiguous: blocks of 64 channels kAttnTile * 128 bytes apart, 16 slots are two groups of eight rows
+            const uint32_t db = desc_low(base + Cfg::kRing + ring * Cfg::kTileBytes, kAttnTile * 128);
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < kAttnTile / kUmmaK; ++k)
+                umma_ts(tm + 256u + u * D, tm + u * kAttnTile, db, 8u * k, (uint32_t)(k * (kUmmaK * 128 / 16)), kIdescO, k == 0 ? more_o : 1u);
+              umma_commit(o_bar(0) + 8u * u);
+              if (w + 1 == streams) umma_commit(empty_bar(0) + 8u * ring);
+            }
+            __syncwarp();
+          }
+          if (more) {
+            if (w == 0) {
+              ok = wait_warp(full_bar(kstage), kphase);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            qk(st, kstage, w + 1 == streams);
+          }
+        }
+        if (!ok) break;
+        for (int u = 0; u < (more ? 2 : 1); ++u)
+          if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      }
     } else {
       // ---------------- the list of visible tiles behind the cached part; then, along the ring, the intervals of tiles that
       // need them, and zeros over the values of slots that hold nothing ----------------
@@ -729,41 +742,62 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       const float lse2 = empty ? -INFINITY : mm * c - AttnType<T>::shift + log2f(sum);
       const int parts = (ntiles + plan.chunk - 1) / plan.chunk;
       const int64_t r = token * a.Hq + head;
-      T* out = reinterpret_cast<T*>(a.out) + token * a.o_ts + (int64_t)head * a.o_hs;
-      float* part = plan.part_o + (r * plan.chunks + chunk) * D;
       if (in) {
         if (parts > 1) plan.part_lse[r * plan.chunks + chunk] = lse2;
         else if (a.lse) a.lse[r] = lse2 * 0.6931471805599453f;
       }
+      // Rows go out through the queries' shared memory, D * 2 bytes of each at a time (whole rows in the outputs' type, halves of
+      // the fp32 sums of a chunk), so that a store covers whole rows: written by its own thread, a row's pieces would
+      // cost one access to L1 each (4,000 cycles of 74,000 in a tile of 12).
+      constexpr int kLanes = D / 8, kRowBytes = D * 2;               // lanes that share a row
+      uint8_t* buf = smem + (TWO ? st * Cfg::kTileBytes : 0) + quarter * 32 * kRowBytes;
+      char* dst = parts > 1 ? reinterpret_cast<char*>(plan.part_o + (r * plan.chunks + chunk) * D)
+                            : a.out + 2 * (token * a.o_ts + (int64_t)head * a.o_hs);
+      const uint32_t rows = __ballot_sync(0xFFFFFFFFu, in);
+      const int sub = lane % kLanes;
+      auto rows_out = [&](int offset) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; i += 32 / kLanes) {
+          const int from = i + lane / kLanes;
+          const uint64_t to = __shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(dst), from);
+          if ((rows >> from) & 1u)
+            *reinterpret_cast<uint4*>(to + offset + sub * 16) = *reinterpret_cast<const uint4*>(buf + from * kRowBytes + ((sub ^ (from & 7)) * 16));
+        }
+        __syncwarp();
+      };
+      uint8_t* mine_at = buf + lane * kRowBytes;
 #pragma unroll 1
-      for (int j = 0; j < D; j += 16) {
-        uint32_t v[16];
+      for (int j = 0; j < D; j += 32) {
+        uint32_t v[32];
         if (done > 0) {
-          ATTS_TMEM_LD_16(t_o + (uint32_t)j, v);
+          ATTS_TMEM_LD_32(t_o + (uint32_t)j, v);
           tmem_ld_wait();
         }
-        float o[16];
+        float o[32];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = empty || done == 0 ? 0.f : __uint_as_float(v[e]) * g0;
+        for (int e = 0; e < 32; ++e) o[e] = empty || done == 0 ? 0.f : __uint_as_float(v[e]) * g0;
         if (joined && !empty) {
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) {
+          for (int e = 0; e < 32; e += 4) {
             const float4 x = *reinterpret_cast<const float4*>(pass + row * (D + 4) + j + e);
             o[e] += x.x * g1; o[e + 1] += x.y * g1; o[e + 2] += x.z * g1; o[e + 3] += x.w * g1;
           }
         }
-        if (in) {
-          if (parts > 1) {
+        if (parts > 1) {
+          const int at = j % (D / 2);
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(part + j + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-          } else {
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<float4*>(mine_at + ((((at + e) / 4) ^ (lane & 7)) * 16)) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          if (at + 32 == D / 2) rows_out((j / (D / 2)) * kRowBytes);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 16; e += 8)
-              *reinterpret_cast<uint4*>(out + j + e) = make_uint4(Pack<T>::pack(o[e], o[e + 1]), Pack<T>::pack(o[e + 2], o[e + 3]),
-                                                                 Pack<T>::pack(o[e + 4], o[e + 5]), Pack<T>::pack(o[e + 6], o[e + 7]));
-          }
+          for (int e = 0; e < 32; e += 8)
+            *reinterpret_cast<uint4*>(mine_at + ((((j + e) / 8) ^ (lane & 7)) * 16)) =
+                make_uint4(Pack<T>::pack(o[e], o[e + 1]), Pack<T>::pack(o[e + 2], o[e + 3]), Pack<T>::pack(o[e + 4], o[e + 5]), Pack<T>::pack(o[e + 6], o[e + 7]));
         }
       }
+      if (parts <= 1) rows_out(0);
     }
   }
 
@@ -996,25 +1030,28 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0 && work && wait_one(k_bar, 0)) {
+    if (work && wait_warp(k_bar, 0)) {
       const uint32_t idesc = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24) |
-                             ((uint32_t)(ncols >> 3) << 17);
+                             (uniform((uint32_t)ncols >> 3) << 17);
+      const uint32_t tm = uniform(tmem_base), base = uniform(smem_base), da = desc_low(base, 16);
       uint32_t phase = 0;
       int stage = 0;   // stage, accumulator and stream at once
       for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1)) {
-        if (!wait_one(q_full(stage), phase) || !wait_one(s_empty(stage), phase ^ 1u)) break;
+        if (!wait_warp(q_full(stage), phase) || !wait_warp(s_empty(stage), phase ^ 1u)) break;
         tc_fence_after();
-        const uint32_t da = desc_low(smem_base, 16), db = desc_low(smem_base + Cfg::kQ + (uint32_t)stage * Cfg::kTileBytes, 16);
+        const uint32_t u = uniform((uint32_t)stage), db = desc_low(base + Cfg::kQ + u * Cfg::kTileBytes, 16);
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < D / kUmmaK; ++k)
-          umma_ss(tmem_base + (uint32_t)stage * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), idesc, (uint32_t)(k != 0));
-        umma_commit(q_empty(stage));
-        umma_commit(s_full(stage));
+          for (int k = 0; k < D / kUmmaK; ++k)
+            umma_ss(tm + u * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), idesc, (uint32_t)(k != 0));
+          umma_commit(q_empty(0) + 8u * u);
+          umma_commit(s_full(0) + 8u * u);
+        }
+        __syncwarp();
         stage ^= 1;
         phase ^= (uint32_t)(stage == 0);
       }
     }
-    __syncwarp();
   } else {
     const int st = (warp - 2) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t t_s = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)st * kAttnTile;
