@@ -392,9 +392,17 @@ int atts_cache_select(const float* weights, int64_t weights_cols, const int32_t*
   int st = device_info(&di);
   if (st != ATTS_OK) return st;
   if (num_seqs == 0) return ATTS_OK;
-  cache_select_kernel<<<(unsigned)(num_seqs * heads), kSelectThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
-      weights, weights_cols, lens, heads, (int)budget, (int)sinks, (int)recent, kept, counts, di->dev_status);
-  return launch_status();
+  const SelectArgs a{weights, weights_cols, lens, heads, (int)budget, (int)sinks, (int)recent, kept, counts};
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const dim3 grid((unsigned)(num_seqs * heads));
+  // the smallest number of keys a thread (of 1024, or of fewer for the shortest rows) that covers a row
+  if (weights_cols > kSelectMaxItems * kSelectThreads)
+    return launch_pdl(cache_select_long_kernel, grid, dim3(kSelectThreads), 0, stream, a, di->dev_status);
+  const unsigned threads = weights_cols >= kSelectThreads ? kSelectThreads : (unsigned)round_up((size_t)(weights_cols < 1 ? 1 : weights_cols), 32);
+  if (weights_cols <= 1024) return launch_pdl(cache_select_kernel<1>, grid, dim3(threads), 0, stream, a, di->dev_status);
+  if (weights_cols <= 4096) return launch_pdl(cache_select_kernel<4>, grid, dim3(threads), 0, stream, a, di->dev_status);
+  if (weights_cols <= 12288) return launch_pdl(cache_select_kernel<12>, grid, dim3(threads), 0, stream, a, di->dev_status);
+  return launch_pdl(cache_select_kernel<kSelectMaxItems>, grid, dim3(threads), 0, stream, a, di->dev_status);
 }
 
 int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kept_cols, const int32_t* counts,
@@ -414,11 +422,12 @@ int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kep
   st = device_info(&di);
   if (st != ATTS_OK) return st;
   if (src->num_seqs == 0 || kept_cols == 0) return ATTS_OK;
-  const int64_t gx = (kept_cols * (src->head_dim / 8) + 255) / 256;
-  const dim3 grid((unsigned)gx, (unsigned)src->heads, (unsigned)src->num_seqs);
-  cache_gather_kernel<<<grid, 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(s, d, src->head_dim, kept, kept_cols, counts,
-                                                                                weights_in, in_cols, weights_out, di->dev_status);
-  return launch_status();
+  const int lanes = src->head_dim / 8, per = kGatherThreads / lanes * kGatherRows;
+  const int64_t gx = (kept_cols + per - 1) / per * src->heads;
+  if (gx > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  const dim3 grid((unsigned)gx, (unsigned)src->num_seqs);
+  return launch_pdl(cache_gather_kernel, grid, dim3(kGatherThreads), 0, static_cast<cudaStream_t>(cuda_stream), s, d, lanes, kept, kept_cols,
+                    counts, weights_in, in_cols, weights_out, di->dev_status);
 }
 
 }  // extern "C"

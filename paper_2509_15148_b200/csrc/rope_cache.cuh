@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "conformal.cuh"
+
 namespace atts {
 
 constexpr unsigned kDevPageRange = 16u, kDevSeqRange = 32u;  // ATTS_DEV_PAGE_RANGE, ATTS_DEV_SEQ_RANGE
@@ -194,11 +196,17 @@ rope_append_kernel(const RopeArgs a, unsigned* __restrict__ dev_status) {
 
 // ------------------------------------------------------------------------------------------------------------------
 // Eviction, selection.  Weights are ordered by a monotone 32-bit key (-0 as +0; NaN below every number); the slots that
-// stay in any case get the largest key.  One block per (sequence, head) finds the key of the last slot to keep digit by
-// digit (four digits of eight bits, a histogram each over the slots that still match), then writes the slots above it
-// and, from the lowest on, as many of the slots equal to it as there is room for.
-// ------------------------------------------------------------------------------------------------------------------
+// stay in any case get the largest key.  T, the budget-th largest key, is found from its highest bit down: a bit of T is
+// set if at least `budget` keys are not below T with it.  Kept are the keys above T and, from the lowest slot on, as many
+// of those equal to T as there is room for.  As soon as a count is the budget itself the set is known.
+//
+// Rows of up to 32,768 slots: one block, its keys in registers (a warp owns consecutive slots, so one scan over the warps
+// places everything).  A pass over all keys costs a comparison and an addition each and one barrier; once no more keys than
+// threads lie between the bounds of T, those go to shared memory and the remaining bits are found among them, two a
+// pass.  (A histogram of digits needs fewer passes over the keys, but weights share a few exponents and its atomics then
+// meet in a few bins: 87 us for 64 rows of 32,000 slots, 47 us with all passes over all keys.)
 constexpr int kSelectThreads = 1024;
+constexpr int kSelectMaxItems = 32;     // keys of a thread: rows of up to 32 * 1024 slots
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t u = __float_as_uint(w);
@@ -207,47 +215,195 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);     // -inf has key 0x007FFFFF, +inf 0xFF800000
 }
 
+struct SelectArgs {
+  const float* weights;
+  int64_t cols;
+  const int32_t* lens;
+  int heads, budget, sinks, recent;
+  int32_t *kept, *counts;
+};
+
+// Length of the block's row, the counts' entry, and rows that keep everything; false: nothing is left to do.
+__device__ __forceinline__ bool select_row(const SelectArgs& a, int& len, unsigned* dev_status) {
+  const int seq = blockIdx.x / a.heads;
+  const int len0 = a.lens[seq];
+  len = (int)max((int64_t)0, min((int64_t)len0, a.cols));
+  if (threadIdx.x == 0 && blockIdx.x == seq * a.heads) {
+    if (len != len0) atomicOr(dev_status, kDevSeqRange);
+    a.counts[seq] = min(len, a.budget);
+  }
+  if (len > a.budget) return true;
+  int32_t* out = a.kept + (int64_t)blockIdx.x * a.budget;
+  for (int i = threadIdx.x; i < a.budget; i += blockDim.x) out[i] = i < len ? i : -1;
+  return false;
+}
+
+template <int ITEMS>
 __global__ void __launch_bounds__(kSelectThreads)
-cache_select_kernel(const float* __restrict__ weights, int64_t cols, const int32_t* __restrict__ lens, int heads, int budget,
-                    int sinks, int recent, int32_t* __restrict__ kept, int32_t* __restrict__ counts,
-                    unsigned* __restrict__ dev_status) {
+cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
+  pdl_wait();
+  __shared__ uint32_t part[2][3][32];
+  __shared__ uint32_t window[kSelectThreads];
+  __shared__ uint32_t windowed;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  int len;
+  if (!select_row(a, len, dev_status)) return;
+  const float* w = a.weights + (int64_t)blockIdx.x * a.cols;
+  const int first = warp * 32 * ITEMS + lane;             // this thread's slots: first + 32 k
+  uint32_t key[ITEMS];
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = first + 32 * k;
+    key[k] = i < len ? __float_as_uint(w[i]) : 0u;
+  }
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const int i = first + 32 * k;
+    key[k] = i >= len ? 0u : (i < a.sinks || i >= len - a.recent) ? 0xFFFFFFFFu : weight_key(__uint_as_float(key[k]));
+  }
+  // Slots behind the row have key 0, like NaNs: never above T, and last in the order among equals.
+  const uint32_t budget = (uint32_t)a.budget;
+  uint32_t T = 0, at_t = (uint32_t)(ITEMS * blockDim.x), above = 0;   // keys >= T, keys above the bits still open
+  bool exact = false;     // as many keys >= T as are kept
+  int shift = 31, buf = 0;
+  auto total = [&](int c) { return __reduce_add_sync(0xFFFFFFFFu, lane < warps ? part[buf][c][lane] : 0u); };
+  if (tid == 0) windowed = 0;
+  if (ITEMS > 1) {
+    for (; shift >= 0 && !exact && at_t - above > blockDim.x; --shift, buf ^= 1) {
+      const uint32_t cand = T | (1u << shift);
+      uint32_t n = 0;
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) n += key[k] >= cand ? 1u : 0u;
+      n = __reduce_add_sync(0xFFFFFFFFu, n);
+      if (lane == 0) part[buf][0][warp] = n;
+      __syncthreads();    // the other buffer is written next: nobody can be a whole pass behind
+      n = total(0);
+      if (n >= budget) {
+        T = cand;
+        at_t = n;
+        exact = n == budget;
+      } else {
+        above = n;
+      }
+    }
+  }
+  if (shift >= 0 && !exact) {
+    uint32_t mine = 0;
+    if (ITEMS > 1) {
+      const uint32_t span = shift == 31 ? 0xFFFFFFFFu : (2u << shift) - 1u;   // T .. T + span are open
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k)
+        if (key[k] - T <= span) window[atomicAdd(&windowed, 1u)] = key[k];
+      __syncthreads();
+      if (tid < (int)windowed) mine = window[tid];
+    } else {
+      mine = key[0];
+    }
+    while (shift >= 0 && !exact) {
+      const int bits = shift >= 1 ? 2 : 1, low = shift + 1 - bits, cands = (1 << bits) - 1;
+      for (int c = 0; c < cands; ++c) {
+        const uint32_t n = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine >= (T | ((uint32_t)(c + 1) << low))));
+        if (lane == 0) part[buf][c][warp] = n;
+      }
+      __syncthreads();
+      for (int c = cands - 1; c >= 0; --c) {
+        const uint32_t n = above + total(c);
+        if (n >= budget) {
+          T |= (uint32_t)(c + 1) << low;
+          exact = n == budget;
+          break;
+        }
+      }
+      // (`above` counts keys beyond the window; those inside it are all counted again)
+      shift -= bits;
+      buf ^= 1;
+    }
+  }
+  // places: keys above T (or all from T on, if that is exactly the budget), then the first ones equal to it
+  uint32_t gt = 0, eq = 0;
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    gt += key[k] > T ? 1u : 0u;
+    eq += key[k] == T ? 1u : 0u;
+  }
+  gt = __reduce_add_sync(0xFFFFFFFFu, gt);
+  eq = __reduce_add_sync(0xFFFFFFFFu, eq);
+  __syncthreads();
+  uint32_t* sum = &part[0][0][0];
+  uint32_t* sum_eq = &part[1][0][0];
+  if (lane == 0) {
+    sum[warp] = gt;
+    sum_eq[warp] = eq;
+  }
+  __syncthreads();
+  uint32_t all_gt = lane < warps ? sum[lane] : 0u, all_eq = lane < warps ? sum_eq[lane] : 0u;
+  const uint32_t before_gt = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? all_gt : 0u);
+  const uint32_t before_eq = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? all_eq : 0u);
+  all_gt = __reduce_add_sync(0xFFFFFFFFu, all_gt);
+  const uint32_t need = budget - all_gt;                  // of the keys equal to T
+  uint32_t g = before_gt, e = before_eq;
+  const uint32_t lower = (1u << lane) - 1u;
+  int32_t* out = a.kept + (int64_t)blockIdx.x * a.budget;
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    const bool is_gt = key[k] > T, is_eq = key[k] == T;
+    const uint32_t bg = __ballot_sync(0xFFFFFFFFu, is_gt), be = __ballot_sync(0xFFFFFFFFu, is_eq);
+    const uint32_t my_e = e + __popc(be & lower);
+    if (is_gt || (is_eq && my_e < need)) out[g + __popc(bg & lower) + min(my_e, need)] = first + 32 * k;
+    g += __popc(bg);
+    e += __popc(be);
+  }
+}
+
+// Longer rows: digits of eight bits, a histogram each over the slots that still match.  Lanes that hit the same bin count
+// together first.
+__global__ void __launch_bounds__(kSelectThreads)
+cache_select_long_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
+  pdl_wait();
   __shared__ uint32_t hist[256];
   __shared__ uint32_t scan[32];
   __shared__ uint32_t sh_prefix, sh_need;
-  const int seq = blockIdx.x / heads, head = blockIdx.x - seq * heads;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int len0 = lens[seq];
-  const int len = (int)max((int64_t)0, min((int64_t)len0, cols));
-  if (tid == 0 && head == 0) {
-    if (len != len0) atomicOr(dev_status, kDevSeqRange);
-    counts[seq] = min(len, budget);
-  }
-  const float* w = weights + (int64_t)blockIdx.x * cols;
-  int32_t* out = kept + (int64_t)blockIdx.x * budget;
-  if (len <= budget) {
-    for (int i = tid; i < budget; i += kSelectThreads) out[i] = i < len ? i : -1;
-    return;
-  }
-  auto key_of = [&](int i) { return (i < sinks || i >= len - recent) ? 0xFFFFFFFFu : weight_key(w[i]); };
-  uint32_t prefix = 0, need = (uint32_t)budget;  // need: rank, among the matching slots, of the last one to keep
+  int len;
+  if (!select_row(a, len, dev_status)) return;
+  const float* w = a.weights + (int64_t)blockIdx.x * a.cols;
+  int32_t* out = a.kept + (int64_t)blockIdx.x * a.budget;
+  auto key_of = [&](int i) { return (i < a.sinks || i >= len - a.recent) ? 0xFFFFFFFFu : weight_key(w[i]); };
+  uint32_t prefix = 0, need = (uint32_t)a.budget;  // need: rank, among the matching slots, of the last one to keep
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
     __syncthreads();
     const uint32_t mask = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
-    for (int i = tid; i < len; i += kSelectThreads) {
-      const uint32_t k = key_of(i);
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    for (int base = 0; base < len; base += kSelectThreads) {
+      const int i = base + tid;
+      uint32_t k = 0;
+      bool hit = i < len;
+      if (hit) {
+        k = key_of(i);
+        hit = (k & mask) == prefix;
+      }
+      const uint32_t bin = hit ? (k >> shift) & 255u : 256u;
+      const uint32_t same = __match_any_sync(0xFFFFFFFFu, bin);
+      if (hit && (same & ((1u << lane) - 1u)) == 0u) atomicAdd(&hist[bin], (uint32_t)__popc(same));
     }
     __syncthreads();
-    if (tid == 0) {
-      uint32_t above = 0;
-      int d = 255;
-      for (; d > 0; --d) {
-        if (above + hist[d] >= need) break;
-        above += hist[d];
+    if (warp == 0) {   // lane 0 has the highest eight bins
+      uint32_t own = 0;
+      for (int d = 0; d < 8; ++d) own += hist[255 - lane * 8 - d];
+      uint32_t upto = own;
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += x;
       }
-      sh_prefix = prefix | ((uint32_t)d << shift);
-      sh_need = need - above;
+      const uint32_t has = __ballot_sync(0xFFFFFFFFu, upto >= need);   // some lane's: the matching slots are at least `need`
+      if (lane == __ffs(has) - 1) {
+        uint32_t above = upto - own;
+        int d = 255 - lane * 8;
+        while (above + hist[d] < need) above += hist[d--];
+        sh_prefix = prefix | ((uint32_t)d << shift);
+        sh_need = need - above;
+      }
     }
     __syncthreads();
     prefix = sh_prefix;
@@ -262,11 +418,8 @@ cache_select_kernel(const float* __restrict__ weights, int64_t cols, const int32
     const uint32_t bg = __ballot_sync(0xFFFFFFFFu, gt), be = __ballot_sync(0xFFFFFFFFu, eq);
     if (lane == 0) scan[warp] = (uint32_t)__popc(bg) | ((uint32_t)__popc(be) << 16);
     __syncthreads();
-    uint32_t before = 0, total = 0;
-    for (int j = 0; j < 32; ++j) {
-      if (j < warp) before += scan[j];
-      total += scan[j];
-    }
+    const uint32_t mine = scan[lane];
+    const uint32_t before = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? mine : 0u), total = __reduce_add_sync(0xFFFFFFFFu, mine);
     const uint32_t lower = (1u << lane) - 1u;
     const uint32_t g = done + (before & 0xFFFFu) + __popc(bg & lower);
     const uint32_t e = equal_done + (before >> 16) + __popc(be & lower);
@@ -278,39 +431,73 @@ cache_select_kernel(const float* __restrict__ weights, int64_t cols, const int32
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Eviction, move.  One warp-wide copy per kept row: D / 8 threads per (sequence, slot, head).
+// Eviction, move.  D / 8 threads share a kept row, 16 bytes of its key and of its value each; a thread takes kGatherRows rows
+// whose look-ups (slot, page, page) and loads are under way together: the chain of four dependent accesses, not the
+// bandwidth, is what a row by itself waits for (8 x 32,000 slots cut to 8192: 110 us with one row a thread).
 // ------------------------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256)
-cache_gather_kernel(const CacheView src, const CacheView dst, int D, const int32_t* __restrict__ kept, int64_t kept_cols,
+constexpr int kGatherThreads = 256, kGatherRows = 4;
+
+__global__ void __launch_bounds__(kGatherThreads)
+cache_gather_kernel(const CacheView src, const CacheView dst, int lanes, const int32_t* __restrict__ kept, int64_t kept_cols,
                     const int32_t* __restrict__ counts, const float* __restrict__ win, int64_t in_cols,
                     float* __restrict__ wout, unsigned* __restrict__ dev_status) {
-  const int seq = blockIdx.z, head = blockIdx.y;
-  const int lanes = D / 8;
-  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
-  const int piece = (int)(((int64_t)blockIdx.x * 256 + threadIdx.x) % lanes);
-  if (c >= kept_cols) return;
+  pdl_wait();
+  // blocks of the same slots and other heads run side by side: a slot's heads are neighbours in memory
+  const int seq = blockIdx.y, head = blockIdx.x % src.heads;
+  const int per = kGatherThreads / lanes;                          // rows of a block at a time
+  const int sub = threadIdx.x / lanes, piece = threadIdx.x - sub * lanes;
+  if (sub >= per) return;
   const int64_t row = (int64_t)seq * src.heads + head;
-  const bool live = c < counts[seq];
-  int slot = live ? kept[row * kept_cols + c] : -1;
-  if (live && slot < 0) {
-    atomicOr(dev_status, kDevPageRange);
-  } else if (live) {
-    const int from = cache_page(src, seq, slot, dev_status), to = cache_page(dst, seq, (int)c, dev_status);
-    if (from >= 0 && to >= 0) {
-      const int64_t a = cache_offset(src, from, slot) + head * src.head_stride + 8 * piece;
-      const int64_t b = cache_offset(dst, to, (int)c) + head * dst.head_stride + 8 * piece;
-      *reinterpret_cast<uint4*>(dst.k + 2 * b) = *reinterpret_cast<const uint4*>(src.k + 2 * a);
-      *reinterpret_cast<uint4*>(dst.v + 2 * b) = *reinterpret_cast<const uint4*>(src.v + 2 * a);
+  const int64_t c0 = (int64_t)(blockIdx.x / src.heads) * per * kGatherRows + sub;
+  const int64_t live_to = min((int64_t)counts[seq], kept_cols);
+  int slot[kGatherRows], from[kGatherRows], to[kGatherRows];
+#pragma unroll
+  for (int r = 0; r < kGatherRows; ++r) {
+    const int64_t c = c0 + (int64_t)r * per;
+    slot[r] = c < live_to ? kept[row * kept_cols + c] : -1;
+    const int col = (int)(c >> dst.page_log2);
+    to[r] = c < live_to ? (col < dst.table_cols ? dst.table[seq * dst.table_stride + col] : -1) : 0;
+  }
+#pragma unroll
+  for (int r = 0; r < kGatherRows; ++r) {
+    const int col = slot[r] >> src.page_log2;
+    from[r] = slot[r] < 0 ? -1 : (col < src.table_cols ? src.table[seq * src.table_stride + col] : -1);
+  }
+  uint4 k[kGatherRows], v[kGatherRows];
+  float w[kGatherRows];
+  unsigned bad = 0;
+#pragma unroll
+  for (int r = 0; r < kGatherRows; ++r) {
+    const int64_t c = c0 + (int64_t)r * per;
+    w[r] = 0.f;
+    if (c >= live_to) {
+      from[r] = -1;
+      continue;
+    }
+    const bool ok = from[r] >= 0 && from[r] < src.num_pages && to[r] >= 0 && to[r] < dst.num_pages;
+    if (!ok) {
+      bad = kDevPageRange;
+      from[r] = -1;
+    } else {
+      const int64_t at = 2 * (cache_offset(src, from[r], slot[r]) + head * src.head_stride + 8 * piece);
+      k[r] = *reinterpret_cast<const uint4*>(src.k + at);
+      v[r] = *reinterpret_cast<const uint4*>(src.v + at);
+    }
+    if (wout && piece == 0 && slot[r] >= 0) {
+      if (slot[r] < in_cols) w[r] = win[row * in_cols + slot[r]];
+      else bad = kDevPageRange;
     }
   }
-  if (wout && piece == 0) {
-    float x = 0.f;
-    if (live && slot >= 0) {
-      if (slot < in_cols) x = win[row * in_cols + slot];
-      else atomicOr(dev_status, kDevPageRange);
-    }
-    wout[row * kept_cols + c] = x;
+#pragma unroll
+  for (int r = 0; r < kGatherRows; ++r) {
+    const int64_t c = c0 + (int64_t)r * per;
+    if (c < kept_cols && wout && piece == 0) wout[row * kept_cols + c] = w[r];
+    if (from[r] < 0) continue;
+    const int64_t at = 2 * (cache_offset(dst, to[r], (int)c) + head * dst.head_stride + 8 * piece);
+    *reinterpret_cast<uint4*>(dst.k + at) = k[r];
+    *reinterpret_cast<uint4*>(dst.v + at) = v[r];
   }
+  if (bad) atomicOr(dev_status, bad);
 }
 
 }  // namespace atts
