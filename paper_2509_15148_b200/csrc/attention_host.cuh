@@ -89,6 +89,12 @@ static int encode_cache(const DeviceInfo* di, CUtensorMap* map, const atts_kv_ca
   return encode_rows(di, map, c->dtype == ATTS_BF16, base, 4, dims, st, box);
 }
 
+// Tokens of a row tile: as many as fit 128 rows, and no more than a sequence can have (the rest would be loaded in vain).
+static int row_tile_tokens(int G, int64_t max_tokens) {
+  const int fit = kAttnTile / G;
+  return max_tokens < 1 ? 1 : max_tokens < fit ? (int)max_tokens : fit;
+}
+
 // How an attention call is cut up.  Row tiles: as many whole tokens as fit 128 rows; two of them to a CTA if the longest
 // sequence has more than one.  Chunks: the number that makes the launch shortest when a slot tile takes one unit of time
 // (about 1.4 us: 64 KB per SM at the device's bandwidth), a CTA's start and end 2.5, writing and reading back its rows'
@@ -100,7 +106,7 @@ struct AttnShape {
 static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens, int64_t max_len) {
   AttnShape r{};
   const int G = Hq / heads;
-  r.p.tpt = kAttnTile / G;
+  r.p.tpt = row_tile_tokens(G, max_tokens);
   r.two = max_tokens > r.p.tpt;
   const int64_t per = r.p.tpt * (r.two ? 2 : 1);
   r.p.nq = (int)((max_tokens + per - 1) / per);
@@ -138,7 +144,7 @@ static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const 
   return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool MANY>
 static int launch_weights(const CUtensorMap& mq, const CUtensorMap& mk, const WeightArgs& a, dim3 grid, unsigned* status, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
@@ -152,7 +158,7 @@ static int launch_weights(const CUtensorMap& mq, const CUtensorMap& mk, const We
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.cluster > 1 ? 1 : 0;
-  if (cudaLaunchKernelEx(&cfg, cache_weights_kernel<T, D>, mq, mk, a, status) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, cache_weights_kernel<T, D, MANY>, mq, mk, a, status) != cudaSuccess) {
     cudaGetLastError();
     return ATTS_ERR_CUDA;
   }
@@ -360,14 +366,22 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
   a.q.scale = scale;
   a.lse = lse;
   a.win = weights_in; a.wout = weights_out; a.wcols = weights_cols;
-  a.tpt = kAttnTile / G;
+  a.tpt = row_tile_tokens(G, max_tokens);
   a.wait_limit = wait_limit();
   a.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
-  // a cluster's CTAs take at least two row tiles each
-  const int64_t nq = (max_tokens + a.tpt - 1) / a.tpt;
+  // One row tile: a CTA goes over as many slot tiles as leave two CTAs an SM something to do, eight at most (measured on 8 x
+  // 2000 slots of 8 heads: spans 1, 2, 4, 8 take @SPANS@).  More: slot tiles are dealt to clusters whose CTAs take at
+  // least two row tiles each.
+  const int64_t nq = (max_tokens + a.tpt - 1) / a.tpt, tiles = (max_len + kAttnTile - 1) / kAttnTile;
+  const bool many = nq > 1;
   a.cluster = 1;
-  while (a.cluster < kWeightMaxCluster && nq >= 4 * a.cluster) a.cluster *= 2;
-  const int64_t gx = (max_len + kAttnTile - 1) / kAttnTile * a.cluster;
+  a.span = 1;
+  if (many) {
+    while (a.cluster < kWeightMaxCluster && nq >= 4 * a.cluster) a.cluster *= 2;
+  } else {
+    while (a.span < 8 && tiles * cache->heads * cache->num_seqs > 2 * a.span * (int64_t)di->sm_count) a.span *= 2;
+  }
+  const int64_t gx = many ? tiles * a.cluster : (tiles + a.span - 1) / a.span;
   const dim3 grid((unsigned)gx, (unsigned)cache->heads, (unsigned)cache->num_seqs);
   CUtensorMap mq, mk;
   // without queries (M == 0) the kernel only writes; the map then describes the cache's keys and is not used
@@ -376,8 +390,12 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
     return ATTS_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const bool bf = cache->dtype == ATTS_BF16;
-  if (cache->head_dim == 128) return bf ? launch_weights<__nv_bfloat16, 128>(mq, mk, a, grid, di->dev_status, stream) : launch_weights<__half, 128>(mq, mk, a, grid, di->dev_status, stream);
-  return bf ? launch_weights<__nv_bfloat16, 64>(mq, mk, a, grid, di->dev_status, stream) : launch_weights<__half, 64>(mq, mk, a, grid, di->dev_status, stream);
+#define ATTS_WEIGH(D, MANY)                                                                  \
+  (bf ? launch_weights<__nv_bfloat16, D, MANY>(mq, mk, a, grid, di->dev_status, stream)      \
+      : launch_weights<__half, D, MANY>(mq, mk, a, grid, di->dev_status, stream))
+  if (cache->head_dim == 128) return many ? ATTS_WEIGH(128, true) : ATTS_WEIGH(128, false);
+  return many ? ATTS_WEIGH(64, true) : ATTS_WEIGH(64, false);
+#undef ATTS_WEIGH
 }
 
 int atts_cache_select(const float* weights, int64_t weights_cols, const int32_t* lens, int64_t num_seqs, int32_t heads,

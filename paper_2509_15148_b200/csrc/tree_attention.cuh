@@ -864,80 +864,134 @@ struct WeightArgs {
   const float* win;
   float* wout;
   int64_t wcols;
-  int tpt, cluster;        // tokens per row tile, CTAs that share a slot tile's queries
+  int tpt;                 // tokens per row tile
+  int cluster, span;       // CTAs that share a slot tile's row tiles; slot tiles of a CTA that has one row tile
   long long wait_limit;
   int withhold_loads;
 };
 
 // ------------------------------------------------------------------------------------------------------------------
-// Attention weight per slot.  A CTA takes one tile of 128 slots of one key head and goes over row tiles of queries:
+// Attention weight per slot.  The product of one slot tile (128 slots of a key head) and one row tile of queries is
 //   S^T = K Q^T (tcgen05, fp32 in tensor memory), a thread per slot, and each thread adds 2^(c s - lse2) over the columns
-// of its own row: no sum crosses threads, so the order is fixed and nothing is stored but one number per slot.  Even and
-// odd row tiles go to two groups of four warps with an accumulator each, and two CTAs share an SM: the exponentials (one
-// per visible pair, 16 a clock and SM) are what the time goes to.  Long query lists are dealt to the CTAs of a cluster,
-// whose first one adds up their sums in order through the cluster's shared memory.
+// of its own row: no sum crosses threads, so the order is fixed and nothing is stored but one number per slot.  Products
+// alternate between two groups of four warps with an accumulator each, and two CTAs share an SM: the exponentials (one per
+// pair, 16 a clock and SM) are what the time goes to.
+//
+// One operand stays, the other streams.  MANY = false (one row tile covers every sequence's drafts): the queries stay and a CTA
+// goes over `span` slot tiles.  MANY = true: a slot tile stays and the row tiles stream.  Every row sees the cached slots,
+// so their tiles are dealt to the CTAs of a cluster, whose first one adds up the sums in order through the cluster's shared
+// memory; behind the cached part a tree's tile is seen by its own branch only and a CTA takes it alone (a chain's tiles
+// are seen by all later rows and are dealt like cached ones).
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kWeightThreads = 320;     // warp 0 loads, warp 1 products, 2-5 and 6-9 slots
-constexpr int kWeightTiles = 512;       // row tiles of a CTA whose visibility is looked up ahead
+constexpr int kWeightItems = 1024;      // products of a CTA whose visibility is looked up ahead; further ones are all made
 constexpr int kWeightMaxCluster = 8;
 
 template <int D>
 struct WeightCfg {
   static constexpr int kTileBytes = kAttnTile * D * 2;
-  static constexpr int kQ = kTileBytes;                            // two stages
-  static constexpr int kCols = kQ + 2 * kTileBytes;                // [2 streams][2][128] lse2, then places
-  static constexpr int kFlags = kCols + 2 * 4 * kAttnTile * 4;
-  static constexpr int kSums = kFlags + kWeightTiles;              // [cluster][128] sums, [128] of the odd stream
+  static constexpr int kRing = kTileBytes;                         // the operand that stays, then two stages
+  static constexpr int kCols = kRing + 2 * kTileBytes;             // [2 groups][2][128] -lse2, then places
+  static constexpr int kFlags = kCols + 2 * 4 * kAttnTile * 4;     // [items] bytes
+  static constexpr int kList = kFlags + kWeightItems;              // [items] uint16
+  static constexpr int kSums = kList + 2 * kWeightItems;           // [cluster][128] sums, [128] of the odd group
   static constexpr int kBars = kSums + (kWeightMaxCluster + 1) * kAttnTile * 4;
   static constexpr int kSmemBytes = kBars + 128 + 1024;
 };
 
-template <typename T, int D>
+// Sum over one accumulator's 32 columns from `v` on: 2^(c s - lse2), pairs of columns side by side.
+template <bool MASKED>
+__device__ __forceinline__ void weight_columns(uint32_t (&v)[32], const float* nlse, const int* place, int2 iv, uint64_t c2, uint64_t (&sum)[2]) {
+  if (MASKED) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+      const int4 w = *reinterpret_cast<const int4*>(place + e);
+      if ((unsigned)(w.x - iv.x) >= (unsigned)iv.y) v[e] = 0xFF800000u;
+      if ((unsigned)(w.y - iv.x) >= (unsigned)iv.y) v[e + 1] = 0xFF800000u;
+      if ((unsigned)(w.z - iv.x) >= (unsigned)iv.y) v[e + 2] = 0xFF800000u;
+      if ((unsigned)(w.w - iv.x) >= (unsigned)iv.y) v[e + 3] = 0xFF800000u;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) {
+    const float4 w = *reinterpret_cast<const float4*>(nlse + e);
+    const uint64_t x = fma2(pair2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), c2, pair2(w.x, w.y));
+    const uint64_t y = fma2(pair2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), c2, pair2(w.z, w.w));
+    sum[0] = add2(sum[0], pair2(ex2_approx(low2(x)), ex2_approx(high2(x))));
+    sum[1] = add2(sum[1], pair2(ex2_approx(low2(y)), ex2_approx(high2(y))));
+  }
+}
+
+template <typename T, int D, bool MANY>
 __global__ void __launch_bounds__(kWeightThreads, 2)
 cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ WeightArgs a, unsigned* __restrict__ dev_status) {
   using Cfg = WeightCfg<D>;
   extern __shared__ uint8_t smem_raw[];
-  const int ranks = a.cluster, rank = blockIdx.x % ranks, tile = blockIdx.x / ranks, hk = blockIdx.y, seq = blockIdx.z;
+  const int hk = blockIdx.y, seq = blockIdx.z;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   SeqView s;
   const bool ok_seq = seq_view(a.q.cu, a.q.ctx, seq, a.q.M, a.q.max_tokens, a.q.max_len, s, dev_status,
                                threadIdx.x == 0 && blockIdx.x == 0 && hk == 0);
-  const int slot0 = tile * kAttnTile;
+  const int tpt = a.tpt, nq = (s.n + tpt - 1) / tpt;
+  // this CTA's slot tiles [tile0, tile1), and for MANY its row tiles q0, q0 + step, ...
+  int ranks = 1, rank = 0, tile0, tile1, q0 = 0, step = 1;
+  if (MANY) {
+    const int in_cluster = blockIdx.x % a.cluster, cluster = blockIdx.x / a.cluster;
+    const int dealt = !ok_seq ? 0 : a.q.pre ? min((s.ctx + kAttnTile - 1) / kAttnTile, (s.len + kAttnTile - 1) / kAttnTile) : (s.len + kAttnTile - 1) / kAttnTile;
+    if (cluster < dealt) {      // the same for every CTA of a cluster
+      ranks = a.cluster;
+      rank = q0 = in_cluster;
+      step = a.cluster;
+      tile0 = cluster;
+    } else {
+      tile0 = dealt + (cluster - dealt) * a.cluster + in_cluster;
+    }
+    tile1 = tile0 + 1;
+  } else {
+    tile0 = blockIdx.x * a.span;
+    tile1 = min(tile0 + a.span, (a.q.max_len + kAttnTile - 1) / kAttnTile);
+  }
   float* wout = a.wout + ((int64_t)seq * a.q.cache.heads + hk) * a.wcols;
   const float* win = a.win ? a.win + ((int64_t)seq * a.q.cache.heads + hk) * a.wcols : nullptr;
-  if (!ok_seq || slot0 >= s.len || s.n == 0) {   // the same for every CTA of a cluster
-    const int slot = slot0 + threadIdx.x;
-    if (rank == 0 && threadIdx.x < kAttnTile && slot < a.q.max_len) wout[slot] = ok_seq && slot < s.len && win ? win[slot] : 0.f;
+  const int len = ok_seq ? s.len : 0;
+  auto old_weight = [&](int slot) { return win && slot < len ? win[slot] : 0.f; };
+  if ((int64_t)tile0 * kAttnTile >= a.q.max_len) return;       // (a cluster behind the dealt tiles reaches beyond the row)
+  if (tile0 * kAttnTile >= len || s.n == 0) {
+    for (int slot = tile0 * kAttnTile + threadIdx.x; slot < min(tile1 * kAttnTile, a.q.max_len); slot += kWeightThreads) wout[slot] = old_weight(slot);
     return;
   }
-  const int tpt = a.tpt, nq = (s.n + tpt - 1) / tpt;                 // row tiles; this CTA's are rank, rank + ranks, ...
-  const int mine_n = nq > rank ? (nq - rank + ranks - 1) / ranks : 0;
+  const int items = MANY ? (nq > q0 ? (nq - q0 + step - 1) / step : 0) : min(tile1, (len + kAttnTile - 1) / kAttnTile) - tile0;
   const int ncols = (tpt * a.q.G + 31) & ~31;
+  auto slot_tile = [&](int i) { return MANY ? tile0 : tile0 + i; };
+  auto row_tile = [&](int i) { return MANY ? q0 + i * step : 0; };
 
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
   float* col_lse = reinterpret_cast<float*>(smem + Cfg::kCols);
   int* col_place = reinterpret_cast<int*>(smem + Cfg::kCols + 4 * kAttnTile * 4);
-  uint8_t* flags = smem + Cfg::kFlags;
+  uint32_t* flags = reinterpret_cast<uint32_t*>(smem + Cfg::kFlags);
+  volatile uint16_t* list = reinterpret_cast<volatile uint16_t*>(smem + Cfg::kList);
   float* sums = reinterpret_cast<float*>(smem + Cfg::kSums);
   const uint32_t bar0 = smem_base + Cfg::kBars;
-  const uint32_t k_bar = bar0;
-  auto q_full = [&](int i) { return bar0 + 8u + 8u * (uint32_t)i; };
-  auto q_empty = [&](int i) { return bar0 + 24u + 8u * (uint32_t)i; };
+  const uint32_t stay_bar = bar0;
+  auto r_full = [&](int i) { return bar0 + 8u + 8u * (uint32_t)i; };
+  auto r_empty = [&](int i) { return bar0 + 24u + 8u * (uint32_t)i; };
   auto s_full = [&](int i) { return bar0 + 40u + 8u * (uint32_t)i; };
   auto s_empty = [&](int i) { return bar0 + 56u + 8u * (uint32_t)i; };
   auto c_bar = [&](int i) { return bar0 + 72u + 8u * (uint32_t)i; };
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kBars + 88);
   volatile uint32_t* abort_flag = tmem_slot + 1;
+  volatile int* listed = reinterpret_cast<volatile int*>(tmem_slot + 2);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < kWeightItems / 4; i += kWeightThreads) flags[i] = 0;
   if (threadIdx.x == 0) {
     prefetch_tmap(&map_q);
     prefetch_tmap(&map_k);
-    mbar_init(k_bar, 1);
+    mbar_init(stay_bar, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(q_full(i), 1);
-      mbar_init(q_empty(i), 1);
+      mbar_init(r_full(i), 1);
+      mbar_init(r_empty(i), 1);
       mbar_init(s_full(i), 1);
       mbar_init(s_empty(i), 4);
       mbar_init(c_bar(i), 4);
@@ -949,56 +1003,102 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"(256u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // rows of a query tile that no token fills stay zero (a box never writes them)
-  for (int i = threadIdx.x; i < 2 * (D / 64) * (kAttnTile - tpt * a.q.G) * 8; i += kWeightThreads) {
-    const int x = i & 7, r = (i >> 3) % (kAttnTile - tpt * a.q.G), blk = (i >> 3) / (kAttnTile - tpt * a.q.G);
-    *reinterpret_cast<uint4*>(smem + Cfg::kQ + blk * (kAttnTile * 128) + (tpt * a.q.G + r) * 128 + x * 16) = make_uint4(0, 0, 0, 0);
-  }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  // which row tiles see any of these slots, and which see all of them from all rows
+  // rows of a query tile that no token fills, up to the columns used, are zero (a box never writes them)
   {
-    int2 v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = slot_interval(a.q, s, slot0 + e * 32 + lane);
-    const int live = s.len - slot0;
-    for (int i = warp; i < min(mine_n, kWeightTiles); i += kWeightThreads / 32) {
-      const int t0 = (rank + i * ranks) * tpt, nt = min(tpt, s.n - t0);
-      int qmin = 0x7FFFFFFF, qmax = -1;
-      bool whole = nt == tpt;
-      for (int t = lane; t < nt; t += 32) {
-        const int p = a.q.pre ? a.q.pre[s.first + t0 + t] : t0 + t;
-        if (p >= 0) qmin = min(qmin, p);
-        else whole = false;
-        qmax = max(qmax, p);
-      }
-      qmin = __reduce_min_sync(0xFFFFFFFFu, qmin);
-      qmax = __reduce_max_sync(0xFFFFFFFFu, qmax);
-      whole = __all_sync(0xFFFFFFFFu, whole);
-      bool any = false, all = true;
+    const int used = tpt * a.q.G, rows = ncols - used, tiles = MANY ? 2 : 1;
+    uint8_t* q = smem + (MANY ? Cfg::kRing : 0);
+    for (int r = warp; r < rows * tiles * (D / 64); r += kWeightThreads / 32) {
+      const int blk = r / rows;
+      if (lane < 8) *reinterpret_cast<uint4*>(q + blk * (kAttnTile * 128) + (used + r - blk * rows) * 128 + lane * 16) = make_uint4(0, 0, 0, 0);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  // Which products have anything visible: bit 0 of an item's byte, some row may see some slot; bit 1, some pair is not visible.
+  // A slot tile's intervals are taken together: nobody outside of [lo, hi) sees anything, everybody in [in_lo, in_hi) sees all.
+  const int known = min(items, kWeightItems);
+  __syncthreads();
+  {
+    auto bounds = [&](int tile, int& lo, int& hi, int& in_lo, int& in_hi) {
+      int2 v[4];
+      tile_intervals(a.q, s, tile, lane, v);
+      lo = in_hi = 0x7FFFFFFF;
+      hi = in_lo = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const unsigned last = (unsigned)v[e].x + (unsigned)v[e].y;
-        any |= v[e].y != 0 && v[e].x <= qmax && (unsigned)qmin < last;
-        all &= e * 32 + lane >= live || (v[e].y != 0 && v[e].x <= qmin && (unsigned)qmax < last);
+        const int end = (int)min((unsigned)v[e].x + (unsigned)v[e].y, 0x7FFFFFFFu);
+        const bool none = v[e].y == 0;
+        if (!none) {
+          lo = min(lo, v[e].x);
+          hi = max(hi, end);
+          in_lo = max(in_lo, v[e].x);
+          in_hi = min(in_hi, end);
+        } else if (tile * kAttnTile + e * 32 + lane < s.len) {
+          in_hi = -1;            // padding: nobody sees all
+        }
       }
-      any = __any_sync(0xFFFFFFFFu, any) && qmax >= 0;
-      all = __all_sync(0xFFFFFFFFu, all) && whole;
-      if (lane == 0) flags[i] = !any ? 0u : all ? 2u : 1u;   // as a group of slots: 1 pairs differ, 2 all
+      lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+      hi = __reduce_max_sync(0xFFFFFFFFu, hi);
+      in_lo = __reduce_max_sync(0xFFFFFFFFu, in_lo);
+      in_hi = __reduce_min_sync(0xFFFFFFFFu, in_hi);
+    };
+    int lo, hi, in_lo, in_hi;
+    if (MANY) {
+      bounds(tile0, lo, hi, in_lo, in_hi);
+      for (int t = threadIdx.x; t < s.n; t += kWeightThreads) {
+        const int tile = t / tpt, i = (tile - q0) / step;
+        if (tile < q0 || tile != q0 + i * step || i >= known) continue;
+        const int p = a.q.pre ? a.q.pre[s.first + t] : t;
+        uint32_t f = p >= lo && p < hi ? 1u : 0u;
+        if (!(p >= in_lo && p < in_hi) || (tile + 1) * tpt > s.n) f |= 2u;
+        if (f) atomicOr(&flags[i >> 2], f << (8 * (i & 3)));
+      }
+    } else {
+      for (int i = warp; i < known; i += kWeightThreads / 32) {
+        bounds(tile0 + i, lo, hi, in_lo, in_hi);
+        uint32_t f = s.n != tpt ? 2u : 0u;
+        for (int t = lane; t < s.n; t += 32) {
+          const int p = a.q.pre ? a.q.pre[s.first + t] : t;
+          if (p >= lo && p < hi) f |= 1u;
+          if (!(p >= in_lo && p < in_hi)) f |= 2u;
+        }
+        f = __reduce_or_sync(0xFFFFFFFFu, f);
+        if (lane == 0) atomicOr(&flags[i >> 2], f << (8 * (i & 3)));
+      }
     }
+  }
+  __syncthreads();
+  if (warp == 0) {     // the visible ones in order; bit 15: pairs have to be looked at one by one
+    int n = 0;
+    for (int base = 0; base < known; base += 32) {
+      const int i = base + lane;
+      const uint32_t f = i < known ? (flags[i >> 2] >> (8 * (i & 3))) & 3u : 0u;
+      const uint32_t some = __ballot_sync(0xFFFFFFFFu, f & 1u);
+      if (f & 1u) list[n + __popc(some & ((1u << lane) - 1u))] = (uint16_t)(i | (f & 2u ? 0x8000 : 0));
+      n += __popc(some);
+    }
+    if (lane == 0) *listed = n;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  auto flags_of = [&](int i) -> uint32_t { return i < kWeightTiles ? flags[i] : 1u; };
-  auto next_tile = [&](int i) {
-    while (i < mine_n && flags_of(i) == 0u) ++i;
-    return i;
+  const int nlist = *listed, count = nlist + items - known;     // products that are made
+  auto item_of = [&](int n, bool& masked) -> int {
+    if (n < nlist) {
+      const int e = list[n];
+      masked = (e & 0x8000) != 0;
+      return e & 0x7FFF;
+    }
+    masked = true;
+    return known + n - nlist;
+  };
+  auto item = [&](int n) -> int {
+    bool masked;
+    return item_of(n, masked);
   };
   const long long limit = a.wait_limit;
-  auto wait_one = [&](uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity, abort_flag, limit, 0u); };
-  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, wait_one(bar, parity)) != 0; };
-  const bool work = next_tile(0) < mine_n;
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, limit, 0u)) != 0; };
+  const bool work = count > 0;
   float total = 0.f;
   // another CTA's shared memory may be written once that CTA runs: awaited below
   if (ranks > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -1006,134 +1106,161 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   if (warp == 0) {
     if (!a.withhold_loads && work) {
       const TileBoxes<D> bx(a.q.cache.page_log2, lane);
-      int page = a.q.cache.num_pages;                           // out of the map: filled with zeros
-      if (lane < bx.boxes && slot0 + bx.slot < s.len) {
-        const int p = cache_page(a.q.cache, seq, slot0 + bx.slot, dev_status);
-        if (p >= 0) page = p;
-      }
-      if (lane == 0) mbar_expect_tx(k_bar, Cfg::kTileBytes);
-      __syncwarp();
-      bx.issue(smem_base, &map_k, k_bar, tile, hk, page, lane);
-      if (lane == 0) {
-        uint32_t phase = 0;
-        int stage = 0;
-        for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1)) {
-          if (!wait_one(q_empty(stage), phase ^ 1u)) break;
-          mbar_expect_tx(q_full(stage), (uint32_t)(a.q.G * tpt * D * 2));
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_3d(smem_base + Cfg::kQ + (uint32_t)stage * Cfg::kTileBytes + (uint32_t)c * (kAttnTile * 128), &map_q, q_full(stage),
-                        c * 64, hk * a.q.G, s.first + (rank + i * ranks) * tpt);
-          stage ^= 1;
-          phase ^= (uint32_t)(stage == 0);
+      auto page_of = [&](int tile) {
+        const int slot = tile * kAttnTile + bx.slot;
+        if (tile >= tile1 || lane >= bx.boxes || slot >= s.len) return a.q.cache.num_pages;   // out of the map: filled with zeros
+        const int p = cache_page(a.q.cache, seq, slot, dev_status);
+        return p >= 0 ? p : a.q.cache.num_pages;
+      };
+      auto load_rows = [&](uint32_t dst, uint32_t bar, int tile) {
+        if (lane == 0) {
+          mbar_expect_tx(bar, (uint32_t)(a.q.G * tpt * D * 2));
+          for (int c = 0; c < D / 64; ++c) tma_load_3d(dst + (uint32_t)c * (kAttnTile * 128), &map_q, bar, c * 64, hk * a.q.G, s.first + tile * tpt);
         }
+        __syncwarp();
+      };
+      auto load_slots = [&](uint32_t dst, uint32_t bar, int tile, int page) {
+        if (lane == 0) mbar_expect_tx(bar, Cfg::kTileBytes);
+        __syncwarp();
+        bx.issue(dst, &map_k, bar, tile, hk, page, lane);
+      };
+      int page = page_of(slot_tile(item(0)));
+      if (MANY) load_slots(smem_base, stay_bar, tile0, page);
+      else load_rows(smem_base, stay_bar, 0);
+      for (int n = 0; n < count; ++n) {
+        const int next_page = MANY || n + 1 >= count ? 0 : page_of(slot_tile(item(n + 1)));
+        const int stage = n & 1;
+        if (!wait_warp(r_empty(stage), ((uint32_t)(n >> 1) & 1u) ^ 1u)) break;
+        const uint32_t dst = smem_base + Cfg::kRing + (uint32_t)stage * Cfg::kTileBytes;
+        if (MANY) load_rows(dst, r_full(stage), row_tile(item(n)));
+        else load_slots(dst, r_full(stage), slot_tile(item(n)), page);
+        page = next_page;
       }
     }
-    __syncwarp();
   } else if (warp == 1) {
-    if (work && wait_warp(k_bar, 0)) {
+    if (work && wait_warp(stay_bar, 0)) {
       const uint32_t idesc = (1u << 4) | (AttnType<T>::fmt << 7) | (AttnType<T>::fmt << 10) | ((uint32_t)(kAttnTile >> 4) << 24) |
                              (uniform((uint32_t)ncols >> 3) << 17);
-      const uint32_t tm = uniform(tmem_base), base = uniform(smem_base), da = desc_low(base, 16);
-      uint32_t phase = 0;
-      int stage = 0;   // stage, accumulator and stream at once
-      for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1)) {
-        if (!wait_warp(q_full(stage), phase) || !wait_warp(s_empty(stage), phase ^ 1u)) break;
+      const uint32_t tm = uniform(tmem_base), base = uniform(smem_base), stay = desc_low(base, 16);
+      for (int n = 0; n < count; ++n) {
+        const int at = n & 1;   // stage, accumulator and group at once
+        const uint32_t phase = (uint32_t)(n >> 1) & 1u;
+        if (!wait_warp(r_full(at), phase) || !wait_warp(s_empty(at), phase ^ 1u)) break;
         tc_fence_after();
-        const uint32_t u = uniform((uint32_t)stage), db = desc_low(base + Cfg::kQ + u * Cfg::kTileBytes, 16);
+        const uint32_t u = uniform((uint32_t)at), ring = desc_low(base + Cfg::kRing + u * Cfg::kTileBytes, 16);
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / kUmmaK; ++k)
-            umma_ss(tm + u * kAttnTile, da, db, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), idesc, (uint32_t)(k != 0));
-          umma_commit(q_empty(0) + 8u * u);
+            umma_ss(tm + u * kAttnTile, MANY ? stay : ring, MANY ? ring : stay, (uint32_t)((k / 4) * (kAttnTile * 128 / 16) + (k % 4) * 2), idesc, (uint32_t)(k != 0));
+          umma_commit(r_empty(0) + 8u * u);
           umma_commit(s_full(0) + 8u * u);
         }
         __syncwarp();
-        stage ^= 1;
-        phase ^= (uint32_t)(stage == 0);
       }
     }
   } else {
     const int st = (warp - 2) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
     const uint32_t t_s = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)st * kAttnTile;
-    const int slot = slot0 + row;
-    const int2 iv = slot_interval(a.q, s, slot);
-    const bool warp_in = slot0 + quarter * 32 < s.len;
+    int2 iv = slot_interval(a.q, s, tile0 * kAttnTile + row);
     const float c = a.q.scale * 1.4426950408889634f;
-    // column `row` of a tile: which token and head it stands for
+    const uint64_t c2 = pair2(c, c);
+    // column `row` of a row tile: which token and head it stands for
     const int ct = row / a.q.G, ch = hk * a.q.G + row % a.q.G;
-    int n = 0, k = 0;   // tiles of all streams, of this one
-    for (int i = next_tile(0); i < mine_n; i = next_tile(i + 1), ++n) {
-      if ((n & 1) != st) continue;
-      float* lse = col_lse + (st * 2 + (k & 1)) * kAttnTile;
-      int* place = col_place + (st * 2 + (k & 1)) * kAttnTile;
-      const int t = (rank + i * ranks) * tpt + ct;
-      float l2 = INFINITY;
-      int p = -1;
+    auto column = [&](int tile, float& nl, int& p) {
+      const int t = tile * tpt + ct;
+      nl = -INFINITY;      // no row: 2^(x - inf) = 0
+      p = -1;
       if (ct < tpt && t < s.n) {
         const int64_t token = s.first + t;
         p = a.q.pre ? a.q.pre[token] : t;
         const float x = a.lse[token * a.q.Hq + ch];
-        if (x != -INFINITY) l2 = x * 1.4426950408889634f;
+        if (x != -INFINITY) nl = x * -1.4426950408889634f;
       }
-      lse[row] = l2;
-      place[row] = p;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(c_bar(st));
-      if (!wait_warp(c_bar(st), (uint32_t)k & 1u) || !wait_warp(s_full(st), (uint32_t)k & 1u)) break;
+    };
+    float nl;
+    int p;
+    bool ok = true;
+    if (st < count) column(row_tile(item(st)), nl, p);
+    for (int n = st, k = 0; n < count; n += 2, ++k) {
+      float* nlse = col_lse + (st * 2 + (MANY ? k & 1 : 0)) * kAttnTile;
+      int* place = col_place + (st * 2 + (MANY ? k & 1 : 0)) * kAttnTile;
+      bool masked;
+      const int i = item_of(n, masked);
+      const int slot = slot_tile(i) * kAttnTile + row;
+      if (MANY || k == 0) {
+        nlse[row] = nl;
+        place[row] = p;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c_bar(st));
+        ok = wait_warp(c_bar(st), (uint32_t)k & 1u);
+        if (MANY && n + 2 < count) column(row_tile(item(n + 2)), nl, p);   // the next one's, while this one's products are waited for
+      }
+      float before = 0.f;
+      if (!MANY) {
+        iv = slot_interval(a.q, s, slot);
+        before = old_weight(slot);
+      }
+      ok = ok && wait_warp(s_full(st), (uint32_t)k & 1u);
+      if (!ok) break;
       tc_fence_after();
+      const bool warp_in = slot - lane < s.len;
+      uint64_t sum[2] = {0, 0};
       if (warp_in) {
-        const bool masked = flags_of(i) == 1u;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int j = 0; j < ncols; j += 32) {
-          uint32_t v[32];
-          ATTS_TMEM_LD_32(t_s + (uint32_t)j, v);
+        uint32_t v[32], w[32];
+        ATTS_TMEM_LD_32(t_s, v);
+        for (int j = 0; j < ncols; j += 64) {   // the next 32 columns are read while these are worked on
           tmem_ld_wait();
-          if (masked) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const int4 w = *reinterpret_cast<const int4*>(place + j + e);
-              if ((unsigned)(w.x - iv.x) >= (unsigned)iv.y) v[e] = 0xFF800000u;
-              if ((unsigned)(w.y - iv.x) >= (unsigned)iv.y) v[e + 1] = 0xFF800000u;
-              if ((unsigned)(w.z - iv.x) >= (unsigned)iv.y) v[e + 2] = 0xFF800000u;
-              if ((unsigned)(w.w - iv.x) >= (unsigned)iv.y) v[e + 3] = 0xFF800000u;
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            const float4 w = *reinterpret_cast<const float4*>(lse + j + e);
-            sum[0] += ex2_approx(fmaf(__uint_as_float(v[e]), c, -w.x));
-            sum[1] += ex2_approx(fmaf(__uint_as_float(v[e + 1]), c, -w.y));
-            sum[2] += ex2_approx(fmaf(__uint_as_float(v[e + 2]), c, -w.z));
-            sum[3] += ex2_approx(fmaf(__uint_as_float(v[e + 3]), c, -w.w));
+          if (j + 32 < ncols) ATTS_TMEM_LD_32(t_s + (uint32_t)(j + 32), w);
+          if (masked) weight_columns<true>(v, nlse + j, place + j, iv, c2, sum);
+          else weight_columns<false>(v, nlse + j, place + j, iv, c2, sum);
+          if (j + 32 < ncols) {
+            tmem_ld_wait();
+            if (j + 64 < ncols) ATTS_TMEM_LD_32(t_s + (uint32_t)(j + 64), v);
+            if (masked) weight_columns<true>(w, nlse + j + 32, place + j + 32, iv, c2, sum);
+            else weight_columns<false>(w, nlse + j + 32, place + j + 32, iv, c2, sum);
           }
         }
-        total += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_empty(st));
-      ++k;
+      const uint64_t both = add2(sum[0], sum[1]);
+      const float x = low2(both) + high2(both);
+      if (MANY) total += x;
+      else if (slot < a.q.max_len) wout[slot] = slot < s.len ? before + x : 0.f;
     }
-    if (st == 1) sums[kWeightMaxCluster * kAttnTile + row] = total;
+    if (MANY) {
+      if (st == 1) sums[kWeightMaxCluster * kAttnTile + row] = total;
+    } else {
+      // tiles of which nothing is visible, and those behind the sequence
+      for (int t = tile0 + st; t < tile1; t += 2)
+        if (t - tile0 >= items || !((flags[(t - tile0) >> 2] >> (8 * ((t - tile0) & 3))) & 1u)) {   // (a span is at most 8 tiles)
+          const int slot = t * kAttnTile + row;
+          if (slot < a.q.max_len) wout[slot] = old_weight(slot);
+        }
+    }
   }
 
-  // ---------------- sums of the two streams, then of the cluster's CTAs in order ----------------
+  // ---------------- sums of the two groups, then of the cluster's CTAs in order ----------------
   tc_fence_before();
   __syncthreads();
-  if (ranks > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-  if (warp >= 2 && warp < 6) {
+  if (MANY) {
+    if (ranks > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     const int row = (warp & 3) * 32 + lane;
-    total += sums[kWeightMaxCluster * kAttnTile + row];
-    if (rank == 0) sums[row] = total;
-    else
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(smem_u32(sums + rank * kAttnTile + row), 0)), "f"(total) : "memory");
-  }
-  if (ranks > 1) cluster_sync_all();
-  if (rank == 0 && warp >= 2 && warp < 6) {
-    const int row = (warp & 3) * 32 + lane, slot = slot0 + row;
-    float w = 0.f;
-    for (int i = 0; i < ranks; ++i) w += sums[i * kAttnTile + row];
-    if (slot < a.q.max_len) wout[slot] = slot < s.len ? (win ? win[slot] : 0.f) + w : 0.f;
+    const bool first = warp >= 2 && warp < 6;
+    if (first) {
+      total += sums[kWeightMaxCluster * kAttnTile + row];
+      if (rank == 0) sums[row] = total;
+      else
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(smem_u32(sums + rank * kAttnTile + row), 0)), "f"(total) : "memory");
+    }
+    if (ranks > 1) cluster_sync_all();
+    if (rank == 0 && first) {
+      const int slot = tile0 * kAttnTile + row;
+      float w = 0.f;
+      for (int i = 0; i < ranks; ++i) w += sums[i * kAttnTile + row];
+      if (slot < a.q.max_len) wout[slot] = slot < s.len ? old_weight(slot) + w : 0.f;
+    }
   }
   if (*abort_flag) {
     if (threadIdx.x == 0) atomicOr(dev_status, 2u);
@@ -1153,7 +1280,9 @@ static cudaError_t attention_attributes_of() {
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(tree_attention_kernel<T, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, false>::kSmemBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(cache_weights_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightCfg<D>::kSmemBytes);
+    e = cudaFuncSetAttribute(cache_weights_kernel<T, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightCfg<D>::kSmemBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(cache_weights_kernel<T, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightCfg<D>::kSmemBytes);
   return e;
 }
 static cudaError_t attention_attributes() {
