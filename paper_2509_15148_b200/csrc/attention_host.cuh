@@ -381,8 +381,9 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
   } else {
     while (a.span < 8 && tiles * cache->heads * cache->num_seqs > 2 * a.span * (int64_t)di->sm_count) a.span *= 2;
   }
-  const int64_t gx = many ? tiles * a.cluster : (tiles + a.span - 1) / a.span;
-  const dim3 grid((unsigned)gx, (unsigned)cache->heads, (unsigned)cache->num_seqs);
+  const int64_t gx = (many ? tiles * a.cluster : (tiles + a.span - 1) / a.span) * cache->heads;
+  if (gx > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  const dim3 grid((unsigned)gx, (unsigned)cache->num_seqs);
   CUtensorMap mq, mk;
   // without queries (M == 0) the kernel only writes; the map then describes the cache's keys and is not used
   if (encode_queries(di, &mq, cache, M > 0 ? q : cache->k, q_token_stride, q_head_stride, M > 0 ? M : 1, M > 0 ? Hq : cache->heads, a.tpt) != ATTS_OK ||

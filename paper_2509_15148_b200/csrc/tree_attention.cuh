@@ -885,7 +885,7 @@ struct WeightArgs {
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kWeightThreads = 320;     // warp 0 loads, warp 1 products, 2-5 and 6-9 slots
 constexpr int kWeightItems = 1024;      // products of a CTA whose visibility is looked up ahead; further ones are all made
-constexpr int kWeightMaxCluster = 8;
+constexpr int kWeightMaxCluster = 4;     // larger ones leave SMs idle while they wait for room together
 
 template <int D>
 struct WeightCfg {
@@ -928,28 +928,31 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                      const __grid_constant__ WeightArgs a, unsigned* __restrict__ dev_status) {
   using Cfg = WeightCfg<D>;
   extern __shared__ uint8_t smem_raw[];
-  const int hk = blockIdx.y, seq = blockIdx.z;
+  // Heads run side by side (a slot's heads are neighbours in memory), and every head's cached tiles, which all rows see, come
+  // before the tiles behind them.
+  const int ranks_all = MANY ? a.cluster : 1;
+  const int in_cluster = blockIdx.x % ranks_all, group = blockIdx.x / ranks_all;
+  const int hk = group % a.q.cache.heads, unit = group / a.q.cache.heads, seq = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   SeqView s;
   const bool ok_seq = seq_view(a.q.cu, a.q.ctx, seq, a.q.M, a.q.max_tokens, a.q.max_len, s, dev_status,
-                               threadIdx.x == 0 && blockIdx.x == 0 && hk == 0);
+                               threadIdx.x == 0 && blockIdx.x == 0);
   const int tpt = a.tpt, nq = (s.n + tpt - 1) / tpt;
   // this CTA's slot tiles [tile0, tile1), and for MANY its row tiles q0, q0 + step, ...
   int ranks = 1, rank = 0, tile0, tile1, q0 = 0, step = 1;
   if (MANY) {
-    const int in_cluster = blockIdx.x % a.cluster, cluster = blockIdx.x / a.cluster;
     const int dealt = !ok_seq ? 0 : a.q.pre ? min((s.ctx + kAttnTile - 1) / kAttnTile, (s.len + kAttnTile - 1) / kAttnTile) : (s.len + kAttnTile - 1) / kAttnTile;
-    if (cluster < dealt) {      // the same for every CTA of a cluster
+    if (unit < dealt) {      // the same for every CTA of a cluster
       ranks = a.cluster;
       rank = q0 = in_cluster;
       step = a.cluster;
-      tile0 = cluster;
+      tile0 = unit;
     } else {
-      tile0 = dealt + (cluster - dealt) * a.cluster + in_cluster;
+      tile0 = dealt + (unit - dealt) * a.cluster + in_cluster;
     }
     tile1 = tile0 + 1;
   } else {
-    tile0 = blockIdx.x * a.span;
+    tile0 = unit * a.span;
     tile1 = min(tile0 + a.span, (a.q.max_len + kAttnTile - 1) / kAttnTile);
   }
   float* wout = a.wout + ((int64_t)seq * a.q.cache.heads + hk) * a.wcols;
