@@ -899,12 +899,13 @@ struct WeightCfg {
   static constexpr int kSmemBytes = kBars + 128 + 1024;
 };
 
-// Sum over one accumulator's 32 columns from `v` on: 2^(c s - lse2), pairs of columns side by side.
+// Sum over 16 columns of an accumulator: 2^(c s - lse2), pairs of columns side by side.  (With 32 at a time the registers of two
+// blocks, their columns' numbers and the sums do not fit, and the exponentials wait for shared memory.)
 template <bool MASKED>
-__device__ __forceinline__ void weight_columns(uint32_t (&v)[32], const float* nlse, const int* place, int2 iv, uint64_t c2, uint64_t (&sum)[2]) {
+__device__ __forceinline__ void weight_columns(uint32_t (&v)[16], const float* nlse, const int* place, int2 iv, uint64_t c2, uint64_t (&sum)[2]) {
   if (MASKED) {
 #pragma unroll
-    for (int e = 0; e < 32; e += 4) {
+    for (int e = 0; e < 16; e += 4) {
       const int4 w = *reinterpret_cast<const int4*>(place + e);
       if ((unsigned)(w.x - iv.x) >= (unsigned)iv.y) v[e] = 0xFF800000u;
       if ((unsigned)(w.y - iv.x) >= (unsigned)iv.y) v[e + 1] = 0xFF800000u;
@@ -913,7 +914,7 @@ __device__ __forceinline__ void weight_columns(uint32_t (&v)[32], const float* n
     }
   }
 #pragma unroll
-  for (int e = 0; e < 32; e += 4) {
+  for (int e = 0; e < 16; e += 4) {
     const float4 w = *reinterpret_cast<const float4*>(nlse + e);
     const uint64_t x = fma2(pair2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), c2, pair2(w.x, w.y));
     const uint64_t y = fma2(pair2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), c2, pair2(w.z, w.w));
@@ -1209,19 +1210,18 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
       const bool warp_in = slot - lane < s.len;
       uint64_t sum[2] = {0, 0};
       if (warp_in) {
-        uint32_t v[32], w[32];
-        ATTS_TMEM_LD_32(t_s, v);
-        for (int j = 0; j < ncols; j += 64) {   // the next 32 columns are read while these are worked on
+        uint32_t v[16], w[16];
+        ATTS_TMEM_LD_16(t_s, v);
+#pragma unroll 1
+        for (int j = 0; j < ncols; j += 32) {   // 16 columns are read while 16 are worked on
           tmem_ld_wait();
-          if (j + 32 < ncols) ATTS_TMEM_LD_32(t_s + (uint32_t)(j + 32), w);
+          ATTS_TMEM_LD_16(t_s + (uint32_t)(j + 16), w);
           if (masked) weight_columns<true>(v, nlse + j, place + j, iv, c2, sum);
           else weight_columns<false>(v, nlse + j, place + j, iv, c2, sum);
-          if (j + 32 < ncols) {
-            tmem_ld_wait();
-            if (j + 64 < ncols) ATTS_TMEM_LD_32(t_s + (uint32_t)(j + 64), v);
-            if (masked) weight_columns<true>(w, nlse + j + 32, place + j + 32, iv, c2, sum);
-            else weight_columns<false>(w, nlse + j + 32, place + j + 32, iv, c2, sum);
-          }
+          tmem_ld_wait();
+          if (j + 32 < ncols) ATTS_TMEM_LD_16(t_s + (uint32_t)(j + 32), v);
+          if (masked) weight_columns<true>(w, nlse + j + 16, place + j + 16, iv, c2, sum);
+          else weight_columns<false>(w, nlse + j + 16, place + j + 16, iv, c2, sum);
         }
       }
       tc_fence_before();
