@@ -132,10 +132,16 @@ def _ptr(t) -> int | None:
 def _stream() -> int:
     """The current stream of the current device (the raw handle where torch hands it out directly: 0.1 against 3.3 us)."""
     import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is not None:
-        return raw(torch.cuda.current_device())
-    return torch.cuda.current_stream().cuda_stream
+    global _raw_stream
+    if _raw_stream is None:
+        get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _raw_stream = (lambda: torch.cuda.current_stream().cuda_stream) if get is None else (lambda: get(device()))
+        torch.cuda.current_device()       # the first use brings the device up
+    return _raw_stream()
+
+
+_raw_stream = None
 
 
 def score_workspace_bytes(M: int, d: int, V: int, S: int) -> int:
@@ -403,21 +409,20 @@ class PagedCache:
         self._ref = ctypes.addressof(self._c)
 
 
-def _rows(t, name: str, M: int, heads, cache: PagedCache):
+def _rows(t, name: str, M: int, heads: int, cache: PagedCache):
     """(pointer, token stride, head stride) of a [M, heads, head_dim] tensor of the cache's type."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != M or (heads is not None and shape[1] != heads) or shape[2] != cache.head_dim:
-        raise ValueError(f"{name}: expected [{M}, {'heads' if heads is None else heads}, {cache.head_dim}], got {tuple(shape)}")
-    if t.dtype != cache.dtype or t.device != cache.device:
-        raise ValueError(f"{name}: has to be {cache.dtype} on {cache.device} like the cache")
-    if stride[2] != 1 and t.numel():
+    if t.shape != (M, heads, cache.head_dim) or t.dtype is not cache.dtype or t.device != cache.device:
+        raise ValueError(f"{name}: has to be [{M}, {heads}, {cache.head_dim}], {cache.dtype}, on {cache.device} like the cache; got "
+                         f"{list(t.shape)}, {t.dtype}, on {t.device}")
+    token, head, channel = t.stride()
+    if channel != 1 and t.numel():
         raise ValueError(f"{name}: head_dim has to be contiguous")
-    return t.data_ptr(), stride[0] if M > 1 else 0, stride[1] if shape[1] > 1 else 0
+    return t.data_ptr(), token if M > 1 else 0, head if heads > 1 else 0
 
 
 def _vec(t, name: str, dtype, n: int, device):
     """Pointer of a contiguous tensor of n entries."""
-    if t.dtype != dtype or t.numel() != n or t.device != device or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != n or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name}: has to be a contiguous {dtype} tensor of {n} entries on {device}")
     return t.data_ptr()
 
@@ -478,7 +483,7 @@ def rope_append(q, k, v, positions, freqs, cache: PagedCache, ctx_lens, cu_token
     M, dev, B = k.shape[0], cache.device, cache.num_seqs
     kr, vr = _rows(k, "k", M, cache.heads, cache), _rows(v, "v", M, cache.heads, cache)
     Hq = 0 if q is None else q.shape[1]
-    qr, outr = ((0, 0, 0), (0, 0, 0)) if q is None else (_rows(q, "q", M, None, cache), _rows(q_out, "q_out", M, Hq, cache))
+    qr, outr = ((0, 0, 0), (0, 0, 0)) if q is None else (_rows(q, "q", M, Hq, cache), _rows(q_out, "q_out", M, Hq, cache))
     n = freqs.numel()
     _check(load().atts_rope_append(*qr, *kr, *vr, _vec(positions, "positions", torch.int32, M, dev),
                                    _vec(freqs, "freqs", torch.float64, n, dev), n, mscale, 1 if interleaved else 0, cache._ref,

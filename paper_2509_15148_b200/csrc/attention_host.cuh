@@ -137,8 +137,7 @@ static size_t attn_workspace(const AttnShape& s, int64_t M, int32_t Hq, int32_t 
 template <typename T, int D, bool TWO>
 static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, const AttnPlan& p,
                             dim3 grid, unsigned* status, cudaStream_t stream) {
-  tree_attention_kernel<T, D, TWO><<<grid, kAttnThreads, AttnCfg<D, TWO>::kSmemBytes, stream>>>(mq, mk, mv, a, p, status);
-  int st = launch_status();
+  int st = launch_pdl(tree_attention_kernel<T, D, TWO>, grid, dim3(kAttnThreads), AttnCfg<D, TWO>::kSmemBytes, stream, mq, mk, mv, a, p, status);
   if (st != ATTS_OK || p.chunks <= 1) return st;
   const int64_t rows = (int64_t)a.max_tokens * a.Hq;
   return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
@@ -151,13 +150,15 @@ static int launch_weights(const CUtensorMap& mq, const CUtensorMap& mk, const We
   cfg.blockDim = dim3(kWeightThreads);
   cfg.dynamicSmemBytes = WeightCfg<D>::kSmemBytes;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)a.cluster;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)a.cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = a.cluster > 1 ? 1 : 0;
+  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
   if (cudaLaunchKernelEx(&cfg, cache_weights_kernel<T, D, MANY>, mq, mk, a, status) != cudaSuccess) {
     cudaGetLastError();
     return ATTS_ERR_CUDA;
@@ -267,7 +268,7 @@ int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
   const dim3 grid((unsigned)gx, (unsigned)cache->num_seqs);
   const size_t smem = sizeof(float2) * a.tpb * (size_t)rotary_pairs;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-#define ATTS_ROPE(T, I, W) rope_append_kernel<T, I, W><<<grid, kRopeThreads, smem, stream>>>(a, di->dev_status)
+#define ATTS_ROPE(T, I, W) return launch_pdl(rope_append_kernel<T, I, W>, grid, dim3(kRopeThreads), smem, stream, a, di->dev_status)
 #define ATTS_ROPE_T(T)                                                                        \
   do {                                                                                        \
     if (interleaved) { if (wide) ATTS_ROPE(T, true, true); else ATTS_ROPE(T, true, false); }  \
@@ -277,7 +278,6 @@ int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
   else ATTS_ROPE_T(__half);
 #undef ATTS_ROPE_T
 #undef ATTS_ROPE
-  return launch_status();
 }
 
 int atts_tree_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,

@@ -96,6 +96,8 @@ template <typename T, bool INTERLEAVED, bool WIDE>
 __global__ void __launch_bounds__(kRopeThreads)
 rope_append_kernel(const RopeArgs a, unsigned* __restrict__ dev_status) {
   extern __shared__ float2 rope_cs[];  // [tpb][pairs]
+  pdl_wait();
+  pdl_launch_dependents();
   const int seq = blockIdx.y;
   int first, n;
   const bool ok = seq_rows(a.cu, seq, a.M, first, n);
@@ -242,6 +244,7 @@ template <int ITEMS>
 __global__ void __launch_bounds__(kSelectThreads)
 cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
   pdl_wait();
+  pdl_launch_dependents();
   __shared__ uint32_t part[2][3][32];
   __shared__ uint32_t window[kSelectThreads];
   __shared__ uint32_t windowed;
@@ -361,6 +364,7 @@ cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
 __global__ void __launch_bounds__(kSelectThreads)
 cache_select_long_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
   pdl_wait();
+  pdl_launch_dependents();
   __shared__ uint32_t hist[256];
   __shared__ uint32_t scan[32];
   __shared__ uint32_t sh_prefix, sh_need;
@@ -442,6 +446,7 @@ cache_gather_kernel(const CacheView src, const CacheView dst, int lanes, const i
                     const int32_t* __restrict__ counts, const float* __restrict__ win, int64_t in_cols,
                     float* __restrict__ wout, unsigned* __restrict__ dev_status) {
   pdl_wait();
+  pdl_launch_dependents();
   // blocks of the same slots and other heads run side by side: a slot's heads are neighbours in memory
   const int seq = blockIdx.y, head = blockIdx.x % src.heads;
   const int per = kGatherThreads / lanes;                          // rows of a block at a time

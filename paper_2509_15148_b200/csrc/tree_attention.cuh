@@ -287,6 +287,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   const int seq = blockIdx.z, hk = blockIdx.y;
   const int qt = plan.nq - 1 - (int)(blockIdx.x % plan.nq), chunk = blockIdx.x / plan.nq;   // late rows see most: first
 
+  pdl_wait();
   // ---- what this CTA works on: nothing at all, or rows [tok0, tok0 + ntok) and slot tiles [tile0, tile1) ----
   SeqView s;
   if (!seq_view(a.cu, a.ctx, seq, a.M, a.max_tokens, a.max_len, s, dev_status, threadIdx.x == 0 && blockIdx.x == 0 && hk == 0)) return;
@@ -399,6 +400,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     f = kTileUnknown;
     return t0 + kAttnTreeTiles + (i - npre - nlist);
   };
+
+  pdl_launch_dependents();
 
   // A row's 128 scores stay in registers: 224 for the rows' warps and 56 for the others, 384 x 168 in all as launched.
   if (warp < 4) {
@@ -936,6 +939,7 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   const int hk = group % a.q.cache.heads, unit = group / a.q.cache.heads, seq = blockIdx.y;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   SeqView s;
+  pdl_wait();
   const bool ok_seq = seq_view(a.q.cu, a.q.ctx, seq, a.q.M, a.q.max_tokens, a.q.max_len, s, dev_status,
                                threadIdx.x == 0 && blockIdx.x == 0);
   const int tpt = a.tpt, nq = (s.n + tpt - 1) / tpt;
@@ -1103,6 +1107,7 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   const long long limit = a.wait_limit;
   auto wait_warp = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, limit, 0u)) != 0; };
   const bool work = count > 0;
+  pdl_launch_dependents();
   float total = 0.f;
   // another CTA's shared memory may be written once that CTA runs: awaited below
   if (ranks > 1) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
