@@ -441,11 +441,13 @@ int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kep
   st = device_info(&di);
   if (st != ATTS_OK) return st;
   if (src->num_seqs == 0 || kept_cols == 0) return ATTS_OK;
-  const int lanes = src->head_dim / 8, per = kGatherThreads / lanes * kGatherRows;
-  const int64_t gx = (kept_cols + per - 1) / per * src->heads;
+  const int lanes = src->head_dim / 8;
+  int span = kGatherSpan;
+  while (span > 32 && (kept_cols + span - 1) / span * src->heads * src->num_seqs < 2 * (int64_t)di->sm_count) span /= 2;
+  const int64_t gx = (kept_cols + span - 1) / span * src->heads;
   if (gx > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
   const dim3 grid((unsigned)gx, (unsigned)src->num_seqs);
-  return launch_pdl(cache_gather_kernel, grid, dim3(kGatherThreads), 0, static_cast<cudaStream_t>(cuda_stream), s, d, lanes, kept, kept_cols,
+  return launch_pdl(cache_gather_kernel, grid, dim3(kGatherThreads), 0, static_cast<cudaStream_t>(cuda_stream), s, d, lanes, span, kept, kept_cols,
                     counts, weights_in, in_cols, weights_out, di->dev_status);
 }
 

@@ -435,74 +435,72 @@ cache_select_long_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) 
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Eviction, move.  D / 8 threads share a kept row, 16 bytes of its key and of its value each; a thread takes kGatherRows rows
-// whose look-ups (slot, page, page) and loads are under way together: the chain of four dependent accesses, not the
-// bandwidth, is what a row by itself waits for (8 x 32,000 slots cut to 8192: 110 us with one row a thread).
+// Eviction, move.  A block takes up to kGatherSpan kept rows of one head: its threads first look up a row each (slot, then the two
+// pages), then copy, D / 8 threads to a row with 16 bytes of its key and of its value each.  The look-ups are a chain of
+// dependent accesses: done by every copying thread for its own rows they, not the bandwidth, set the time.
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kGatherThreads = 256, kGatherRows = 4;
+constexpr int kGatherThreads = 256, kGatherSpan = 256, kGatherUnroll = 4;   // (a span of 256 rows, fewer where that leaves SMs idle)
 
 __global__ void __launch_bounds__(kGatherThreads)
-cache_gather_kernel(const CacheView src, const CacheView dst, int lanes, const int32_t* __restrict__ kept, int64_t kept_cols,
+cache_gather_kernel(const CacheView src, const CacheView dst, int lanes, int span, const int32_t* __restrict__ kept, int64_t kept_cols,
                     const int32_t* __restrict__ counts, const float* __restrict__ win, int64_t in_cols,
                     float* __restrict__ wout, unsigned* __restrict__ dev_status) {
   pdl_wait();
   pdl_launch_dependents();
+  __shared__ int64_t from[kGatherSpan], to[kGatherSpan];   // byte offsets, -1: nothing to copy
   // blocks of the same slots and other heads run side by side: a slot's heads are neighbours in memory
   const int seq = blockIdx.y, head = blockIdx.x % src.heads;
-  const int per = kGatherThreads / lanes;                          // rows of a block at a time
-  const int sub = threadIdx.x / lanes, piece = threadIdx.x - sub * lanes;
-  if (sub >= per) return;
   const int64_t row = (int64_t)seq * src.heads + head;
-  const int64_t c0 = (int64_t)(blockIdx.x / src.heads) * per * kGatherRows + sub;
+  const int64_t c0 = (int64_t)(blockIdx.x / src.heads) * span;
   const int64_t live_to = min((int64_t)counts[seq], kept_cols);
-  int slot[kGatherRows], from[kGatherRows], to[kGatherRows];
-#pragma unroll
-  for (int r = 0; r < kGatherRows; ++r) {
-    const int64_t c = c0 + (int64_t)r * per;
-    slot[r] = c < live_to ? kept[row * kept_cols + c] : -1;
-    const int col = (int)(c >> dst.page_log2);
-    to[r] = c < live_to ? (col < dst.table_cols ? dst.table[seq * dst.table_stride + col] : -1) : 0;
-  }
-#pragma unroll
-  for (int r = 0; r < kGatherRows; ++r) {
-    const int col = slot[r] >> src.page_log2;
-    from[r] = slot[r] < 0 ? -1 : (col < src.table_cols ? src.table[seq * src.table_stride + col] : -1);
-  }
-  uint4 k[kGatherRows], v[kGatherRows];
-  float w[kGatherRows];
-  unsigned bad = 0;
-#pragma unroll
-  for (int r = 0; r < kGatherRows; ++r) {
-    const int64_t c = c0 + (int64_t)r * per;
-    w[r] = 0.f;
-    if (c >= live_to) {
-      from[r] = -1;
-      continue;
+  {
+    const int64_t c = c0 + threadIdx.x;
+    int64_t a = -1, b = -1;
+    float w = 0.f;
+    if (threadIdx.x < span && c < live_to) {
+      const int slot = kept[row * kept_cols + c];
+      const int to_col = (int)(c >> dst.page_log2), from_col = slot >> src.page_log2;
+      const int q = to_col < dst.table_cols ? dst.table[seq * dst.table_stride + to_col] : -1;
+      const int p = slot >= 0 && from_col < src.table_cols ? src.table[seq * src.table_stride + from_col] : -1;
+      bool ok = p >= 0 && p < src.num_pages && q >= 0 && q < dst.num_pages;
+      if (ok) {
+        a = 2 * (cache_offset(src, p, slot) + head * src.head_stride);
+        b = 2 * (cache_offset(dst, q, (int)c) + head * dst.head_stride);
+      }
+      if (wout && slot >= 0) {
+        if (slot < in_cols) w = win[row * in_cols + slot];
+        else ok = false;
+      }
+      if (!ok) atomicOr(dev_status, kDevPageRange);
     }
-    const bool ok = from[r] >= 0 && from[r] < src.num_pages && to[r] >= 0 && to[r] < dst.num_pages;
-    if (!ok) {
-      bad = kDevPageRange;
-      from[r] = -1;
-    } else {
-      const int64_t at = 2 * (cache_offset(src, from[r], slot[r]) + head * src.head_stride + 8 * piece);
-      k[r] = *reinterpret_cast<const uint4*>(src.k + at);
-      v[r] = *reinterpret_cast<const uint4*>(src.v + at);
-    }
-    if (wout && piece == 0 && slot[r] >= 0) {
-      if (slot[r] < in_cols) w[r] = win[row * in_cols + slot[r]];
-      else bad = kDevPageRange;
-    }
+    from[threadIdx.x] = a;
+    to[threadIdx.x] = b;
+    if (wout && threadIdx.x < span && c < kept_cols) wout[row * kept_cols + c] = w;
   }
+  __syncthreads();
+  const int per = kGatherThreads / lanes;                          // rows of the block at a time
+  const int sub = threadIdx.x / lanes, piece = 16 * (threadIdx.x - sub * lanes);
+  if (sub >= per) return;
+  const int rows = (int)min((int64_t)span, live_to - c0);
+  for (int r0 = sub; r0 < rows; r0 += per * kGatherUnroll) {
+    uint4 k[kGatherUnroll], v[kGatherUnroll];
 #pragma unroll
-  for (int r = 0; r < kGatherRows; ++r) {
-    const int64_t c = c0 + (int64_t)r * per;
-    if (c < kept_cols && wout && piece == 0) wout[row * kept_cols + c] = w[r];
-    if (from[r] < 0) continue;
-    const int64_t at = 2 * (cache_offset(dst, to[r], (int)c) + head * dst.head_stride + 8 * piece);
-    *reinterpret_cast<uint4*>(dst.k + at) = k[r];
-    *reinterpret_cast<uint4*>(dst.v + at) = v[r];
+    for (int u = 0; u < kGatherUnroll; ++u) {
+      const int r = r0 + u * per;
+      if (r < rows && from[r] >= 0) {
+        k[u] = *reinterpret_cast<const uint4*>(src.k + from[r] + piece);
+        v[u] = *reinterpret_cast<const uint4*>(src.v + from[r] + piece);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kGatherUnroll; ++u) {
+      const int r = r0 + u * per;
+      if (r < rows && from[r] >= 0) {
+        *reinterpret_cast<uint4*>(dst.k + to[r] + piece) = k[u];
+        *reinterpret_cast<uint4*>(dst.v + to[r] + piece) = v[u];
+      }
+    }
   }
-  if (bad) atomicOr(dev_status, bad);
 }
 
 }  // namespace atts
