@@ -96,33 +96,38 @@ static int row_tile_tokens(int G, int64_t max_tokens) {
 }
 
 // How an attention call is cut up.  Row tiles: as many whole tokens as fit 128 rows; two of them to a CTA if the longest
-// sequence has more than one.  Chunks: the number that makes the launch shortest when a slot tile takes one unit of time
-// (about 1.4 us: 64 KB per SM at the device's bandwidth), a CTA's start and end 2.5, writing and reading back its rows'
-// sums one per 64 KB, and the second launch 3.
+// sequence has more than one.  Chunks: the number that makes the launch shortest by these measured times (us): a CTA's
+// start and end 9, a slot tile 1.2 (2.0 for two row tiles), a chunk's sums one per 45 KB of them, the second launch 3.
+// One row tile and more CTAs than SMs: kRowsBrief if its 8 + 3.5 a tile, two CTAs an SM, come out below that.
 struct AttnShape {
-  bool two;
+  AttnMode mode;
   AttnPlan p;
 };
 static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens, int64_t max_len) {
   AttnShape r{};
   const int G = Hq / heads;
   r.p.tpt = row_tile_tokens(G, max_tokens);
-  r.two = max_tokens > r.p.tpt;
-  const int64_t per = r.p.tpt * (r.two ? 2 : 1);
+  r.mode = max_tokens > r.p.tpt ? kRowsTwo : kRowsOne;
+  const int64_t per = r.p.tpt * (r.mode == kRowsTwo ? 2 : 1);
   r.p.nq = (int)((max_tokens + per - 1) / per);
   const int64_t tiles = (max_len + kAttnTile - 1) / kAttnTile;
   const int64_t base = num_seqs * heads * r.p.nq;
-  const double part = (double)((max_tokens < per ? max_tokens : per) * G) * head_dim * 8 / 65536;
+  const double tile = r.mode == kRowsTwo ? 2.0 : 1.2;
+  const double part = (double)((max_tokens < per ? max_tokens : per) * G) * head_dim * 8 / (45 * 1024);
   double best = 0.0;
   int64_t best_n = 1;
   for (int64_t n = 1; n <= tiles && n <= 256 && (n == 1 || base * n <= 64 * (int64_t)sms); ++n) {
     const int64_t ct = (tiles + n - 1) / n;
     if ((tiles + ct - 1) / ct != n) continue;   // the same chunk length with fewer chunks was looked at
-    const double cost = (double)((base * n + sms - 1) / sms) * (2.5 + (double)ct + (n > 1 ? part : 0.0)) + (n > 1 ? 3.0 : 0.0);
+    const double cost = (double)((base * n + sms - 1) / sms) * (9.0 + tile * (double)ct + (n > 1 ? part : 0.0)) + (n > 1 ? 3.0 : 0.0);
     if (n == 1 || cost < best) {
       best = cost;
       best_n = n;
     }
+  }
+  if (r.mode == kRowsOne && base > sms && (double)((base + 2 * sms - 1) / (2 * sms)) * (8.0 + 3.5 * (double)tiles) < best) {
+    r.mode = kRowsBrief;
+    best_n = 1;
   }
   r.p.chunk = (int)(tiles > 0 ? (tiles + best_n - 1) / best_n : 1);
   r.p.chunks = (int)(tiles > 0 ? (tiles + r.p.chunk - 1) / r.p.chunk : 1);
@@ -134,10 +139,10 @@ static size_t attn_workspace(const AttnShape& s, int64_t M, int32_t Hq, int32_t 
   return round_up(rows * 4, 256) + round_up(rows * head_dim * 4, 256);
 }
 
-template <typename T, int D, bool TWO>
+template <typename T, int D, AttnMode MODE>
 static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, const AttnPlan& p,
                             dim3 grid, unsigned* status, cudaStream_t stream) {
-  int st = launch_pdl(tree_attention_kernel<T, D, TWO>, grid, dim3(kAttnThreads), AttnCfg<D, TWO>::kSmemBytes, stream, mq, mk, mv, a, p, status);
+  int st = launch_pdl(tree_attention_kernel<T, D, MODE>, grid, dim3(AttnCfg<D, MODE>::kThreads), AttnCfg<D, MODE>::kSmemBytes, stream, mq, mk, mv, a, p, status);
   if (st != ATTS_OK || p.chunks <= 1) return st;
   const int64_t rows = (int64_t)a.max_tokens * a.Hq;
   return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
@@ -332,11 +337,14 @@ int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
   const dim3 grid((unsigned)gx, (unsigned)cache->heads, (unsigned)cache->num_seqs);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const bool bf = cache->dtype == ATTS_BF16;
-#define ATTS_ATTEND(D, TWO)                                                                                       \
-  (bf ? launch_attention<__nv_bfloat16, D, TWO>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream)                \
-      : launch_attention<__half, D, TWO>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream))
-  if (cache->head_dim == 128) return sh.two ? ATTS_ATTEND(128, true) : ATTS_ATTEND(128, false);
-  return sh.two ? ATTS_ATTEND(64, true) : ATTS_ATTEND(64, false);
+#define ATTS_ATTEND(D, MODE)                                                                                      \
+  (bf ? launch_attention<__nv_bfloat16, D, MODE>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream)               \
+      : launch_attention<__half, D, MODE>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream))
+#define ATTS_ATTEND_D(D)                                  \
+  (sh.mode == kRowsTwo ? ATTS_ATTEND(D, kRowsTwo)         \
+                       : sh.mode == kRowsOne ? ATTS_ATTEND(D, kRowsOne) : ATTS_ATTEND(D, kRowsBrief))
+  return cache->head_dim == 128 ? ATTS_ATTEND_D(128) : ATTS_ATTEND_D(64);
+#undef ATTS_ATTEND_D
 #undef ATTS_ATTEND
 }
 

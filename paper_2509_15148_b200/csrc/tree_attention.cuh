@@ -128,7 +128,10 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 //   S = Q K^T (tcgen05, fp32 in tensor memory) -> one thread per row: running maximum, p = 2^(c s - c m), sum
 //   -> p rounded to the inputs' type, back into tensor memory over S -> O += P V (A operand from tensor memory).
 // Two streams of this alternate on the tensor pipe, so that one's products hide the other's exponentials:
-//   TWO: two row tiles against the same slots;  otherwise: one row tile, even and odd slot tiles, joined at the end.
+//   kRowsTwo: two row tiles against the same slots;  kRowsOne: one row tile, even and odd slot tiles, joined at the end.
+// Short sequences in great number take kRowsBrief instead, one stream a CTA and two CTAs an SM: what a CTA costs to start and
+// end (about 9 us) is then hidden by the other one (384 CTAs of two tiles: 41 us with kRowsOne, 30 us; 128 CTAs of up to
+// 20 tiles: 38 against 50 us, since half the shared memory leaves no room to load ahead).
 // The running maximum that p refers to only moves when a row exceeds it by 2^8: p <= 256 and sums stay exact in fp32, and
 // O is rescaled (a pass over tensor memory) in a few tiles instead of in every one.
 // The slots may be cut into chunks of `chunk` tiles over CTAs (few rows, long caches); the parts are then joined by
@@ -142,25 +145,29 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // of the tiles that need them and clears the values of slots that hold nothing (whatever lies there, 0 * NaN must not reach
 // O), 4-7 and 8-11 are the two streams' rows.
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kAttnThreads = 384;
+enum AttnMode { kRowsTwo, kRowsOne, kRowsBrief };
 constexpr int kAttnTile = 128;          // rows of a tile, slots of a tile
 constexpr int kAttnTreeTiles = 1024;    // tiles behind the cached part that are listed; further ones are all looked at
 constexpr int kMaskRing = 4;
 
-template <int D, bool TWO>
+template <int D, AttnMode MODE>
 struct AttnCfg {
+  static constexpr int kStreams = MODE == kRowsBrief ? 1 : 2;
+  static constexpr int kThreads = 128 + 128 * kStreams;
+  static constexpr int kTmem = 256 * kStreams;                       // columns: scores (over them the probabilities), then O
   static constexpr int kTileBytes = kAttnTile * D * 2;
-  static constexpr int kQBytes = (TWO ? 2 : 1) * kTileBytes;
-  static constexpr int kStages = D == 128 ? (TWO ? 4 : 5) : 8;
+  static constexpr int kQBytes = (MODE == kRowsTwo ? 2 : 1) * kTileBytes;
+  static constexpr int kStages = D == 128 ? (MODE == kRowsTwo ? 4 : MODE == kRowsOne ? 5 : 2) : MODE == kRowsBrief ? 4 : 8;
   static constexpr int kRing = kQBytes;                              // byte offsets in (aligned) shared memory
   static constexpr int kMask = kRing + kStages * kTileBytes;         // [kMaskRing][128] int2
   static constexpr int kList = kMask + kMaskRing * kAttnTile * 8;    // [kAttnTreeTiles] uint32
   static constexpr int kStats = kList + kAttnTreeTiles * 4;          // [128] float2: maximum and sum of the odd stream
   static constexpr int kBars = kStats + kAttnTile * 8;
   static constexpr int kSmemBytes = kBars + 512 + 1024;
-  static constexpr int kLead = TWO ? 1 : 2;                          // key tiles loaded ahead of the first value tile
+  static constexpr int kLead = MODE == kRowsOne ? 2 : 1;             // key tiles loaded ahead of the first value tile
   static_assert(kSmemBytes <= 232448, "shared memory of one SM");
-  static_assert(kStages * kTileBytes >= kAttnTile * (D + 4) * 4, "the odd stream's sums are joined through the ring");
+  static_assert(MODE != kRowsBrief || 2 * (kSmemBytes + 1024) <= 233472, "two CTAs share an SM");
+  static_assert(MODE != kRowsOne || kStages * kTileBytes >= kAttnTile * (D + 4) * 4, "the odd stream's sums are joined through the ring");
 };
 
 // A tile's flags: two bits for each group of 32 slots (0 nobody sees any, 1 pairs differ, 2 everybody sees all), then
@@ -275,12 +282,15 @@ __device__ __forceinline__ void rescale_o(uint32_t taddr, float f) {
   tmem_st_wait();
 }
 
-template <typename T, int D, bool TWO>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+template <typename T, int D, AttnMode MODE>
+__global__ void __launch_bounds__(AttnCfg<D, MODE>::kThreads, MODE == kRowsBrief ? 2 : 1)
 tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a,
                       const __grid_constant__ AttnPlan plan, unsigned* __restrict__ dev_status) {
-  using Cfg = AttnCfg<D, TWO>;
+  using Cfg = AttnCfg<D, MODE>;
+  constexpr bool TWO = MODE != kRowsOne;                // a stream's rows are its own, and it takes every tile
+  constexpr int kStreams = Cfg::kStreams;
+  constexpr uint32_t kO = 128u * kStreams;              // first column of O
   constexpr int kStages = Cfg::kStages;
   constexpr int kLead = Cfg::kLead;
   extern __shared__ uint8_t smem_raw[];
@@ -291,14 +301,14 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   // ---- what this CTA works on: nothing at all, or rows [tok0, tok0 + ntok) and slot tiles [tile0, tile1) ----
   SeqView s;
   if (!seq_view(a.cu, a.ctx, seq, a.M, a.max_tokens, a.max_len, s, dev_status, threadIdx.x == 0 && blockIdx.x == 0 && hk == 0)) return;
-  const int per = plan.tpt * (TWO ? 2 : 1);
+  const int per = plan.tpt * (MODE == kRowsTwo ? 2 : 1);
   const int tok0 = qt * per;
   if (tok0 >= s.n) return;
   const int ntok = min(per, s.n - tok0);
   const int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
   const int tile0 = chunk * plan.chunk, tile1 = min(ntiles, tile0 + plan.chunk);
   if (chunk > 0 && tile0 >= ntiles) return;
-  const bool two = TWO && ntok > plan.tpt;
+  const bool two = MODE == kRowsTwo && ntok > plan.tpt;
   const int tree0 = min(s.ctx / kAttnTile, ntiles);   // first tile that is not all cached slots
 
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -334,7 +344,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     mbar_init(q_bar, 1);
     mbar_init(clean_bar, 1);
     mbar_init(join_bar, 4);
-    mbar_init(flag_bar, 8);
+    mbar_init(flag_bar, 4 * kStreams);
     mbar_init(list_bar, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_bar(i), 1);
@@ -343,13 +353,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     }
     for (int i = 0; i < kMaskRing; ++i) {
       mbar_init(m_full(i), 1);
-      mbar_init(m_empty(i), TWO && two ? 8 : 4);   // the warps that read it
+      mbar_init(m_empty(i), two ? 8 : 4);   // the warps that read it
     }
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"((uint32_t)kTmemCols) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"((uint32_t)Cfg::kTmem) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (warp == 2) {
@@ -403,7 +413,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 
   pdl_launch_dependents();
 
-  // A row's 128 scores stay in registers: 224 for the rows' warps and 56 for the others, 384 x 168 in all as launched.
+  // A row's 128 scores stay in registers: 224 (200) for the rows' warps and 56 for the others, 384 x 168 (256 x 128) in all as
+  // launched.
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0 || warp == 2) {
@@ -510,7 +521,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             if (elect_one()) {
 #pragma unroll
               for (int k = 0; k < kAttnTile / kUmmaK; ++k)
-                umma_ts(tm + 256u + u * D, tm + u * kAttnTile, db, 8u * k, (uint32_t)(k * (kUmmaK * 128 / 16)), kIdescO, k == 0 ? more_o : 1u);
+                umma_ts(tm + kO + u * D, tm + u * kAttnTile, db, 8u * k, (uint32_t)(k * (kUmmaK * 128 / 16)), kIdescO, k == 0 ? more_o : 1u);
               umma_commit(o_bar(0) + 8u * u);
               if (w + 1 == streams) umma_commit(empty_bar(0) + 8u * ring);
             }
@@ -600,10 +611,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     }
   } else {
     // ---------------- rows ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    if (MODE == kRowsBrief) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     {
       const int qmin = range[0], qmax = range[1];    // all rows padding: qmax is -1 and no tile is visible
-      for (int t = t0 + warp - 4; t < t_far; t += 8) {
+      for (int t = t0 + warp - 4; t < t_far; t += 4 * kStreams) {
         const uint32_t f = qmax < 0 ? 0u : tile_flags(a, s, t, qmin, qmax, lane);
         if (lane == 0) list[t - t0] = f;
       }
@@ -614,7 +626,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     const int quarter = warp & 3;
     const int row = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-    const uint32_t t_s = tmem_base + lane_base + (uint32_t)st * kAttnTile, t_o = tmem_base + lane_base + 256u + (uint32_t)st * D;
+    const uint32_t t_s = tmem_base + lane_base + (uint32_t)st * kAttnTile, t_o = tmem_base + lane_base + kO + (uint32_t)st * D;
     const int tok = (TWO ? st * plan.tpt : 0) + row / a.G;           // within the CTA's tokens
     const bool in = row < plan.tpt * a.G && tok < ntok;
     const bool warp_in = __any_sync(0xFFFFFFFFu, in);
@@ -815,7 +827,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   }
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)kTmemCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)Cfg::kTmem) : "memory");
   }
 }
 
@@ -1284,9 +1296,11 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 // Opt-in shared memory of the kernels above (once per device).
 template <typename T, int D>
 static cudaError_t attention_attributes_of() {
-  cudaError_t e = cudaFuncSetAttribute(tree_attention_kernel<T, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, true>::kSmemBytes);
+  cudaError_t e = cudaFuncSetAttribute(tree_attention_kernel<T, D, kRowsTwo>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, kRowsTwo>::kSmemBytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(tree_attention_kernel<T, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, false>::kSmemBytes);
+    e = cudaFuncSetAttribute(tree_attention_kernel<T, D, kRowsOne>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, kRowsOne>::kSmemBytes);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(tree_attention_kernel<T, D, kRowsBrief>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, kRowsBrief>::kSmemBytes);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(cache_weights_kernel<T, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightCfg<D>::kSmemBytes);
   if (e == cudaSuccess)
