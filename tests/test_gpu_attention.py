@@ -241,11 +241,13 @@ def test_maximum_that_grows_along_the_cache():
     b.check(out, lse, want_out, want_lse)
 
 
-def test_many_sequences_and_empty_ones():
+@pytest.mark.parametrize("Hq,Hk,D,dtype,most", [(8, 2, 64, BF, 4), (16, 8, 128, BF, 2), (24, 4, 128, FP, 17), (7, 1, 64, FP, 40)])
+def test_many_sequences_and_empty_ones(Hq, Hk, D, dtype, most):
+    """More (sequence, head) pairs than SMs, each short, some without drafts."""
     rs = np.random.RandomState(11)
-    tokens = rs.randint(0, 4, 300)
+    tokens = rs.randint(0, most, 300)
     ctx = rs.randint(0, 200, 300)
-    b = Batch(11, tokens, ctx, 8, 2, 64, 16, BF)
+    b = Batch(11, tokens, ctx, Hq, Hk, D, 16, dtype, pad=0.1)
     out, lse = b.attend()
     want_out, want_lse, want_w = b.dense()
     b.check(out, lse, want_out, want_lse)
@@ -335,6 +337,61 @@ def test_lengths_that_do_not_fit_are_recorded():
     b.ml = 90                                       # cut
     b.attend()
     assert binding.last_device_status() & binding.DEV_SEQ_RANGE
+
+
+@pytest.mark.parametrize("tokens,ctx,Hq,Hk", [([2], [300], 8, 2), ([200], [300], 16, 2), ([1] * 80, [20] * 80, 8, 4)])
+def test_waits_that_run_out_are_reported(tokens, ctx, Hq, Hk):
+    """The kernels' loads are withheld by the library's diagnostic switch: the first wait for data gives up, the condition is
+    reported and cleared, and the next call is correct (nothing is in flight when a kernel gives up)."""
+    b = Batch(17, tokens, ctx, Hq, Hk, 128, 16, BF)
+    want_out, want_lse, want_w = b.dense()
+    assert binding.last_device_status() == 0
+    for call in (lambda: b.attend(), lambda: b.weights(want_lse.float())):
+        try:
+            binding.debug_set_wait(2_000_000, withhold_loads=True)
+            call()
+            with pytest.raises(binding.AttsError) as err:
+                binding.last_device_status()
+            assert err.value.status == 9
+        finally:
+            binding.debug_set_wait(0, withhold_loads=False)
+        assert binding.last_device_status() == 0
+        b.check(*b.attend(), want_out, want_lse)
+        b.check_weights(b.weights(want_lse.float()), want_w)
+        assert binding.last_device_status() == 0
+
+
+@pytest.mark.parametrize("sinks", [0.0, 1.0])
+def test_keys_that_stand_out(sinks):
+    """A few cached slots far above the rest, late in the cache: the running maximum jumps once, sums before it vanish."""
+    b = Batch(18, [5, 60], [700, 1500], 8, 2, 128, 32, FP)
+    for s, c in enumerate(b.ctx_h):
+        slot = int(c) - 3
+        b.k[b.table_h[s, slot // 32], slot % 32] = b.q[int(b.cu_h[s]), ::4] * 2.0 * sinks + 1.0
+    out, lse = b.attend()
+    want_out, want_lse, want_w = b.dense()
+    b.check(out, lse, want_out, want_lse)
+    b.check_weights(b.weights(want_lse.float()), want_w)
+
+
+def test_weights_of_a_tree_with_more_row_tiles_than_are_listed():
+    """One head a group and thousands of drafts: more products than a CTA lists ahead."""
+    n = 1024 * 3 + 50
+    b = Batch(19, [n], [10], 126, 1, 64, 128, BF, tree="fan")        # a token a row tile
+    out, lse = b.attend()
+    want = b.weights(lse)
+    assert want.sum().item() == pytest.approx(n * 126, rel=1e-4)
+    pick = [0, 5, 9, 10, 11, 500, n // 2, n + 9]
+    par = b.parent
+    for slot in pick:
+        seen = torch.zeros(n, dtype=torch.bool)
+        each = -(-n // 4)
+        i = torch.arange(n)
+        seen = torch.ones(n, dtype=torch.bool) if slot < 10 else (i >= slot - 10) & (i // each == (slot - 10) // each)
+        k = b.k[b.table_h[0, slot // 128], slot % 128, 0].double()
+        s = b.q.double() @ k * b.scale
+        w = torch.exp(s - lse.double())[seen.cuda()].sum().item()
+        assert want[0, 0, slot].item() == pytest.approx(w, rel=1e-4)
 
 
 def test_on_another_stream_and_in_a_graph():
@@ -567,3 +624,69 @@ def test_evicted_cache_attends_like_the_kept_slots():
             want = b.k[b.table[s].long()[i // 16], i % 16, h]
             got = ko[small.block_table[s].long()[torch.arange(budget, device="cuda") // 16], torch.arange(budget, device="cuda") % 16, h]
             assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("tree", ["chain", "fan"])
+def test_more_drafted_tiles_than_are_listed(tree):
+    """Over 131,072 drafted tokens: tiles behind the listed ones are all looked at."""
+    n, ctx = 131072 + 900, 5
+    b = Batch(20, [n], [ctx], 1, 1, 64, 128, BF, tree=tree)
+    out, lse = b.attend()
+    k, v = (x[b.table[0].long(), :, 0].flatten(0, 1)[:n + ctx].double() for x in (b.k, b.v))
+    each = -(-n // 4) if tree == "fan" else n
+    for t in (0, 77, each - 1, n // 2, n - 1):
+        first = t // each * each
+        seen = torch.cat([torch.arange(ctx), torch.arange(ctx + first, ctx + t + 1)]).cuda()
+        s = (b.q[t, 0].double() @ k[seen].T) * b.scale
+        want_lse = torch.logsumexp(s, 0)
+        want = torch.softmax(s, 0) @ v[seen]
+        b.check(out[t:t + 1], lse[t:t + 1], want.view(1, 1, -1), want_lse.view(1, 1))
+
+
+def test_verification_step_example():
+    """examples/verify_step.py end to end against the fp64 definitions of its parts."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "verify_step.py")
+    spec = importlib.util.spec_from_file_location("verify_step", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    from oracle import atts_oracle
+
+    torch.manual_seed(3)
+    target = ex.Target(hidden=256, heads=4, kv_heads=2, head_dim=64, vocab=1000, seed=3)
+    samples, slots = 3, 96
+    cache = target.new_cache(samples, slots)
+    lens = i32([20, 0, 7])
+    for b in range(samples):
+        for s in range(int(lens[b])):
+            p = int(cache.block_table[b, s // 16])
+            cache.k[p, s % 16], cache.v[p, s % 16] = (torch.randn(2, 64, device="cuda").to(BF) for _ in range(2))
+    parent, cu = [-1, 0, 1, 1, 0, 4, -1, 0, -1, -1], [0, 6, 8, 10]
+    x = torch.randn(10, 256, device="cuda").bfloat16()
+    ids = torch.randint(0, 1000, (10,), dtype=torch.int32, device="cuda")
+    calib = torch.sort(torch.rand(64, device="cuda") + 6.5)[0]
+    weights = torch.zeros(samples, 2, slots, device="cuda")
+    at = torch.tensor([33, 0, 7])
+    r = ex.verify_step(target, cache, lens, at, x, parent, ids, cu, calib, 64, 0.25, weights)
+    assert binding.last_device_status() == 0
+    assert r["positions"].tolist() == [33, 34, 35, 35, 34, 35, 0, 1, 7, 7]
+    # the projection as the library product leaves it, then everything in fp64
+    qkv = (x @ target.w_qkv.T).double().cpu().numpy()
+    q, f = qkv[:, :256].reshape(10, 4, 64), target.freqs.cpu().numpy()
+    rot = np.stack([orc.rotate(q[i], int(r["positions"][i]), f) for i in range(10)])
+    host_k, host_v = (c.double().cpu().numpy() for c in (cache.k, cache.v))
+    out, lse = orc.tree_attention(rot, host_k, host_v, cache.block_table.cpu().numpy(), [20, 0, 7], cu, np.array(parent), target.scale)
+    hidden = x.double().cpu().numpy() + out.reshape(10, -1) @ target.w_out.double().cpu().numpy().T
+    # bf16 roundings on the way: rotated queries, probabilities, attention, its projection and the sum, each 2^-8 of its size
+    got = r["hidden"].double().cpu().numpy()
+    assert np.abs(got - hidden).max() <= 2.0 ** -8 * (4 * np.abs(out).max() * 2 + np.abs(hidden).max())
+    lm = target.lm_head.view(torch.int16).cpu().numpy().view(np.uint16)
+    want_lp = atts_oracle.token_logprob(r["hidden"].view(torch.int16).cpu().numpy().view(np.uint16), lm, ids.cpu().numpy())
+    assert np.abs(r["logprob"].double().cpu().numpy() - want_lp).max() <= 2e-3
+    # each of a row's weights add up to one over what it sees: 10 tokens, 4 heads
+    assert weights.sum().item() == pytest.approx(40, rel=1e-3)
+    smaller, counts, left = ex.evict(target, cache, i32([26, 2, 9]), weights, 12, 2, 3, 32)
+    assert counts.tolist() == [12, 2, 9] and left.shape == weights.shape
+    assert left[0].sum() <= weights[0].sum() and torch.equal(left[1, :, :2], weights[1, :, :2])
+    ex.main()
