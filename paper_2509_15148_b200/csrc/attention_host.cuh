@@ -6,7 +6,7 @@
 
 namespace atts {
 
-constexpr int64_t kMaxSlots = 1ll << 30;  // slots of one sequence, columns of a weight row
+constexpr int64_t kMaxSlots = kMaxSlotsOfSeq;  // slots of one sequence, columns of a weight row
 
 static inline bool finite_pos(float x) { return x > 0.f && x <= 3.402823466e38f; }
 
@@ -377,9 +377,10 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
   a.tpt = row_tile_tokens(G, max_tokens);
   a.wait_limit = wait_limit();
   a.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
-  // One row tile: a CTA goes over as many slot tiles as leave two CTAs an SM something to do, eight at most (measured on 8 x
-  // 2000 slots of 8 heads: spans 1, 2, 4, 8 take @SPANS@).  More: slot tiles are dealt to clusters whose CTAs take at
-  // least two row tiles each.
+  // One row tile: a CTA goes over as many slot tiles as leave two CTAs an SM something to do, eight at most (8 sequences of
+  // 2000 slots, 8 heads: spans of 1, 2, 4 and 8 tiles take 30.7, 20.5, 18.2 and 22.5 us).  More: cached tiles are dealt to
+  // clusters whose CTAs take at least two row tiles each, of at most four (8 drafts of 500: clusters of 1, 2, 4, 8 take
+  // 311, 171, 155 and 168 us).
   const int64_t nq = (max_tokens + a.tpt - 1) / a.tpt, tiles = (max_len + kAttnTile - 1) / kAttnTile;
   const bool many = nq > 1;
   a.cluster = 1;

@@ -10,6 +10,7 @@
 
 namespace atts {
 
+constexpr int kMaxSlotsOfSeq = 1 << 30;
 constexpr unsigned kDevPageRange = 16u, kDevSeqRange = 32u;  // ATTS_DEV_PAGE_RANGE, ATTS_DEV_SEQ_RANGE
 
 // A paged cache as the kernels see it (atts_kv_cache with the page size as a shift).
@@ -26,7 +27,7 @@ struct CacheView {
 __device__ __forceinline__ int cache_page(const CacheView& c, int seq, int slot, unsigned* dev_status) {
   const int col = slot >> c.page_log2;
   int page = -1;
-  if (col < c.table_cols) page = c.table[(int64_t)seq * c.table_stride + col];
+  if (slot >= 0 && col < c.table_cols) page = c.table[(int64_t)seq * c.table_stride + col];
   if (page < 0 || page >= c.num_pages) {
     atomicOr(dev_status, kDevPageRange);
     page = -1;
@@ -102,7 +103,7 @@ rope_append_kernel(const RopeArgs a, unsigned* __restrict__ dev_status) {
   int first, n;
   const bool ok = seq_rows(a.cu, seq, a.M, first, n);
   const int ctx = a.ctx[seq];
-  if (!ok || ctx < 0 || n > a.max_tokens) {
+  if (!ok || ctx < 0 || ctx > kMaxSlotsOfSeq || n > a.max_tokens) {
     if (threadIdx.x == 0 && blockIdx.x == 0) atomicOr(dev_status, kDevSeqRange);
     return;
   }

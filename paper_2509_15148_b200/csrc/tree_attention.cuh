@@ -27,7 +27,7 @@ __device__ __forceinline__ bool seq_view(const int32_t* cu, const int32_t* ctx, 
                                          SeqView& s, unsigned* dev_status, bool record) {
   bool ok = seq_rows(cu, seq, M, s.first, s.n);
   s.ctx = ctx[seq];
-  ok = ok && s.ctx >= 0 && s.n <= max_tokens;
+  ok = ok && s.ctx >= 0 && s.ctx <= kMaxSlotsOfSeq && s.n <= max_tokens;   // (both at most 2^30: their sum fits)
   s.len = ok ? s.ctx + s.n : 0;
   if (record && (!ok || s.len > max_len)) atomicOr(dev_status, kDevSeqRange);
   s.len = min(s.len, max_len);
@@ -132,7 +132,7 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // Short sequences in great number take kRowsBrief instead, one stream a CTA and two CTAs an SM: what a CTA costs to start and
 // end (about 9 us) is then hidden by the other one (384 CTAs of two tiles: 41 us with kRowsOne, 30 us; 128 CTAs of up to
 // 20 tiles: 38 against 50 us, since half the shared memory leaves no room to load ahead).
-// The running maximum that p refers to only moves when a row exceeds it by 2^8: p <= 256 and sums stay exact in fp32, and
+// The running maximum that p refers to only moves when a row exceeds it by 2^8: p <= 256, and
 // O is rescaled (a pass over tensor memory) in a few tiles instead of in every one.
 // The slots may be cut into chunks of `chunk` tiles over CTAs (few rows, long caches); the parts are then joined by
 // attention_join_kernel.

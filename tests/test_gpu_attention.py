@@ -322,9 +322,13 @@ def test_lengths_that_do_not_fit_are_recorded():
     assert binding.last_device_status() & binding.DEV_SEQ_RANGE
     assert torch.equal(out[4:], good[0][4:])
     b.mt = 4
-    for bad in ([-1, 20], [100, -5]):
+    for bad in ([-1, 20], [100, -5], [2 ** 31 - 1, 20], [100, 2 ** 31 - 2], [(1 << 30) + 1, 20]):
         b.ctx = i32(bad)
         b.attend()
+        assert binding.last_device_status() & binding.DEV_SEQ_RANGE
+        rows = b.q[:, :2].contiguous()
+        binding.rope_append(None, rows, rows, i32([0] * b.M), torch.zeros(1, dtype=torch.float64, device="cuda"),
+                            binding.PagedCache(b.k.clone(), b.v.clone(), b.table), b.ctx, b.cu, 4, None)
         assert binding.last_device_status() & binding.DEV_SEQ_RANGE
         b.weights(good[1])
         assert binding.last_device_status() & binding.DEV_SEQ_RANGE
