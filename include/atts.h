@@ -49,7 +49,7 @@ typedef enum {
 
 /* Bits of the device status word returned by atts_last_device_status. */
 #define ATTS_DEV_TOKEN_ID_RANGE 1u /* a token id was outside [0, V): that row's log-prob is NaN */
-#define ATTS_DEV_WAIT_EXPIRED 2u   /* a pipeline wait in the scoring kernel ran out; outputs invalid */
+#define ATTS_DEV_WAIT_EXPIRED 2u   /* a pipeline wait in a scoring or attention kernel ran out; outputs invalid */
 #define ATTS_DEV_GROUP_ID_RANGE 4u /* a group id was outside [0, G): that candidate has numer 0 */
 #define ATTS_DEV_INDEX_STALE 8u    /* an indexed call was given an index that does not describe fill n; nothing written */
 #define ATTS_DEV_PAGE_RANGE 16u    /* a block-table entry that a sequence needs is missing or outside [0, num_pages) */
@@ -519,8 +519,8 @@ int atts_debug_score_unit(int64_t M, int64_t d, int64_t V, int32_t workers, int3
                           int32_t* out);
 
 /*
- * Bounded waits of the scoring kernel (diagnostic; the paper has no counterpart).  Every wait inside
- * atts_score_logprob's fused kernel (for a shared-memory stage to fill or drain, for an accumulator to complete or be
+ * Bounded waits (diagnostic; the paper has no counterpart).  Every wait inside the kernels of atts_score_logprob,
+ * atts_tree_attention and atts_cache_weights (for a shared-memory stage to fill or drain, for an accumulator to complete or be
  * read) gives up after a number of SM cycles; the kernel then stops, lets copies in flight land, frees its tensor
  * memory and returns, ATTS_DEV_WAIT_EXPIRED is recorded and atts_last_device_status returns ATTS_ERR_TIMEOUT.  The
  * outputs of such a call are invalid; the context stays usable.

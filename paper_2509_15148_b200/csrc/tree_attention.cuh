@@ -132,6 +132,9 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // Short sequences in great number take kRowsBrief instead, one stream a CTA and two CTAs an SM: what a CTA costs to start and
 // end (about 9 us) is then hidden by the other one (384 CTAs of two tiles: 41 us with kRowsOne, 30 us; 128 CTAs of up to
 // 20 tiles: 38 against 50 us, since half the shared memory leaves no room to load ahead).
+// Bound: few rows over a long cache (4 x 13 tokens, 32 / 8 heads of 128, 131,071 slots) 335 us = 5.0 TB/s; many rows (chunk of 2048
+// over 6144, 64 / 8 heads) 881 us = 961 TFLOP/s, where a stream's chain of scores, exponentials (1,400 of a round's 3,750 cycles) and
+// products keeps the tensor pipe 55 % busy and the power cap sets the clock.
 // The running maximum that p refers to only moves when a row exceeds it by 2^8: p <= 256, and
 // O is rescaled (a pass over tensor memory) in a few tiles instead of in every one.
 // The slots may be cut into chunks of `chunk` tiles over CTAs (few rows, long caches); the parts are then joined by
@@ -890,7 +893,8 @@ struct WeightArgs {
 //   S^T = K Q^T (tcgen05, fp32 in tensor memory), a thread per slot, and each thread adds 2^(c s - lse2) over the columns
 // of its own row: no sum crosses threads, so the order is fixed and nothing is stored but one number per slot.  Products
 // alternate between two groups of four warps with an accumulator each, and two CTAs share an SM: the exponentials (one per
-// pair, 16 a clock and SM) are what the time goes to.
+// pair, 16 a clock and SM) are what the time goes to (8 drafts of 500 over 1013 slots, 40 / 8 heads: 130 us for 2.3e8 of them, 0.41
+// of that rate; 8 sequences of one token over 2000 slots: 8 us of kernel for 29 MB).
 //
 // One operand stays, the other streams.  MANY = false (one row tile covers every sequence's drafts): the queries stay and a CTA
 // goes over `span` slot tiles.  MANY = true: a slot tile stays and the row tiles stream.  Every row sees the cached slots,
