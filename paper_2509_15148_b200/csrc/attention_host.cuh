@@ -148,27 +148,34 @@ static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const 
   return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
 }
 
-template <typename T, int D, bool MANY>
-static int launch_weights(const CUtensorMap& mq, const CUtensorMap& mk, const WeightArgs& a, dim3 grid, unsigned* status, cudaStream_t stream) {
+// launch_pdl with `cluster` blocks to a cluster; the grid counts clusters.
+template <typename... KArgs, typename... Args>
+static int launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t stream, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(kWeightThreads);
-  cfg.dynamicSmemBytes = WeightCfg<D>::kSmemBytes;
+  cfg.gridDim = dim3(grid.x * (unsigned)cluster, grid.y, grid.z);
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)a.cluster;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-  if (cudaLaunchKernelEx(&cfg, cache_weights_kernel<T, D, MANY>, mq, mk, a, status) != cudaSuccess) {
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) != cudaSuccess) {
     cudaGetLastError();
     return ATTS_ERR_CUDA;
   }
   return ATTS_OK;
+}
+
+template <typename T, int D, bool MANY>
+static int launch_weights(const CUtensorMap& mq, const CUtensorMap& mk, const WeightArgs& a, dim3 clusters, unsigned* status, cudaStream_t stream) {
+  return launch_pdl_cluster(cache_weights_kernel<T, D, MANY>, clusters, dim3(kWeightThreads), WeightCfg<D>::kSmemBytes, a.cluster, stream, mq, mk, a,
+                            status);
 }
 
 }  // namespace atts
@@ -390,8 +397,8 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
   } else {
     while (a.span < 8 && tiles * cache->heads * cache->num_seqs > 2 * a.span * (int64_t)di->sm_count) a.span *= 2;
   }
-  const int64_t gx = (many ? tiles * a.cluster : (tiles + a.span - 1) / a.span) * cache->heads;
-  if (gx > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  const int64_t gx = (many ? tiles : (tiles + a.span - 1) / a.span) * cache->heads;   // clusters
+  if (gx * a.cluster > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
   const dim3 grid((unsigned)gx, (unsigned)cache->num_seqs);
   CUtensorMap mq, mk;
   // without queries (M == 0) the kernel only writes; the map then describes the cache's keys and is not used
@@ -423,14 +430,15 @@ int atts_cache_select(const float* weights, int64_t weights_cols, const int32_t*
   const SelectArgs a{weights, weights_cols, lens, heads, (int)budget, (int)sinks, (int)recent, kept, counts};
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const dim3 grid((unsigned)(num_seqs * heads));
-  // the smallest number of keys a thread (of 1024, or of fewer for the shortest rows) that covers a row
-  if (weights_cols > kSelectMaxItems * kSelectThreads)
+  // one block with the smallest number of keys a thread (of 1024, or of fewer for the shortest rows) that covers a row, then
+  // clusters, then the form that reads the row again for every digit
+  if (weights_cols > kSelectCluster * kSelectMaxItems * kSelectThreads)
     return launch_pdl(cache_select_long_kernel, grid, dim3(kSelectThreads), 0, stream, a, di->dev_status);
   const unsigned threads = weights_cols >= kSelectThreads ? kSelectThreads : (unsigned)round_up((size_t)(weights_cols < 1 ? 1 : weights_cols), 32);
-  if (weights_cols <= 1024) return launch_pdl(cache_select_kernel<1>, grid, dim3(threads), 0, stream, a, di->dev_status);
-  if (weights_cols <= 4096) return launch_pdl(cache_select_kernel<4>, grid, dim3(threads), 0, stream, a, di->dev_status);
-  if (weights_cols <= 12288) return launch_pdl(cache_select_kernel<12>, grid, dim3(threads), 0, stream, a, di->dev_status);
-  return launch_pdl(cache_select_kernel<kSelectMaxItems>, grid, dim3(threads), 0, stream, a, di->dev_status);
+  if (weights_cols <= 1024) return launch_pdl(cache_select_kernel<1, 1>, grid, dim3(threads), 0, stream, a, di->dev_status);
+  if (weights_cols <= 4096) return launch_pdl(cache_select_kernel<4, 1>, grid, dim3(threads), 0, stream, a, di->dev_status);
+  if (weights_cols <= 16384) return launch_pdl_cluster(cache_select_kernel<8, kSelectCluster>, grid, dim3(threads), 0, kSelectCluster, stream, a, di->dev_status);
+  return launch_pdl_cluster(cache_select_kernel<kSelectMaxItems, kSelectCluster>, grid, dim3(threads), 0, kSelectCluster, stream, a, di->dev_status);
 }
 
 int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kept_cols, const int32_t* counts,

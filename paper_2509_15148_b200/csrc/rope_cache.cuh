@@ -205,13 +205,15 @@ rope_append_kernel(const RopeArgs a, unsigned* __restrict__ dev_status) {
 // set if at least `budget` keys are not below T with it.  Kept are the keys above T and, from the lowest slot on, as many
 // of those equal to T as there is room for.  As soon as a count is the budget itself the set is known.
 //
-// Rows of up to 32,768 slots: one block, its keys in registers (a warp owns consecutive slots, so one scan over the warps
-// places everything).  A pass over all keys costs a comparison and an addition each and one barrier; once no more keys than
-// threads lie between the bounds of T, those go to shared memory and the remaining bits are found among them, two a
-// pass.  (A histogram of digits needs fewer passes over the keys, but weights share a few exponents and its atomics then
-// meet in a few bins: 87 us for 64 rows of 32,000 slots, 47 us with all passes over all keys.)
+// Rows of up to 32,768 slots: keys in registers, of one block or, from 4,097 slots on, of a cluster of two (a warp owns
+// consecutive slots, so one scan over the warps places everything).  A pass over all keys costs a comparison and an addition
+// each, and one barrier behind which every block has every warp's count, written through the cluster's shared memory; once
+// no more keys than threads lie between the bounds of T, a block's share of them goes to its shared memory and the
+// remaining bits are found among them, two a pass.  64 rows of 32,000 slots: 27 us (clusters of four: 35, two waves of them).
+// (A histogram of digits needs fewer passes over the keys, but weights share a few exponents and its atomics then meet in a few
+// bins: 87 us; one block a row 43 us.)
 constexpr int kSelectThreads = 1024;
-constexpr int kSelectMaxItems = 32;     // keys of a thread: rows of up to 32 * 1024 slots
+constexpr int kSelectCluster = 2, kSelectMaxItems = 16;     // keys of a thread: rows of up to 2 * 16 * 1024 slots
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t u = __float_as_uint(w);
@@ -228,34 +230,55 @@ struct SelectArgs {
   int32_t *kept, *counts;
 };
 
-// Length of the block's row, the counts' entry, and rows that keep everything; false: nothing is left to do.
-__device__ __forceinline__ bool select_row(const SelectArgs& a, int& len, unsigned* dev_status) {
-  const int seq = blockIdx.x / a.heads;
+// Length of a row, the counts' entry, and rows that keep everything; false: nothing is left to do.
+__device__ __forceinline__ bool select_row(const SelectArgs& a, int row, bool first, int& len, unsigned* dev_status) {
+  const int seq = row / a.heads;
   const int len0 = a.lens[seq];
   len = (int)max((int64_t)0, min((int64_t)len0, a.cols));
-  if (threadIdx.x == 0 && blockIdx.x == seq * a.heads) {
+  if (first && threadIdx.x == 0 && row == seq * a.heads) {
     if (len != len0) atomicOr(dev_status, kDevSeqRange);
     a.counts[seq] = min(len, a.budget);
   }
   if (len > a.budget) return true;
-  int32_t* out = a.kept + (int64_t)blockIdx.x * a.budget;
-  for (int i = threadIdx.x; i < a.budget; i += blockDim.x) out[i] = i < len ? i : -1;
+  int32_t* out = a.kept + (int64_t)row * a.budget;
+  if (first)
+    for (int i = threadIdx.x; i < a.budget; i += blockDim.x) out[i] = i < len ? i : -1;
   return false;
 }
 
-template <int ITEMS>
+// ITEMS keys a thread, CL blocks a row.
+template <int ITEMS, int CL>
 __global__ void __launch_bounds__(kSelectThreads)
 cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
   pdl_wait();
   pdl_launch_dependents();
-  __shared__ uint32_t part[2][3][32];
+  __shared__ uint32_t part[2][3][CL * 32];     // counts of every warp of the cluster
   __shared__ uint32_t window[kSelectThreads];
   __shared__ uint32_t windowed;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const int row = blockIdx.x / CL, rank = blockIdx.x % CL;
   int len;
-  if (!select_row(a, len, dev_status)) return;
-  const float* w = a.weights + (int64_t)blockIdx.x * a.cols;
-  const int first = warp * 32 * ITEMS + lane;             // this thread's slots: first + 32 k
+  if (!select_row(a, row, rank == 0, len, dev_status)) return;   // the same for a whole cluster
+  const float* w = a.weights + (int64_t)row * a.cols;
+  const int mine_at = rank * 32 + warp;                   // this warp among the cluster's
+  const int first = mine_at * 32 * ITEMS + lane;          // this thread's slots: first + 32 k
+  // Writes a warp's count where every block of the cluster reads it; barrier() makes them visible.  The other buffer is
+  // written next: nobody can be a whole pass behind.
+  auto put = [&](int buffer, int c, uint32_t n) {
+    if (CL == 1) {
+      if (lane == 0) part[buffer][c][warp] = n;
+    } else if (lane < CL) {
+      uint32_t at;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(&part[buffer][c][mine_at])), "r"(lane));
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(n) : "memory");
+    }
+  };
+  auto barrier = [&]() {
+    __syncwarp();
+    if (CL == 1) __syncthreads();
+    else asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  };
+  if (CL > 1) barrier();                                  // the others' shared memory may be written once they run
   uint32_t key[ITEMS];
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
@@ -269,10 +292,15 @@ cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
   }
   // Slots behind the row have key 0, like NaNs: never above T, and last in the order among equals.
   const uint32_t budget = (uint32_t)a.budget;
-  uint32_t T = 0, at_t = (uint32_t)(ITEMS * blockDim.x), above = 0;   // keys >= T, keys above the bits still open
+  uint32_t T = 0, at_t = (uint32_t)(CL * ITEMS * blockDim.x), above = 0;   // keys >= T, keys above the bits still open
   bool exact = false;     // as many keys >= T as are kept
   int shift = 31, buf = 0;
-  auto total = [&](int c) { return __reduce_add_sync(0xFFFFFFFFu, lane < warps ? part[buf][c][lane] : 0u); };
+  auto total = [&](int c) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) n += CL > 1 || lane < warps ? part[buf][c][r * 32 + lane] : 0u;
+    return __reduce_add_sync(0xFFFFFFFFu, n);
+  };
   if (tid == 0) windowed = 0;
   if (ITEMS > 1) {
     for (; shift >= 0 && !exact && at_t - above > blockDim.x; --shift, buf ^= 1) {
@@ -281,8 +309,8 @@ cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
 #pragma unroll
       for (int k = 0; k < ITEMS; ++k) n += key[k] >= cand ? 1u : 0u;
       n = __reduce_add_sync(0xFFFFFFFFu, n);
-      if (lane == 0) part[buf][0][warp] = n;
-      __syncthreads();    // the other buffer is written next: nobody can be a whole pass behind
+      put(buf, 0, n);
+      barrier();
       n = total(0);
       if (n >= budget) {
         T = cand;
@@ -298,9 +326,20 @@ cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
     if (ITEMS > 1) {
       const uint32_t span = shift == 31 ? 0xFFFFFFFFu : (2u << shift) - 1u;   // T .. T + span are open
       __syncthreads();
+      // (one addition a warp: a thousand that wait for one another took 9 us)
+      uint32_t own = 0;
 #pragma unroll
-      for (int k = 0; k < ITEMS; ++k)
-        if (key[k] - T <= span) window[atomicAdd(&windowed, 1u)] = key[k];
+      for (int k = 0; k < ITEMS; ++k) own += (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, key[k] - T <= span));
+      uint32_t at = 0;
+      if (lane == 0 && own) at = atomicAdd(&windowed, own);
+      at = __shfl_sync(0xFFFFFFFFu, at, 0);
+#pragma unroll
+      for (int k = 0; k < ITEMS; ++k) {
+        const bool open = key[k] - T <= span;
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, open);
+        if (open) window[at + __popc(some & ((1u << lane) - 1u))] = key[k];
+        at += __popc(some);
+      }
       __syncthreads();
       if (tid < (int)windowed) mine = window[tid];
     } else {
@@ -310,9 +349,9 @@ cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
       const int bits = shift >= 1 ? 2 : 1, low = shift + 1 - bits, cands = (1 << bits) - 1;
       for (int c = 0; c < cands; ++c) {
         const uint32_t n = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine >= (T | ((uint32_t)(c + 1) << low))));
-        if (lane == 0) part[buf][c][warp] = n;
+        put(buf, c, n);
       }
-      __syncthreads();
+      barrier();
       for (int c = cands - 1; c >= 0; --c) {
         const uint32_t n = above + total(c);
         if (n >= budget) {
@@ -335,22 +374,23 @@ cache_select_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) {
   }
   gt = __reduce_add_sync(0xFFFFFFFFu, gt);
   eq = __reduce_add_sync(0xFFFFFFFFu, eq);
-  __syncthreads();
-  uint32_t* sum = &part[0][0][0];
-  uint32_t* sum_eq = &part[1][0][0];
-  if (lane == 0) {
-    sum[warp] = gt;
-    sum_eq[warp] = eq;
+  put(buf, 0, gt);
+  put(buf, 1, eq);
+  barrier();
+  uint32_t before_gt = 0, before_eq = 0;
+#pragma unroll
+  for (int r = 0; r < CL; ++r) {
+    const bool in_front = r * 32 + lane < mine_at;
+    before_gt += in_front ? part[buf][0][r * 32 + lane] : 0u;
+    before_eq += in_front ? part[buf][1][r * 32 + lane] : 0u;
   }
-  __syncthreads();
-  uint32_t all_gt = lane < warps ? sum[lane] : 0u, all_eq = lane < warps ? sum_eq[lane] : 0u;
-  const uint32_t before_gt = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? all_gt : 0u);
-  const uint32_t before_eq = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? all_eq : 0u);
-  all_gt = __reduce_add_sync(0xFFFFFFFFu, all_gt);
+  before_gt = __reduce_add_sync(0xFFFFFFFFu, before_gt);
+  before_eq = __reduce_add_sync(0xFFFFFFFFu, before_eq);
+  const uint32_t all_gt = total(0);
   const uint32_t need = budget - all_gt;                  // of the keys equal to T
   uint32_t g = before_gt, e = before_eq;
   const uint32_t lower = (1u << lane) - 1u;
-  int32_t* out = a.kept + (int64_t)blockIdx.x * a.budget;
+  int32_t* out = a.kept + (int64_t)row * a.budget;
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
     const bool is_gt = key[k] > T, is_eq = key[k] == T;
@@ -373,7 +413,7 @@ cache_select_long_kernel(const SelectArgs a, unsigned* __restrict__ dev_status) 
   __shared__ uint32_t sh_prefix, sh_need;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int len;
-  if (!select_row(a, len, dev_status)) return;
+  if (!select_row(a, blockIdx.x, true, len, dev_status)) return;
   const float* w = a.weights + (int64_t)blockIdx.x * a.cols;
   int32_t* out = a.kept + (int64_t)blockIdx.x * a.budget;
   auto key_of = [&](int i) { return (i < a.sinks || i >= len - a.recent) ? 0xFFFFFFFFu : weight_key(w[i]); };
