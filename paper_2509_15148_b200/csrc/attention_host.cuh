@@ -274,6 +274,8 @@ int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
                        k_head_stride | v_token_stride | v_head_stride;
   const bool wide = bits % 8 == 0 && aligned(q, 16) && aligned(k, 16) && aligned(v, 16) && aligned(q_out, 16) &&
                     rotary_pairs % (interleaved ? 4 : 8) == 0;
+  a.lanes_log2 = 0;
+  while (a.lanes_log2 < 3 && 16 << a.lanes_log2 < D) ++a.lanes_log2;
   a.tpb = M >= 4 * 8 * (int64_t)di->sm_count ? 4 : 1;
   const int64_t gx = (max_tokens + a.tpb - 1) / a.tpb;
   if (gx > 0x7FFFFFFF) return ATTS_ERR_SHAPE;

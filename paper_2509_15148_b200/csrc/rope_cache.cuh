@@ -79,10 +79,12 @@ struct Pack<__half> {
 // The angle pos * f is formed and reduced to a fraction of a turn in 64 bits (2 multiplications and a rounding per
 // (token, pair), shared by all heads), so the fp32 cosine sees an argument in [-pi, pi] at any position.
 // Bound: HBM.  16,000 tokens of 40 + 8 + 8 heads of 128: 67 us = 5.4 TB/s of reads and writes, 0.82 of a plain copy; one to
-// four tokens a block and eight threads a row keep 32 rows of 256 bytes under way per block.
+// four tokens a block, and one thread for every 32 bytes of a row, keep 8 KB under way per block.  Each thread loads two
+// 16-byte pieces before it stores either; with the pieces one after the other, 19 x 295 tokens of 40 + 8 + 8 heads with
+// half of 128 rotated took 32.8 us instead of 28.6, and 32 x 400 of 16 + 16 + 16 heads of 64, on eight threads a row, 35.2
+// instead of 26.1.  Two or eight tokens a block: 70.7 and 72.1 us at 16,000 tokens, against 67.5 with four.
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kRopeThreads = 256;
-constexpr int kRopeLanes = 8;  // threads that share a row
 
 struct RopeArgs {
   const char *q, *k, *v;
@@ -91,6 +93,7 @@ struct RopeArgs {
   const int32_t *positions, *ctx, *cu;
   const double* freqs;
   int pairs, D, Hq, M, tpb, max_tokens;
+  int lanes_log2;  // threads that share a row: one for every 32 bytes, at most 8
   float mscale;
   CacheView cache;
 };
@@ -123,8 +126,8 @@ rope_append_kernel(const RopeArgs a, unsigned* __restrict__ dev_status) {
   __syncthreads();
 
   const int rows = a.Hq + 2 * a.cache.heads;
-  const int lane = threadIdx.x % kRopeLanes;
-  for (int r = threadIdx.x / kRopeLanes; r < nt * rows; r += kRopeThreads / kRopeLanes) {
+  const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
+  for (int r = threadIdx.x >> a.lanes_log2; r < nt * rows; r += kRopeThreads >> a.lanes_log2) {
     const int t = r / rows, h = r - t * rows;
     const int64_t token = first + t0 + t;
     const T* src;
@@ -154,47 +157,46 @@ rope_append_kernel(const RopeArgs a, unsigned* __restrict__ dev_status) {
       const uint4* s4 = reinterpret_cast<const uint4*>(src);
       uint4* d4 = reinterpret_cast<uint4*>(dst);
       const int turned = turn ? a.pairs / 4 : 0;  // 16-byte pieces that are rotated
-      if (INTERLEAVED) {
-        for (int c = lane; c < a.D / 8; c += kRopeLanes) {
-          uint4 x = s4[c];
-          if (c < turned) {
-            uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      // A thread has two pieces under way at a time: the two halves of eight rotated pairs, or neighbours.
+      const int pieces = a.D / 8, half = INTERLEAVED ? 0 : turned / 2, rest = INTERLEAVED ? 0 : turned;
+      for (int u = lane; u < half + (pieces - rest + 1) / 2; u += lanes) {
+        const bool halves = u < half;
+        const int pa = halves ? u : rest + 2 * (u - half), pb = halves ? u + half : pa + 1;
+        uint4 x = s4[pa], y = make_uint4(0, 0, 0, 0);
+        if (pb < pieces) y = s4[pb];
+        uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+        if (INTERLEAVED) {
+          auto rotate = [&](uint32_t (&w)[4], int piece) {
+            if (piece >= turned) return;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float2 f = Pack<T>::unpack(w[e]), g = cs[4 * c + e];
+              const float2 f = Pack<T>::unpack(w[e]), g = cs[4 * piece + e];
               w[e] = Pack<T>::pack(f.x * g.x - f.y * g.y, f.y * g.x + f.x * g.y);
             }
-            x = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-          d4[c] = x;
-        }
-      } else {
-        const int half = turned / 2;
-        for (int c = lane; c < half; c += kRopeLanes) {
-          const uint4 x = s4[c], y = s4[c + half];
-          const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
-          uint32_t ow[4], pw[4];
+          };
+          rotate(xw, pa);
+          rotate(yw, pb);
+        } else if (halves) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float2 f = Pack<T>::unpack(xw[e]), g = Pack<T>::unpack(yw[e]);
-            const float2 c0 = cs[8 * c + 2 * e], c1 = cs[8 * c + 2 * e + 1];
-            ow[e] = Pack<T>::pack(f.x * c0.x - g.x * c0.y, f.y * c1.x - g.y * c1.y);
-            pw[e] = Pack<T>::pack(g.x * c0.x + f.x * c0.y, g.y * c1.x + f.y * c1.y);
+            const float2 c0 = cs[8 * u + 2 * e], c1 = cs[8 * u + 2 * e + 1];
+            xw[e] = Pack<T>::pack(f.x * c0.x - g.x * c0.y, f.y * c1.x - g.y * c1.y);
+            yw[e] = Pack<T>::pack(g.x * c0.x + f.x * c0.y, g.y * c1.x + f.y * c1.y);
           }
-          d4[c] = make_uint4(ow[0], ow[1], ow[2], ow[3]);
-          d4[c + half] = make_uint4(pw[0], pw[1], pw[2], pw[3]);
         }
-        for (int c = turned + lane; c < a.D / 8; c += kRopeLanes) d4[c] = s4[c];
+        d4[pa] = make_uint4(xw[0], xw[1], xw[2], xw[3]);
+        if (pb < pieces) d4[pb] = make_uint4(yw[0], yw[1], yw[2], yw[3]);
       }
     } else {
       const int turned = turn ? a.pairs : 0;
-      for (int i = lane; i < turned; i += kRopeLanes) {
+      for (int i = lane; i < turned; i += lanes) {
         const int i0 = INTERLEAVED ? 2 * i : i, i1 = INTERLEAVED ? 2 * i + 1 : i + a.pairs;
         const float x = Pack<T>::get(src[i0]), y = Pack<T>::get(src[i1]);
         dst[i0] = Pack<T>::put(x * cs[i].x - y * cs[i].y);
         dst[i1] = Pack<T>::put(y * cs[i].x + x * cs[i].y);
       }
-      for (int i = 2 * turned + lane; i < a.D; i += kRopeLanes) dst[i] = src[i];
+      for (int i = 2 * turned + lane; i < a.D; i += lanes) dst[i] = src[i];
     }
   }
 }
