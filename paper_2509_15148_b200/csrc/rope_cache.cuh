@@ -78,7 +78,7 @@ struct Pack<__half> {
 // and sines (shared by all heads), then streams the rows [query heads | key heads | value heads] of those tokens.
 // The angle pos * f is formed and reduced to a fraction of a turn in 64 bits (2 multiplications and a rounding per
 // (token, pair), shared by all heads), so the fp32 cosine sees an argument in [-pi, pi] at any position.
-// Bound: HBM.  16,000 tokens of 40 + 8 + 8 heads of 128: 67 us = 5.4 TB/s of reads and writes, 0.82 of a plain copy; one to
+// Bound: HBM.  16,000 tokens of 40 + 8 + 8 heads of 128: 67.5 us = 5.4 TB/s of reads and writes, 0.82 of a plain copy; one to
 // four tokens a block, and one thread for every 32 bytes of a row, keep 8 KB under way per block.  Each thread loads two
 // 16-byte pieces before it stores either; with the pieces one after the other, 19 x 295 tokens of 40 + 8 + 8 heads with
 // half of 128 rotated took 32.8 us instead of 28.6, and 32 x 400 of 16 + 16 + 16 heads of 64, on eight threads a row, 35.2
