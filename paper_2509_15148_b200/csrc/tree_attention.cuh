@@ -322,13 +322,16 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   const uint32_t bar0 = smem_base + Cfg::kBars;
   auto full_bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   auto empty_bar = [&](int i) { return bar0 + 8u * (uint32_t)(kStages + i); };
-  const uint32_t q_bar = bar0 + 8u * (2 * kStages), clean_bar = q_bar + 8u, join_bar = q_bar + 16u, flag_bar = q_bar + 24u, list_bar = q_bar + 32u;
-  auto s_bar = [&](int i) { return q_bar + 40u + 8u * (uint32_t)i; };
-  auto p_bar = [&](int i) { return q_bar + 56u + 8u * (uint32_t)i; };
-  auto o_bar = [&](int i) { return q_bar + 72u + 8u * (uint32_t)i; };
-  auto m_full = [&](int i) { return q_bar + 88u + 8u * (uint32_t)i; };
-  auto m_empty = [&](int i) { return q_bar + 88u + 8u * (uint32_t)(kMaskRing + i); };
-  constexpr int kBarCount = 2 * kStages + 11 + 2 * kMaskRing;
+  // One for each stage, so that warp 3 cannot be two completions ahead of warp 1 (whose wait by parity would not see the first):
+  // a stage is cleaned again only after it was refilled, and refilled only after warp 1's products released it.
+  auto clean_bar = [&](int i) { return bar0 + 8u * (uint32_t)(2 * kStages + i); };
+  const uint32_t q_bar = bar0 + 8u * (3 * kStages), join_bar = q_bar + 8u, flag_bar = q_bar + 16u, list_bar = q_bar + 24u;
+  auto s_bar = [&](int i) { return q_bar + 32u + 8u * (uint32_t)i; };
+  auto p_bar = [&](int i) { return q_bar + 48u + 8u * (uint32_t)i; };
+  auto o_bar = [&](int i) { return q_bar + 64u + 8u * (uint32_t)i; };
+  auto m_full = [&](int i) { return q_bar + 80u + 8u * (uint32_t)i; };
+  auto m_empty = [&](int i) { return q_bar + 80u + 8u * (uint32_t)(kMaskRing + i); };
+  constexpr int kBarCount = 3 * kStages + 10 + 2 * kMaskRing;
   static_assert(8 * kBarCount + 32 <= 512, "room for the barriers");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kBars + 8 * kBarCount);
   volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -343,9 +346,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     for (int i = 0; i < kStages; ++i) {
       mbar_init(full_bar(i), 1);
       mbar_init(empty_bar(i), 2);     // the products that read the stage, and warp 3
+      mbar_init(clean_bar(i), 1);
     }
     mbar_init(q_bar, 1);
-    mbar_init(clean_bar, 1);
     mbar_init(join_bar, 4);
     mbar_init(flag_bar, 4 * kStreams);
     mbar_init(list_bar, 1);
@@ -474,7 +477,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       int stage = 0;
       uint32_t phase = 0;
       bool ok = has(0, false) && wait_warp(q_bar, 0);
-      uint32_t p_phase = 0, clean_phase = 0;   // a bit per stream
+      uint32_t p_phase = 0, clean_phase = 0;   // a bit per stream, a bit per stage
       const int streams = TWO ? (two ? 2 : 1) : 1;   // that use each tile
       const uint32_t tm = uniform(tmem_base), base = uniform(smem_base);
       // S_st = Q (of stream st if TWO) K^T of the tile in stage `at`; `last`: nothing else reads the stage
@@ -503,8 +506,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         tile_of(i, f);
         ok = wait_warp(full_bar(stage), phase);
         if (ok && (f & kTileDead)) {
-          ok = wait_warp(clean_bar, clean_phase);
-          clean_phase ^= 1u;
+          ok = wait_warp(clean_bar(stage), (clean_phase >> stage) & 1u);
+          clean_phase ^= 1u << stage;
         }
         const bool more = ok && has(i + kLead, false);
         if (!ok) break;
@@ -606,7 +609,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) mbar_arrive(clean_bar);
+          if (lane == 0) mbar_arrive(clean_bar(stage));
         }
         release();
         if (has(ik, false)) pass_key();

@@ -1,0 +1,103 @@
+"""Attention side at the places where roles of a kernel meet, lengths are cut or a launch takes another form.
+
+Tolerances.  With u the type's unit roundoff, rounding p and then o moves an output by at most u (sum p |v| + |o|); the fp32 part
+(scores of magnitude up to 40 off by 2e-5, exponentials and sums by 1e-5) by 1e-4 sum p |v|; fp16 probabilities, carried 2^6
+larger and at least 1 at a row's maximum, lose at most 2^-31 each below the type's normal range, n 2^-31 max |v| over n slots.
+The roundings are independent and each is spread over at most +-u of its value, u / sqrt(3) in the mean square: so the outputs of
+a whole batch are off by at most sqrt((u^2 / 3) (sum p^2 v^2 + o^2)) plus the fp32 part in the mean square, of which 1.2 times is
+allowed.  lse and weights: as in test_gpu_attention.py."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_15148_b200 import binding
+from tests.test_gpu_attention import BF, FP, UNIT, Batch
+
+pytestmark = pytest.mark.gpu
+
+
+class Exact:
+    """The definition in fp64 over slots below `cut` (of every sequence): out, lse, weights, sum p |v|, sum p^2 v^2."""
+
+    def __init__(self, b, cut=1 << 30):
+        G, f64 = b.Hq // b.Hk, torch.float64
+        self.out, self.pv, self.p2v2 = (torch.zeros(b.M, b.Hq, b.D, dtype=f64, device="cuda") for _ in range(3))
+        self.lse = torch.full((b.M, b.Hq), -float("inf"), dtype=f64, device="cuda")
+        self.w = torch.zeros(b.B, b.Hk, min(b.ml, cut), dtype=f64, device="cuda")
+        self.slots, self.vmax = int(b.len_h.max()), torch.nan_to_num(b.v.float()).abs().max().item()
+        for s in range(b.B):
+            n, c, S = int(b.tokens[s]), int(b.ctx_h[s]), min(int(b.len_h[s]), cut)
+            par = b.parent[b.cu_h[s]:b.cu_h[s + 1]]
+            see = np.zeros((n, c + n), bool)
+            for t in range(n):
+                if par[t] != -2:
+                    see[t, :c] = True
+                    if par[t] >= 0:
+                        see[t, c:] = see[par[t], c:]
+                    see[t, c + t] = True
+            see = torch.from_numpy(see[:, :S]).cuda()
+            held = see.any(0)      # what nobody sees may hold anything
+            pages = b.table[s, :-(-S // b.page)].long()
+            rows = slice(int(b.cu_h[s]), int(b.cu_h[s + 1]))
+            for h in range(b.Hk if n else 0):
+                heads = slice(h * G, (h + 1) * G)
+                k, v = (torch.where(held[:, None], x[pages, :, h].flatten(0, 1)[:S].double(), 0.0) for x in (b.k, b.v))
+                x = torch.einsum("tgd,sd->tgs", b.q[rows, heads].double(), k) * b.scale
+                x.masked_fill_(~see[:, None], -float("inf"))
+                l = torch.logsumexp(x, -1)
+                p = torch.exp(x - torch.where(torch.isinf(l), 0.0, l)[..., None])
+                self.out[rows, heads], self.lse[rows, heads] = p @ v, l
+                self.pv[rows, heads], self.p2v2[rows, heads] = p @ v.abs(), (p * p) @ (v * v)
+                self.w[s, h, :S] = p.sum((0, 1))
+
+    def check(self, b, out, lse, rows=slice(None)):
+        u, got = UNIT[b.dtype], out[rows].double()
+        want, pv, p2v2 = self.out[rows], self.pv[rows], self.p2v2[rows]
+        fp32 = 1e-4 * pv + (self.slots * 2.0 ** -31 * self.vmax if b.dtype is FP else 0.0)
+        err = (got - want).abs()
+        assert not torch.isnan(got).any()
+        assert (err <= u * (pv + want.abs()) + fp32).all(), (err - u * (pv + want.abs()) - fp32).max().item()
+        rms = lambda x: x.square().mean().sqrt().item()  # noqa: E731
+        assert rms(err) <= 1.2 * (rms((u * u / 3 * (p2v2 + want.square())).sqrt()) + rms(fp32)), rms(err)
+        dead, want_lse, got_lse = torch.isinf(self.lse[rows]), self.lse[rows], lse[rows].double()
+        assert torch.equal(got_lse == -float("inf"), dead)
+        assert ((got_lse - want_lse)[~dead].abs() <= 5e-5 + 1e-5 * want_lse[~dead].abs()).all()
+
+    def check_weights(self, b, got):
+        e = (got[..., :self.w.shape[-1]].double() - self.w).abs() - 1e-4 * self.w.abs() - 1e-9
+        assert not torch.isnan(got).any() and e.max().item() <= 0, e.max().item()
+
+
+def padded_chains(b, pad):
+    """Turns a batch's sequences into chains with padding tokens at the given places, whose slots hold NaN."""
+    par = []
+    for s, n in enumerate(b.tokens):
+        p, last = np.full(n, -2), -1
+        for i in range(n):
+            if i in pad:
+                slot = int(b.ctx_h[s]) + i
+                for c in (b.k, b.v):
+                    c[b.table_h[s, slot // b.page], slot % b.page] = float("nan")
+            else:
+                p[i], last = last, i
+        par.append(p)
+    b.parent = np.concatenate(par).astype(np.int32)
+    b.pre, b.end = (x.cuda() for x in binding.tree_plan(b.parent, b.cu_h)[:2])
+
+
+# One row tile (G = 1, drafts over two slot tiles), many of those (one stream, two CTAs an SM), two row tiles with drafts over two,
+# three and four slot tiles.  Every one of those holds padding and the last ends inside, so that they are cleared one after the
+# other, behind nothing or behind several cached tiles.
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tokens,Hq,Hk", [([100], 4, 4), ([120] * 60, 4, 4), ([200], 8, 2), ([330], 8, 2), ([460], 8, 2), ([460, 17, 300], 5, 1)])
+@pytest.mark.parametrize("ctx", [0, 60, 1000])
+def test_several_tiles_with_padding_in_a_row(D, tokens, Hq, Hk, ctx):
+    b = Batch(41, tokens, [ctx] * len(tokens), Hq, Hk, D, 16, BF)
+    padded_chains(b, set(range(5, 460, 40)))
+    want = Exact(b)
+    assert binding.last_device_status() == 0
+    for _ in range(3):
+        out, lse = b.attend()
+        assert binding.last_device_status() == 0
+        want.check(b, out, lse)
+    want.check_weights(b, b.weights(want.lse.float()))
