@@ -490,7 +490,7 @@ int atts_cache_select(const float* weights, int64_t weights_cols, const int32_t*
  * `dst` gets the key and value of slot kept[b, h, c] of `src`.  The pages written must not be pages read.
  *   kept          dev  [num_seqs, heads, kept_cols] int32, each in [0, pages of the sequence in src): a slot whose page is
  *                      missing or out of range is skipped and ATTS_DEV_PAGE_RANGE recorded
- *   counts        dev  [num_seqs] int32, cut at kept_cols
+ *   counts        dev  [num_seqs] int32, 0 <= counts[b] <= kept_cols (else ATTS_DEV_SEQ_RANGE, cut)
  *   weights_in    dev  [num_seqs, heads, in_cols] fp32 or NULL; then weights_out [num_seqs, heads, kept_cols] gets the
  *                      kept slots' weights and 0 behind them.  kept slots must be below in_cols (others: 0, flagged)
  */

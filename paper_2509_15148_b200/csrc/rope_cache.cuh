@@ -498,7 +498,8 @@ cache_gather_kernel(const CacheView src, const CacheView dst, int lanes, int spa
   const int seq = blockIdx.y, head = blockIdx.x % src.heads;
   const int64_t row = (int64_t)seq * src.heads + head;
   const int64_t c0 = (int64_t)(blockIdx.x / src.heads) * span;
-  const int64_t live_to = min((int64_t)counts[seq], kept_cols);
+  const int64_t count = counts[seq], live_to = max((int64_t)0, min(count, kept_cols));
+  if (live_to != count && threadIdx.x == 0 && blockIdx.x == 0) atomicOr(dev_status, kDevSeqRange);
   {
     const int64_t c = c0 + threadIdx.x;
     int64_t a = -1, b = -1;
@@ -527,7 +528,7 @@ cache_gather_kernel(const CacheView src, const CacheView dst, int lanes, int spa
   const int per = kGatherThreads / lanes;                          // rows of the block at a time
   const int sub = threadIdx.x / lanes, piece = 16 * (threadIdx.x - sub * lanes);
   if (sub >= per) return;
-  const int rows = (int)min((int64_t)span, live_to - c0);
+  const int rows = (int)max((int64_t)0, min((int64_t)span, live_to - c0));
   for (int r0 = sub; r0 < rows; r0 += per * kGatherUnroll) {
     uint4 k[kGatherUnroll], v[kGatherUnroll];
 #pragma unroll

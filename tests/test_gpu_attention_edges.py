@@ -101,3 +101,25 @@ def test_several_tiles_with_padding_in_a_row(D, tokens, Hq, Hk, ctx):
         assert binding.last_device_status() == 0
         want.check(b, out, lse)
     want.check_weights(b, b.weights(want.lse.float()))
+
+
+@pytest.mark.parametrize("count", [-3, -300, -2 ** 31, 601, 2 ** 31 - 1])
+def test_gather_cuts_and_records_counts_that_do_not_fit(count):
+    """kept_cols = 600: blocks that begin beyond the count, and beyond their first one."""
+    b = Batch(42, [1, 1], [700, 650], 2, 2, 64, 16, BF)
+    kept = torch.arange(600, dtype=torch.int32, device="cuda").repeat(2, 2, 1)
+    ko, vo = (torch.full((80, 16, 2, 64), 9.0, dtype=BF, device="cuda") for _ in range(2))
+    dst = binding.PagedCache(ko, vo, torch.arange(80, dtype=torch.int32, device="cuda").view(2, 40))
+    w, wo = torch.rand(2, 2, 700, device="cuda"), torch.full((2, 2, 600), 9.0, device="cuda")
+    assert binding.last_device_status() == 0
+    binding.cache_gather(b.cache, kept, torch.tensor([count, 5], dtype=torch.int32, device="cuda"), dst, w, wo)
+    assert binding.last_device_status() == binding.DEV_SEQ_RANGE
+    n = 600 if count > 0 else 0
+    slot = torch.arange(600, device="cuda")
+    pages = b.table.long()[:, slot // 16]
+    for got, src in ((ko, b.k), (vo, b.v)):
+        first, second = got.view(2, 640, 2, 64)
+        assert torch.equal(first[:n], src[pages[0], slot % 16][:n]) and (first[n:] == 9.0).all()
+        assert torch.equal(second[:5], src[pages[1], slot % 16][:5]) and (second[5:] == 9.0).all()
+    assert torch.equal(wo[0, :, :n], w[0, :, :n]) and (wo[0, :, n:] == 0).all()
+    assert torch.equal(wo[1, :, :5], w[1, :, :5]) and (wo[1, :, 5:] == 0).all()
