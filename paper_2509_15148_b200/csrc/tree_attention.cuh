@@ -312,7 +312,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   const int tile0 = chunk * plan.chunk, tile1 = min(ntiles, tile0 + plan.chunk);
   if (chunk > 0 && tile0 >= ntiles) return;
   const bool two = MODE == kRowsTwo && ntok > plan.tpt;
-  const int tree0 = min(s.ctx / kAttnTile, ntiles);   // first tile that is not all cached slots
+  const int tree0 = min(s.ctx, s.len) / kAttnTile;    // first tile that is not all cached slots (a cache cut at max_len ends inside one)
 
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));

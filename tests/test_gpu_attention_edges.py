@@ -123,3 +123,17 @@ def test_gather_cuts_and_records_counts_that_do_not_fit(count):
         assert torch.equal(second[:5], src[pages[1], slot % 16][:5]) and (second[5:] == 9.0).all()
     assert torch.equal(wo[0, :, :n], w[0, :, :n]) and (wo[0, :, n:] == 0).all()
     assert torch.equal(wo[1, :, :5], w[1, :, :5]) and (wo[1, :, 5:] == 0).all()
+
+
+@pytest.mark.parametrize("tree", ["chain", "random"])
+@pytest.mark.parametrize("tokens,ctx,cut,Hq,Hk,D", [([2], [300], 200, 8, 2, 128), ([200], [300], 200, 8, 2, 64), ([4, 9], [5000, 40], 4999, 8, 2, 128),
+                                                    ([4], [300], 256, 8, 2, 128), ([3] * 200, [250] * 200, 130, 8, 4, 128), ([150], [1000], 1100, 8, 2, 64)])
+def test_sequences_cut_at_max_len_see_exactly_the_slots_below_it(tokens, ctx, cut, Hq, Hk, D, tree):
+    b = Batch(43, tokens, ctx, Hq, Hk, D, 16, BF, tree=tree)
+    want = Exact(b, cut)
+    b.ml = cut
+    out, lse = b.attend()
+    assert binding.last_device_status() == binding.DEV_SEQ_RANGE
+    want.check(b, out, lse)
+    want.check_weights(b, b.weights(want.lse.float()))
+    assert binding.last_device_status() == binding.DEV_SEQ_RANGE
