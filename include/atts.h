@@ -462,6 +462,7 @@ int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
  *   weights_out[b, h, s] = weights_in[b, h, s] + sum over tokens i of b and the query heads g of key head h of
  *                          exp(scale * q[i, g] . k_s - lse[i, g]),  over the slots that i sees
  * and 0 for slots s from the sequence's length up to max_len.  lse as atts_tree_attention wrote it for the same batch.
+ * A sequence that is left out (ATTS_DEV_SEQ_RANGE) adds nothing: weights_out = weights_in in all columns up to max_len.
  *   weights_in    dev  [num_seqs, heads, weights_cols] fp32, NULL for zeros, may be weights_out (update in place)
  *   weights_out   dev  the same shape; columns from max_len on are not written.  max_len <= weights_cols
  * Other arguments as atts_tree_attention.  Every sum is made in one order: bit-reproducible.

@@ -982,7 +982,8 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
   float* wout = a.wout + ((int64_t)seq * a.q.cache.heads + hk) * a.wcols;
   const float* win = a.win ? a.win + ((int64_t)seq * a.q.cache.heads + hk) * a.wcols : nullptr;
   const int len = ok_seq ? s.len : 0;
-  auto old_weight = [&](int slot) { return win && slot < len ? win[slot] : 0.f; };
+  // (a sequence that does not fit is left out: what it gathered before stays)
+  auto old_weight = [&](int slot) { return win && (slot < len || !ok_seq) ? win[slot] : 0.f; };
   if ((int64_t)tile0 * kAttnTile >= a.q.max_len) return;       // (a cluster behind the dealt tiles reaches beyond the row)
   if (tile0 * kAttnTile >= len || s.n == 0) {
     for (int slot = tile0 * kAttnTile + threadIdx.x; slot < min(tile1 * kAttnTile, a.q.max_len); slot += kWeightThreads) wout[slot] = old_weight(slot);

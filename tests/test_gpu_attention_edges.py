@@ -11,7 +11,7 @@ import pytest
 import torch
 
 from paper_2509_15148_b200 import binding
-from tests.test_gpu_attention import BF, FP, UNIT, Batch
+from tests.test_gpu_attention import BF, FP, UNIT, Batch, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -137,3 +137,31 @@ def test_sequences_cut_at_max_len_see_exactly_the_slots_below_it(tokens, ctx, cu
     want.check(b, out, lse)
     want.check_weights(b, b.weights(want.lse.float()))
     assert binding.last_device_status() == binding.DEV_SEQ_RANGE
+
+
+# one row tile, and more than one
+@pytest.mark.parametrize("tokens,ctx,Hq,Hk", [([4, 3], [100, 300], 8, 2), ([150, 90], [300, 260], 8, 2)])
+@pytest.mark.parametrize("bad", ["ctx", "tokens", "cu"])
+def test_weights_of_a_sequence_that_does_not_fit_stay(tokens, ctx, Hq, Hk, bad):
+    b = Batch(44, tokens, ctx, Hq, Hk, 128, 16, BF)
+    want = Exact(b)
+    lse = want.lse.float()
+    if bad == "ctx":
+        b.ctx = i32([-1, ctx[1]])
+    elif bad == "tokens":
+        b.mt = tokens[0] - 1
+    else:
+        b.cu = i32([-1] + b.cu_h[1:].tolist())
+    before = torch.rand(2, Hk, b.ml, device="cuda")
+    for inplace in (False, True):
+        win = before.clone()
+        out = win if inplace else torch.full_like(win, float("nan"))
+        binding.cache_weights(b.q, b.cache, lse, b.ctx, b.cu, b.pre, b.end, b.mt, b.ml, b.scale, win, out)
+        assert binding.last_device_status() == binding.DEV_SEQ_RANGE
+        assert torch.equal(out[0], before[0])
+        n = int(b.len_h[1])
+        assert ((out[1, :, :n].double() - before[1, :, :n].double() - want.w[1, :, :n]).abs() <= 1e-4 * want.w[1, :, :n] + 1e-6).all()
+        assert (out[1, :, n:] == 0).all()
+    out = torch.full_like(before, float("nan"))
+    binding.cache_weights(b.q, b.cache, lse, b.ctx, b.cu, b.pre, b.end, b.mt, b.ml, b.scale, None, out)
+    assert binding.last_device_status() == binding.DEV_SEQ_RANGE and (out[0] == 0).all()
