@@ -758,7 +758,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       const float mm = fmaxf(m, other.x);
       const float f0 = m == -INFINITY ? 0.f : ex2_approx((m - mm) * c), f1 = other.x == -INFINITY ? 0.f : ex2_approx((other.x - mm) * c);
       const float sum = l * f0 + other.y * f1;
-      const bool empty = mine < 0 || !(sum > 0.f);
+      const bool empty = mine < 0 || sum == 0.f;     // (a NaN among a row's scores is not empty: it reaches out and lse)
       const float g0 = empty ? 0.f : f0 / sum, g1 = empty ? 0.f : f1 / sum;
       const float lse2 = empty ? -INFINITY : mm * c - AttnType<T>::shift + log2f(sum);
       const int parts = (ntiles + plan.chunk - 1) / plan.chunk;
@@ -870,13 +870,13 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] += w * p[e];
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;    // (NaN stays NaN)
   const int64_t token = row / a.Hq;
   const int head = (int)(row - token * a.Hq);
   uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + token * a.o_ts + (int64_t)head * a.o_hs + lane * E);
 #pragma unroll
   for (int e = 0; e < E; e += 2) out[e / 2] = Pack<T>::pack(o[e] * inv, o[e + 1] * inv);
-  if (a.lse && lane == 0) a.lse[row] = sum > 0.f ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+  if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
 struct WeightArgs {

@@ -165,3 +165,32 @@ def test_weights_of_a_sequence_that_does_not_fit_stay(tokens, ctx, Hq, Hk, bad):
     out = torch.full_like(before, float("nan"))
     binding.cache_weights(b.q, b.cache, lse, b.ctx, b.cu, b.pre, b.end, b.mt, b.ml, b.scale, None, out)
     assert binding.last_device_status() == binding.DEV_SEQ_RANGE and (out[0] == 0).all()
+
+
+# one chunk and several, one row tile, two, and many sequences
+@pytest.mark.parametrize("tokens,ctx,Hq,Hk", [([5], [40], 8, 2), ([5], [9000], 8, 2), ([200], [300], 8, 2), ([3] * 90, [200] * 90, 8, 2)])
+@pytest.mark.parametrize("D,dtype", [(128, BF), (64, FP)])
+@pytest.mark.parametrize("where", ["query", "key", "score"])
+def test_nan_and_infinity_reach_the_rows_that_see_them(tokens, ctx, Hq, Hk, D, dtype, where):
+    """A row is hit where one of its scores is NaN or +inf (a NaN channel of its query, a NaN key, a product that overflows); every
+    other row stays exact."""
+    b = Batch(45, tokens, ctx, Hq, Hk, D, 16, dtype, tree="chain")
+    hit = torch.zeros(b.M, Hq, dtype=torch.bool, device="cuda")
+    want = Exact(b)
+    if where == "key":       # the first sequence's third token: it and its descendants, the heads of key head 1
+        slot = int(b.ctx_h[0]) + 2
+        b.k[b.table_h[0, slot // 16], slot % 16, 1, 3] = float("nan")
+        hit[2:tokens[0], Hq // Hk:] = True
+    else:                    # the first sequence's second token, query head 3
+        hit[1, 3] = True
+        if where == "query":
+            b.q[1, 3, 7] = float("nan")
+        else:                # (a key channel of exactly 1 or -1 in every slot: the score is inf or -inf, some of them inf)
+            b.q[1, 3] = 0
+            b.q[1, 3, 0] = float("inf")
+            assert (b.k[b.table_h[0, 0], :, 0, 0] > 0).any()
+    out, lse = b.attend()
+    assert binding.last_device_status() == 0
+    assert torch.equal(torch.isnan(lse), hit) and torch.equal(torch.isnan(out), hit[..., None].expand_as(out))
+    keep = (~hit).all(1)
+    want.check(b, out, lse, keep)
