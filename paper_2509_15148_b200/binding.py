@@ -420,6 +420,19 @@ def _rows(t, name: str, M: int, heads: int, cache: PagedCache):
     return t.data_ptr(), token if M > 1 else 0, head if heads > 1 else 0
 
 
+def _stream_on(device) -> int:
+    """The current stream, provided that `device`, where the call's tensors are, is the current one: kernels run there."""
+    stream = _stream()
+    if device.index != _current_device():      # (None for the host)
+        raise ValueError(f"the tensors are on {device}, the current device is cuda:{_current_device()}")
+    return stream
+
+
+def _current_device() -> int:
+    import torch
+    return torch._C._cuda_getDevice()
+
+
 def _vec(t, name: str, dtype, n: int, device):
     """Pointer of a contiguous tensor of n entries."""
     if t.dtype is not dtype or t.numel() != n or t.device != device or not t.is_contiguous():
@@ -488,7 +501,7 @@ def rope_append(q, k, v, positions, freqs, cache: PagedCache, ctx_lens, cu_token
     _check(load().atts_rope_append(*qr, *kr, *vr, _vec(positions, "positions", torch.int32, M, dev),
                                    _vec(freqs, "freqs", torch.float64, n, dev), n, mscale, 1 if interleaved else 0, cache._ref,
                                    _vec(ctx_lens, "ctx_lens", torch.int32, B, dev),
-                                   _vec(cu_tokens, "cu_tokens", torch.int32, B + 1, dev), M, Hq, max_tokens, *outr, _stream()),
+                                   _vec(cu_tokens, "cu_tokens", torch.int32, B + 1, dev), M, Hq, max_tokens, *outr, _stream_on(dev)),
            "atts_rope_append")
 
 
@@ -506,11 +519,13 @@ def tree_attention(q, cache: PagedCache, ctx_lens, cu_tokens, pre, end, max_toke
     import torch
     M, Hq = q.shape[0], q.shape[1]
     dev, B, i32 = cache.device, cache.num_seqs, torch.int32
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: has to be contiguous, on {dev}")
     _check(load().atts_tree_attention(*_rows(q, "q", M, Hq, cache), cache._ref, _vec(ctx_lens, "ctx_lens", i32, B, dev),
                                       _vec(cu_tokens, "cu_tokens", i32, B + 1, dev), None if pre is None else _vec(pre, "pre", i32, M, dev),
                                       None if end is None else _vec(end, "end", i32, M, dev), M, Hq, max_tokens, max_len, scale,
                                       *_rows(out, "out", M, Hq, cache), None if lse is None else _vec(lse, "lse", torch.float32, M * Hq, dev),
-                                      _ptr(workspace), _nbytes(workspace), _stream()), "atts_tree_attention")
+                                      _ptr(workspace), _nbytes(workspace), _stream_on(dev)), "atts_tree_attention")
 
 
 def cache_weights(q, cache: PagedCache, lse, ctx_lens, cu_tokens, pre, end, max_tokens: int, max_len: int, scale: float, weights_in,
@@ -527,7 +542,7 @@ def cache_weights(q, cache: PagedCache, lse, ctx_lens, cu_tokens, pre, end, max_
                                      None if pre is None else _vec(pre, "pre", i32, M, dev), None if end is None else _vec(end, "end", i32, M, dev),
                                      M, Hq, max_tokens, max_len, scale,
                                      None if weights_in is None else _vec(weights_in, "weights_in", torch.float32, n, dev),
-                                     _vec(weights_out, "weights_out", torch.float32, n, dev), cols, _stream()), "atts_cache_weights")
+                                     _vec(weights_out, "weights_out", torch.float32, n, dev), cols, _stream_on(dev)), "atts_cache_weights")
 
 
 def cache_select(weights, lens, budget: int, sinks: int, recent: int, kept, counts) -> None:
@@ -539,7 +554,7 @@ def cache_select(weights, lens, budget: int, sinks: int, recent: int, kept, coun
     _check(load().atts_cache_select(_vec(weights, "weights", torch.float32, B * heads * cols, dev), cols,
                                     _vec(lens, "lens", torch.int32, B, dev), B, heads, budget, sinks, recent,
                                     _vec(kept, "kept", torch.int32, B * heads * budget, dev),
-                                    _vec(counts, "counts", torch.int32, B, dev), _stream()), "atts_cache_select")
+                                    _vec(counts, "counts", torch.int32, B, dev), _stream_on(dev)), "atts_cache_select")
 
 
 def cache_gather(src: PagedCache, kept, counts, dst: PagedCache, weights_in=None, weights_out=None) -> None:
@@ -547,6 +562,8 @@ def cache_gather(src: PagedCache, kept, counts, dst: PagedCache, weights_in=None
     must not be src's), weights_out [num_seqs, heads, cols] the kept slots' weights."""
     import torch
     dev = src.device
+    if dst.device != dev:
+        raise ValueError(f"dst: has to be on {dev} like src, not on {dst.device}")
     cols = kept.shape[-1]
     n = src.num_seqs * src.heads * cols
     in_cols = 0 if weights_in is None else weights_in.shape[-1]
@@ -554,4 +571,4 @@ def cache_gather(src: PagedCache, kept, counts, dst: PagedCache, weights_in=None
                                     _vec(counts, "counts", torch.int32, src.num_seqs, dev), dst._ref,
                                     None if weights_in is None else _vec(weights_in, "weights_in", torch.float32, src.num_seqs * src.heads * in_cols, dev),
                                     in_cols, None if weights_out is None else _vec(weights_out, "weights_out", torch.float32, n, dev),
-                                    _stream()), "atts_cache_gather")
+                                    _stream_on(dev)), "atts_cache_gather")
