@@ -447,6 +447,8 @@ def tree_plan(parent, cu_tokens):
     import torch
     parent = torch.as_tensor(parent, dtype=torch.int32).contiguous()
     cu = torch.as_tensor(cu_tokens, dtype=torch.int32).contiguous()
+    if parent.device.type != "cpu" or cu.device.type != "cpu":
+        raise ValueError("parent and cu_tokens have to be on the host")
     if cu.numel() < 1 or int(cu[-1]) != parent.numel():
         raise ValueError("cu_tokens has to end at the number of tokens")
     pre, end, depth = (torch.empty_like(parent) for _ in range(3))

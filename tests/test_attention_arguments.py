@@ -120,3 +120,14 @@ def test_a_workspace_with_gaps_is_refused(calls):
     with pytest.raises(ValueError):
         f(**{**args, "workspace": Tensor((4096,), U8, contiguous=False)})
     assert calls == []
+
+
+def test_tree_plan_refuses_device_tensors(calls):
+    """(meta tensors stand for any that are not on the host)"""
+    host = torch.tensor([-1, 0], dtype=I32), torch.tensor([0, 2], dtype=I32)
+    binding.tree_plan(*host)
+    assert calls == ["atts_tree_plan"]
+    for bad in ((host[0].to("meta"), host[1]), (host[0], host[1].to("meta"))):
+        with pytest.raises(ValueError):
+            binding.tree_plan(*bad)
+    assert calls == ["atts_tree_plan"]
