@@ -918,7 +918,12 @@ struct WeightCfg {
   static constexpr int kList = kFlags + kWeightItems;              // [items] uint16
   static constexpr int kSums = kList + 2 * kWeightItems;           // [cluster][128] sums, [128] of the odd group
   static constexpr int kBars = kSums + (kWeightMaxCluster + 1) * kAttnTile * 4;
-  static constexpr int kSmemBytes = kBars + 128 + 1024;
+  // At most two CTAs to an SM, whatever their registers: each holds 256 of its 512 columns of tensor memory until the last barrier
+  // of its cluster, so a third one would wait for columns while the CTAs that hold them may wait for it.  (With head_dim 64 the
+  // buffers alone would let a third one in.)
+  static constexpr int kNeeded = kBars + 128 + 1024;
+  static constexpr int kSmemBytes = kNeeded > 77824 ? kNeeded : 77824;
+  static_assert(2 * (kSmemBytes + 1024) <= 233472 && 3 * (kSmemBytes + 1024) > 233472, "two CTAs share an SM, three do not");
 };
 
 // Sum over 16 columns of an accumulator: 2^(c s - lse2), pairs of columns side by side.  (With 32 at a time the registers of two
