@@ -10,8 +10,9 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import attention_oracle as orc
 from paper_2509_15148_b200 import binding
-from tests.test_gpu_attention import BF, FP, UNIT, Batch, i32
+from tests.test_gpu_attention import BF, FP, LARGE, UNIT, Batch, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +195,146 @@ def test_nan_and_infinity_reach_the_rows_that_see_them(tokens, ctx, Hq, Hk, D, d
     assert torch.equal(torch.isnan(lse), hit) and torch.equal(torch.isnan(out), hit[..., None].expand_as(out))
     keep = (~hit).all(1)
     want.check(b, out, lse, keep)
+
+
+@pytest.mark.parametrize("case", LARGE + [
+    # few rows over long caches in both types and head sizes: chunks joined
+    ([4], [30000], 8, 2, 64, 32, BF, "random", 0.0),
+    ([4], [30000], 8, 2, 64, 32, FP, "random", 0.0),
+    ([13, 9], [70000, 41000], 8, 2, 128, 64, BF, "random", 0.0),
+    ([13, 9], [70000, 41000], 8, 2, 128, 64, FP, "random", 0.0),
+    ([150], [50000], 4, 2, 128, 128, BF, "fan", 0.0)])
+def test_outputs_at_size_within_their_own_bound(case):
+    """Over tens of thousands of slots outputs are small: the allowance goes by sum p |v| and, in the mean square, by sum p^2 v^2."""
+    tokens, ctx, Hq, Hk, D, page, dtype, tree, pad = case
+    b = Batch(46, tokens, ctx, Hq, Hk, D, page, dtype, tree, pad)
+    want = Exact(b)
+    out, lse = b.attend()
+    assert binding.last_device_status() == 0
+    want.check(b, out, lse)
+    want.check_weights(b, b.weights(want.lse.float()))
+
+
+@pytest.mark.parametrize("tree", ["chain", "fan"])
+def test_tiles_behind_the_listed_ones(tree):
+    """131,972 drafts of two heads: one chunk of 1032 slot tiles, 1024 of which are listed; the last eight are looked at by all."""
+    n, ctx = 131072 + 900, 5
+    assert binding.tree_attention_workspace_bytes(1, n, 2, 2, 64, n, n + ctx) == 256       # one chunk
+    b = Batch(47, [n], [ctx], 2, 2, 64, 128, BF, tree=tree)
+    out, lse = b.attend()
+    assert binding.last_device_status() == 0
+    each = -(-n // 4) if tree == "fan" else n
+    for h in range(2):
+        k, v = (x[b.table[0].long(), :, h].flatten(0, 1)[:n + ctx].double() for x in (b.k, b.v))
+        for t in (0, 1000, each - 1, n // 2, n - 1000, n - 900, n - 700, n - 1):
+            first = t // each * each
+            seen = torch.cat([torch.arange(ctx), torch.arange(ctx + first, ctx + t + 1)]).cuda()
+            s = (b.q[t, h].double() @ k[seen].T) * b.scale
+            p = torch.softmax(s, 0)
+            want, pv = p @ v[seen], p @ v[seen].abs()
+            assert ((out[t, h].double() - want).abs() <= UNIT[BF] * (pv + want.abs()) + 1e-4 * pv).all()
+            assert abs(lse[t, h].item() - torch.logsumexp(s, 0).item()) <= 5e-5 + 1e-5 * abs(lse[t, h].item())
+
+
+@pytest.mark.parametrize("tokens", [[1201, 999, 0, 1, 2600], [7000], [160] * 31])
+@pytest.mark.parametrize("D,pairs,inter", [(128, 64, False), (128, 32, True), (64, 8, False), (96, 20, True), (128, 0, False)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_rope_append_of_many_tokens(tokens, D, pairs, inter, dtype):
+    """From 4736 tokens on (148 SMs) a block takes four of them; lengths that are not multiples of four.  One rounding of a sum of two
+    products of |x|: u |y| + 2e-6 max |x| + fp16's smallest step, cosine and sine in fp64 here."""
+    Hq, Hk, page = 6, 2, 16
+    ctx = [(37 * i) % 100 for i in range(len(tokens))]
+    b = Batch(48, tokens, ctx, Hk, Hk, D, page, dtype, tree="chain")
+    assert b.M >= 4736
+    f = binding.rope_freqs(2 * pairs, 10000.0)[0].cuda()
+    pos = torch.randint(-5, 200000, (b.M,), dtype=torch.int32, device="cuda")
+    qkv = torch.randn(b.M, (Hq + 2 * Hk) * D, device="cuda").to(dtype)
+    q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([Hq * D, Hk * D, Hk * D], dim=1))
+    k0, v0 = b.k.clone(), b.v.clone()
+    angle = pos.double()[:, None] * f
+    c, s = torch.cos(angle)[:, None], torch.sin(angle)[:, None]
+
+    def want(x):
+        x = x.double()
+        y = x.clone()
+        one, two = (slice(0, 2 * pairs, 2), slice(1, 2 * pairs, 2)) if inter else (slice(0, pairs), slice(pairs, 2 * pairs))
+        y[..., one], y[..., two] = x[..., one] * c - x[..., two] * s, x[..., two] * c + x[..., one] * s
+        return y
+    seq = torch.from_numpy(np.repeat(np.arange(b.B), tokens)).cuda()
+    slot = torch.from_numpy(np.concatenate([np.arange(t) + x for t, x in zip(tokens, ctx)])).cuda()
+    pages = b.table.long()[seq, slot // page]
+    touched = torch.zeros(b.n_pages, page, dtype=torch.bool, device="cuda")
+    touched[pages, slot % page] = True
+    odd = torch.zeros(qkv.numel() + 1, dtype=dtype, device="cuda")[1:].view_as(qkv)
+    odd.copy_(qkv)
+    for rows in (qkv, odd):          # aligned, and not
+        qq, kk, vv = (t.unflatten(1, (-1, D)) for t in rows.split([Hq * D, Hk * D, Hk * D], dim=1))
+        out = torch.full((b.M, Hq, D), float("nan"), dtype=dtype, device="cuda")
+        b.k.copy_(k0), b.v.copy_(v0)
+        binding.rope_append(qq, kk, vv, pos, f, b.cache, b.ctx, b.cu, b.mt, out, interleaved=inter)
+        assert binding.last_device_status() == 0
+        for got, x in ((out, q), (b.k[pages, slot % page], k)):
+            w = want(x)
+            assert ((got.double() - w).abs() <= UNIT[dtype] * w.abs() + 2e-6 * x.double().abs().max() + 2.0 ** -25).all()
+        assert torch.equal(b.v[pages, slot % page], v)
+        for now, before in ((b.k, k0), (b.v, v0)):
+            assert torch.equal(torch.nan_to_num(now[~touched]), torch.nan_to_num(before[~touched]))
+
+
+@pytest.mark.parametrize("cols,budget,sinks,recent", [(4097, 4096, 4, 100), (9000, 1, 0, 0), (16384, 8000, 4, 512), (16385, 8192, 4, 512), (20001, 20000, 0, 0),
+                                                      (32000, 8192, 4, 512), (32767, 1, 0, 0), (32768, 16384, 0, 16384), (32768, 31000, 7, 0),
+                                                      (32769, 8192, 4, 512)])
+@pytest.mark.parametrize("kind", ["spread", "ties", "special", "equal"])
+def test_select_on_rows_of_every_form(cols, budget, sinks, recent, kind):
+    """Clusters of two with 8 and 16 keys a thread, their first and last row lengths, and the first of the long form."""
+    rs = np.random.RandomState(cols + budget)
+    lens = [cols, cols - 1, max(budget, cols // 2), budget + 1, 0]
+    B, H = len(lens), 2
+    w = np.exp(rs.randn(B, H, cols) * 3).astype(np.float32)
+    if kind == "ties":
+        w = rs.randint(0, 3, w.shape).astype(np.float32)
+    elif kind == "special":
+        w = rs.choice(np.array([np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-45, -1e-45, 3.4e38, -1.0, 2.0], np.float32), w.shape)
+    elif kind == "equal":
+        w[:] = 0.25
+    kept = torch.full((B, H, budget), 77, dtype=torch.int32, device="cuda")
+    counts = torch.full((B,), 77, dtype=torch.int32, device="cuda")
+    binding.cache_select(torch.from_numpy(w).cuda(), i32(lens), budget, sinks, recent, kept, counts)
+    got = kept.cpu().numpy()
+    for s in range(B):
+        for h in range(H):
+            want = orc.select(w[s, h], lens[s], budget, sinks, recent)
+            assert got[s, h].tolist() == want + [-1] * (budget - len(want))
+    assert counts.tolist() == [min(n, budget) for n in lens]
+    assert binding.last_device_status() == 0
+
+
+def test_batches_without_tokens_or_sequences():
+    """No drafts at all: attention and append do nothing, weights are carried over.  No sequences: nothing is done."""
+    b = Batch(49, [2, 1], [100, 30], 8, 2, 128, 16, BF)
+    none, cu = torch.empty(0, 8, 128, dtype=BF, device="cuda"), i32([0, 0, 0])
+    e = i32(np.zeros(0))
+    kv = torch.empty(0, 2, 128, dtype=BF, device="cuda")
+    f = torch.zeros(4, dtype=torch.float64, device="cuda")
+    ws = torch.empty(binding.tree_attention_workspace_bytes(2, 0, 8, 2, 128, 0, 103), dtype=torch.uint8, device="cuda")
+    lse = torch.empty(0, 8, device="cuda")
+    k0 = b.k.clone()
+    binding.rope_append(none, kv, kv, e, f, b.cache, b.ctx, cu, 0, none)
+    binding.tree_attention(none, b.cache, b.ctx, cu, e, e, 0, 103, 0.1, none, lse, ws)
+    win = torch.rand(2, 2, 110, device="cuda")
+    for bounds in (0, 5):
+        out = torch.full_like(win, 7.0)
+        binding.cache_weights(none, b.cache, lse, b.ctx, cu, None, None, bounds, 103, 0.1, win, out)
+        for s, n in enumerate((100, 30)):
+            assert torch.equal(out[s, :, :n], win[s, :, :n]) and (out[s, :, n:103] == 0).all() and (out[s, :, 103:] == 7).all()
+    assert torch.equal(torch.nan_to_num(b.k), torch.nan_to_num(k0))
+    empty = binding.PagedCache(b.k, b.v, torch.empty(0, 4, dtype=torch.int32, device="cuda"))
+    zero = i32([0])
+    binding.rope_append(none, kv, kv, e, f, empty, e, zero, 0, none)
+    binding.tree_attention(none, empty, e, zero, None, None, 0, 0, 0.1, none, lse, ws)
+    w = torch.empty(0, 2, 10, device="cuda")
+    binding.cache_weights(none, empty, lse, e, zero, None, None, 0, 10, 0.1, None, w)
+    kept = torch.empty(0, 2, 5, dtype=torch.int32, device="cuda")
+    binding.cache_select(w, e, 5, 0, 0, kept, e)
+    binding.cache_gather(empty, kept, e, empty)
+    assert binding.last_device_status() == 0
