@@ -131,17 +131,17 @@ def _ptr(t) -> int | None:
 
 def _stream() -> int:
     """The current stream of the current device (the raw handle where torch hands it out directly: 0.1 against 3.3 us)."""
-    import torch
-    global _raw_stream
+    global _raw_stream, _current_device
     if _raw_stream is None:
+        import torch
         get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-        _raw_stream = (lambda: torch.cuda.current_stream().cuda_stream) if get is None else (lambda: get(device()))
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _raw_stream = (lambda: torch.cuda.current_stream().cuda_stream) if get is None else (lambda: get(_current_device()))
         torch.cuda.current_device()       # the first use brings the device up
     return _raw_stream()
 
 
-_raw_stream = None
+_raw_stream = _current_device = None
 
 
 def score_workspace_bytes(M: int, d: int, V: int, S: int) -> int:
@@ -426,11 +426,6 @@ def _stream_on(device) -> int:
     if device.index != _current_device():      # (None for the host)
         raise ValueError(f"the tensors are on {device}, the current device is cuda:{_current_device()}")
     return stream
-
-
-def _current_device() -> int:
-    import torch
-    return torch._C._cuda_getDevice()
 
 
 def _vec(t, name: str, dtype, n: int, device):
