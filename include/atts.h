@@ -445,7 +445,9 @@ int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
  *   pre, end      dev  [M] int32 (atts_tree_plan); both NULL: every sequence's drafts are one chain (causal)
  *   scale              finite and > 0
  *   out           dev  rows [M, Hq, head_dim], aligned as q;   lse  dev [M, Hq] fp32, may be NULL
- *   workspace     dev  256-byte aligned, at least atts_tree_attention_workspace_bytes(...) for the same sizes
+ *   workspace     dev  256-byte aligned, at least atts_tree_attention_workspace_bytes(...) for the same sizes (else
+ *                      ATTS_ERR_WORKSPACE).  It does not grow with the sizes: fewer rows over the same slots are cut into more
+ *                      chunks and may need more.  A caller that keeps one buffer asks for each of its batches
  * Values of slots below a sequence's length have to be finite unless the slot is padding: a masked product is 0 * v.
  * Slots from a sequence's length on may hold anything.  Arithmetic: products accumulated in fp32, statistics and sums in
  * fp32, probabilities rounded to the inputs' type before they multiply v.  Bit-reproducible for given sizes and bounds.
@@ -466,7 +468,8 @@ int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
  * A sequence that is left out (ATTS_DEV_SEQ_RANGE) adds nothing: weights_out = weights_in in all columns up to max_len.
  *   weights_in    dev  [num_seqs, heads, weights_cols] fp32, NULL for zeros, may be weights_out (update in place)
  *   weights_out   dev  the same shape; columns from max_len on are not written.  max_len <= weights_cols
- * Other arguments as atts_tree_attention.  Every sum is made in one order: bit-reproducible.
+ * Other arguments as atts_tree_attention.  Exponentials in fp32 by the hardware's approximation, 5e-7 of a weight; every sum is
+ * made in one order: bit-reproducible.
  */
 int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
                        const float* lse, const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre,

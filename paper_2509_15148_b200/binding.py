@@ -503,6 +503,7 @@ def rope_append(q, k, v, positions, freqs, cache: PagedCache, ctx_lens, cu_token
 
 
 def tree_attention_workspace_bytes(num_seqs: int, M: int, Hq: int, heads: int, head_dim: int, max_tokens: int, max_len: int) -> int:
+    """Bytes that tree_attention needs for these sizes. Ask for every batch: a smaller one may need more (more chunks)."""
     out = c_size_t(0)
     _check(load().atts_tree_attention_workspace_bytes(num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, ctypes.byref(out)),
            "atts_tree_attention_workspace_bytes")

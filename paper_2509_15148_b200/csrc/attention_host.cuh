@@ -387,9 +387,9 @@ int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_str
   a.wait_limit = wait_limit();
   a.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
   // One row tile: a CTA goes over as many slot tiles as leave two CTAs an SM something to do, eight at most (8 sequences of
-  // 2000 slots, 8 heads: spans of 1, 2, 4 and 8 tiles take 30.7, 20.5, 18.2 and 22.5 us).  More: cached tiles are dealt to
-  // clusters whose CTAs take at least two row tiles each, of at most four (8 drafts of 500: clusters of 1, 2, 4, 8 take
-  // 311, 171, 155 and 168 us).
+  // 2000 slots, 8 heads: spans of 1, 2, 4 and 8 tiles take 25.0, 16.3, 11.8 and 14.2 us; inputs beyond L2, calls in a
+  // graph).  More: cached tiles are dealt to clusters whose CTAs take at least two row tiles each, of at most four (8 drafts
+  // of 500: clusters of 1, 2, 4 and 8 take 207, 126, 128 and 136 us).
   const int64_t nq = (max_tokens + a.tpt - 1) / a.tpt, tiles = (max_len + kAttnTile - 1) / kAttnTile;
   const bool many = nq > 1;
   a.cluster = 1;

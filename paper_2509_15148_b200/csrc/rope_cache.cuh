@@ -211,7 +211,9 @@ rope_append_kernel(const RopeArgs a, unsigned* __restrict__ dev_status) {
 // consecutive slots, so one scan over the warps places everything).  A pass over all keys costs a comparison and an addition
 // each, and one barrier behind which every block has every warp's count, written through the cluster's shared memory; once
 // no more keys than threads lie between the bounds of T, a block's share of them goes to its shared memory and the
-// remaining bits are found among them, two a pass.  64 rows of 32,000 slots: 27 us (clusters of four: 35, two waves of them).
+// remaining bits are found among them, two a pass.  64 rows of 32,000 slots: 25 us (clusters of four, two waves of them: 35;
+// of eight: 82); 8 rows: 23 us (22, 25); 64 rows of 16,000: 22 us (33, 79).  So the launch does not look at the number of rows.
+// Longer rows read their weights again for every digit, one block a row: 32 rows of 131,071 slots 273 us, 8 rows 261.
 // (A histogram of digits needs fewer passes over the keys, but weights share a few exponents and its atomics then meet in a few
 // bins: 87 us; one block a row 43 us.)
 constexpr int kSelectThreads = 1024;

@@ -132,9 +132,12 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // Short sequences in great number take kRowsBrief instead, one stream a CTA and two CTAs an SM: what a CTA costs to start and
 // end (about 9 us) is then hidden by the other one (384 CTAs of two tiles: 41 us with kRowsOne, 30 us; 128 CTAs of up to
 // 20 tiles: 38 against 50 us, since half the shared memory leaves no room to load ahead).
-// Bound: few rows over a long cache (4 x 13 tokens, 32 / 8 heads of 128, 131,071 slots) 335 us = 5.0 TB/s; many rows (chunk of 2048
-// over 6144, 64 / 8 heads) 881 us = 961 TFLOP/s, where a stream's chain of scores, exponentials (1,400 of a round's 3,750 cycles) and
-// products keeps the tensor pipe 55 % busy and the power cap sets the clock.
+// Bound: few rows over a long cache (4 x 13 tokens, 32 / 8 heads of 128, 131,071 slots) 332 to 367 us on different GPUs = 4.6 to
+// 5.1 TB/s; many rows (chunk of 2048 over 6144, 64 / 8 heads) 881 to 920 us = 921 to 961 TFLOP/s, where a stream's chain of scores,
+// exponentials (1,400 of a round's 3,750 cycles) and products keeps the tensor pipe 55 % busy and the power cap sets the clock.
+// Probabilities are rounded because the tensor pipe multiplies 16-bit operands: the output's error against 64 bits is 0.0019 of it
+// in bf16 and 0.00028 in fp16, where the output's own rounding makes 0.0017 and 0.00021; the sums are of the unrounded ones.
+// Registers: ptxas spills 8 to 24 bytes a thread, loaded again 472 to 476 bytes' worth in kRowsOne and 140 to 148 in the others.
 // The running maximum that p refers to only moves when a row exceeds it by 2^8: p <= 256, and
 // O is rescaled (a pass over tensor memory) in a few tiles instead of in every one.
 // The slots may be cut into chunks of `chunk` tiles over CTAs (few rows, long caches); the parts are then joined by
@@ -896,8 +899,11 @@ struct WeightArgs {
 //   S^T = K Q^T (tcgen05, fp32 in tensor memory), a thread per slot, and each thread adds 2^(c s - lse2) over the columns
 // of its own row: no sum crosses threads, so the order is fixed and nothing is stored but one number per slot.  Products
 // alternate between two groups of four warps with an accumulator each, and two CTAs share an SM: the exponentials (one per
-// pair, 16 a clock and SM) are what the time goes to (8 drafts of 500 over 1013 slots, 40 / 8 heads: 130 us for 2.3e8 of them, 0.41
-// of that rate; 8 sequences of one token over 2000 slots: 8 us of kernel for 29 MB).
+// pair, 16 a clock and SM) are what the time goes to first: 8 drafts of 500 over 1013 slots, 40 / 8 heads, have 2.0e8 visible pairs,
+// 43 us at that rate, and take 130 us (0.33).  The rest: 14,096 products of which the last of 296 places ends at 63 where an even
+// deal ends at 48, and the products themselves (about 1,900 cycles an SM each, where their exponentials take 1,000).  8 sequences of
+// one token over 2000 slots: 8 us of kernel for 29 MB.  The exponential is the hardware's approximation (2 ulp) of an argument
+// made by one fp32 multiply-add: a weight is off by 5e-7 of itself where an fp32 exponential makes 1e-7.
 //
 // One operand stays, the other streams.  MANY = false (one row tile covers every sequence's drafts): the queries stay and a CTA
 // goes over `span` slot tiles.  MANY = true: a slot tile stays and the row tiles stream.  Every row sees the cached slots,
