@@ -311,7 +311,7 @@ def _norm_rope_append(st):
 
 
 # The cache in 4 bits.  32 neighbouring channels of a slot share a scale, a number of five exponent and three fraction bits:
-# the largest magnitude over 7, at most 8192, to fp16 and then to the nearest of them (ties to even); a channel is its
+# the largest magnitude over 7, at most 2048, to fp16 and then to the nearest of them (ties to even); a channel is its
 # nearest whole multiple of it, -7 to 7.  A group with a value that is not finite has the scale NaN.
 # A page of a head is laid out by eights of slots, 8 * D / 2 bytes of codes and 8 * D / 32 bytes of scales each.  A code c is
 # held as c + 8; eight channels share a little-endian word with channel 2 i in bits 4 i and channel 2 i + 1 in bits 16 + 4 i.
@@ -322,7 +322,7 @@ def _quantise(x):
     """(whole multiples, scales' bytes) of [..., D] in groups of 32 channels: float [..., D / 32, 32] and int [..., D / 32]."""
     x = x.float().unflatten(-1, (-1, 32))
     top = x.abs().amax(-1)
-    h = torch.clamp(top / 7.0, max=8192.0).half().view(torch.int16).int()
+    h = torch.clamp(top / 7.0, max=2048.0).half().view(torch.int16).int()
     byte = torch.where(torch.isfinite(top), (h + 63 + ((h >> 7) & 1)) >> 7, 255)
     s = _scale(byte)[..., None]
     return torch.where(s > 0, torch.round(x / torch.where(s > 0, s, 1.0)), 0.0).clamp(-7, 7), byte
@@ -503,7 +503,7 @@ def _numbers():
 def _in_four_bits(x):
     """x [..., D] as the cache holds it."""
     x = x.double().unflatten(-1, (-1, 32))
-    a = (x.abs().amax(-1) / 7.0).clamp(max=8192.0)
+    a = (x.abs().amax(-1) / 7.0).clamp(max=2048.0)
     scales = _numbers().cuda()
     up = torch.searchsorted(scales, a).clamp(1, 254)
     low, high = scales[up - 1], scales[up]
