@@ -503,7 +503,7 @@ def _numbers():
 def _in_four_bits(x):
     """x [..., D] as the cache holds it."""
     x = x.double().unflatten(-1, (-1, 32))
-    a = (x.abs().amax(-1) / 7.0).clamp(max=2048.0)
+    a = (x.abs().amax(-1) / 7.0).clamp(max=2048.0).half().double()
     scales = _numbers().cuda()
     up = torch.searchsorted(scales, a).clamp(1, 254)
     low, high = scales[up - 1], scales[up]
