@@ -370,6 +370,10 @@ int atts_calib_update_static(float* calib, int64_t n, int64_t cap, const float* 
  *   atts_tree_attention  attends from every drafted token to the cache and to its own ancestors among the drafts
  *   atts_cache_weights   adds up what attention every cached slot received
  *   atts_cache_select, atts_cache_gather   keep the slots that received most and move them to other pages
+ * Beside them, for other target models and tighter memory:
+ *   atts_norm_rope_append, atts_norm_rope  the same rotation behind a norm of every query and key head
+ *   atts_window_attention                  attention through a sliding window with sinks
+ *   atts_packed_append, atts_packed_read, atts_packed_attention   a cache that holds keys and values in 4 bits
  *
  * The batch.  num_seqs sequences; sequence b holds ctx_lens[b] cached tokens and drafts cu_tokens[b+1] - cu_tokens[b]
  * further ones, rows cu_tokens[b] .. of the [M, heads, head_dim] arrays.  Slot s of sequence b is entry s % page_size of
@@ -504,6 +508,104 @@ int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kep
                       void* cuda_stream);
 
 /*
+ * Norms of queries and keys for each head with the rotation in the same pass.  A row x of head_dim channels becomes
+ *   y = x / sqrt(mean(x^2) + eps) * gain   (channel by channel, in fp32),
+ * then pairs of y are turned as in atts_rope_append, and the row is rounded once.
+ *   q_gain, k_gain  dev  [head_dim] in the rows' type, shared by the heads; NULL: that side is only rotated
+ *   eps             finite, >= 0 (a row of zeros with eps = 0 gives NaN)
+ * atts_norm_rope_append: everything else as atts_rope_append.  Mean squares are taken in fp32: magnitudes up to 1e18.
+ * atts_norm_rope: rows to rows, no cache (what atts_packed_append takes): q [M, Hq, head_dim] into q_out, k [M, Hk, head_dim]
+ * into k_out; either may be written in place (same strides).  Hq or Hk may be 0, its pointers then NULL.  dtype ATTS_BF16 or
+ * ATTS_FP16; head_dim a multiple of 8, <= 256.
+ */
+int atts_norm_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                          int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                          const int32_t* positions, const double* freqs, int32_t rotary_pairs, float mscale,
+                          int32_t interleaved, const void* q_gain, const void* k_gain, float eps, const atts_kv_cache* cache,
+                          const int32_t* ctx_lens, const int32_t* cu_tokens, int64_t M, int32_t Hq, int64_t max_tokens,
+                          void* q_out, int64_t out_token_stride, int64_t out_head_stride, void* cuda_stream);
+int atts_norm_rope(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                   int64_t k_head_stride, const int32_t* positions, const double* freqs, int32_t rotary_pairs, float mscale,
+                   int32_t interleaved, const void* q_gain, const void* k_gain, float eps, int32_t dtype, int64_t M, int32_t Hq,
+                   int32_t Hk, int32_t head_dim, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                   void* k_out, int64_t k_out_token_stride, int64_t k_out_head_stride, void* cuda_stream);
+
+/*
+ * Attention through a sliding window with sinks.  Every item has a place on its line: cached slot s of a sequence the place
+ * s, drafted token j the place ctx_lens[b] + depth[j].  Of what atts_tree_attention shows token i, it sees the items x with
+ *   place(i) - place(x) < window   or   place(x) < sinks
+ * (window counts the token itself: 1 shows it alone, and the sinks).
+ *   depth         dev  [M] int32 (atts_tree_plan), needed with pre and end; NULL with them: chains, whose depths are known.  A
+ *                      value outside [0, drafted tokens) counts as the nearest inside; where a token's depth is not its
+ *                      number of ancestors, the outputs of its sequence are undefined
+ *   window        1 <= window <= 2^30;  sinks  0 <= sinks <= 2^30
+ * Everything else as atts_tree_attention; the workspace is asked for with the same window and sinks.  What lies behind the
+ * window costs nothing, and a page none of whose slots any drafted token of the sequence sees need not be there any more (its
+ * table entry may be -1).
+ */
+int atts_window_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,
+                                          int64_t max_tokens, int64_t max_len, int64_t window, int64_t sinks, size_t* bytes);
+int atts_window_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
+                          const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre, const int32_t* end,
+                          const int32_t* depth, int64_t window, int64_t sinks, int64_t M, int32_t Hq, int64_t max_tokens,
+                          int64_t max_len, float scale, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * A paged cache in 4 bits.  32 neighbouring channels of a slot share a scale s; a channel is c * s with a whole c, -7 .. 7.
+ *   s: the group's largest magnitude over 7, at most 2048, rounded to fp16 and then to three fraction bits (to nearest, ties
+ *      to even); held as the byte of its five exponent and three fraction bits: byte << 7 is s in fp16 (208 the largest).  A group that has a
+ *      NaN or an infinity gets the byte 255, which is NaN and makes every channel of the group one.
+ *   c: x / s to the nearest whole number, ties to even, cut to -7 .. 7 (0 where s is 0: magnitudes below 7 * 2^-18).
+ * Values up to 14,336 are held to half a scale; 4.25 bits a channel.  c * s is exact in bf16 and fp16.
+ * A page of a head is a contiguous block of page_size / 8 * 4.25 * head_dim bytes (page_size / 8 pieces of
+ * 4 * head_dim bytes of codes of eight slots, then head_dim / 4 bytes of their scales).  A slot has head_dim / 2 bytes of codes:
+ * eight channels to a little-endian word, c + 8 of channel 2 i in bits 4 i .. and of channel 2 i + 1 in bits 16 + 4 i ..
+ */
+typedef struct {
+  void* k;                    /* dev, 16-byte aligned: block of (page p, head h) at k + p * page_stride + h * head_stride */
+  void* v;                    /*   bytes; v likewise                                                                      */
+  const int32_t* block_table; /* dev [num_seqs][table_stride], the first table_cols columns used                          */
+  int64_t num_seqs, table_cols, table_stride;
+  int64_t num_pages, page_size;       /* page_size a power of two, 8 .. 4096                                              */
+  int64_t page_stride, head_stride;   /* bytes, multiples of 16, at least a block where there is more than one            */
+  int32_t heads, head_dim;            /* head_dim 64, 128, 192 or 256                                                     */
+} atts_packed_cache;
+
+/*
+ * Append: keys and values of the drafted tokens, rows [M, heads, head_dim] (rotated already), into their slots.  Rows of any
+ * alignment (16-byte aligned ones take the wide path); dtype ATTS_BF16 or ATTS_FP16 is the rows'.  Other arguments as
+ * atts_rope_append.  The result is the format above to the bit, whatever the batch.
+ */
+int atts_packed_append(const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                       int64_t v_head_stride, int32_t dtype, const atts_packed_cache* cache, const int32_t* ctx_lens,
+                       const int32_t* cu_tokens, int64_t M, int64_t max_tokens, void* cuda_stream);
+
+/*
+ * Reads back: slot s < lens[b] of every sequence, as the values it stands for, into the same slot of the 16-bit cache `dst` (its
+ * own pages and table; num_seqs, heads and head_dim as src): for calls that read 16 bits (atts_cache_weights, an eviction).
+ *   lens          dev  [num_seqs] int32, 0 <= lens[b] <= max_len (else ATTS_DEV_SEQ_RANGE, cut);  max_len  host bound
+ * A slot whose page is missing in src or dst is skipped and ATTS_DEV_PAGE_RANGE recorded.
+ */
+int atts_packed_read(const atts_packed_cache* src, const int32_t* lens, int64_t max_len, const atts_kv_cache* dst,
+                     void* cuda_stream);
+
+/*
+ * Attention over a packed cache: atts_window_attention, or with window = 0 (then depth may be NULL and sinks mean nothing)
+ * atts_tree_attention, on the values that the cache stands for; q and out of type dtype, head_dim 64 or 128.  Those values go to
+ * the tensor cores exactly, so the arithmetic behind them is that of the calls over 16 bits.  A missing page's slots
+ * read as zeros; a NaN group makes out and lse of the rows that see its key NaN, and out of all rows of its head that see its value's
+ * tile (a masked product is 0 * v, as with 16 bits).
+ */
+int atts_packed_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,
+                                          int64_t max_tokens, int64_t max_len, int64_t window, int64_t sinks, size_t* bytes);
+int atts_packed_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t dtype,
+                          const atts_packed_cache* cache, const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre,
+                          const int32_t* end, const int32_t* depth, int64_t window, int64_t sinks, int64_t M, int32_t Hq,
+                          int64_t max_tokens, int64_t max_len, float scale, void* out, int64_t out_token_stride,
+                          int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Waits for `cuda_stream`, then returns in *bits (host out) the OR of the ATTS_DEV_* conditions
  * device code has recorded on the current device since the last call, and clears them.  Returns
  * ATTS_ERR_TIMEOUT if ATTS_DEV_WAIT_EXPIRED is among them, else ATTS_ERR_INDEX if ATTS_DEV_INDEX_STALE is,
@@ -525,7 +627,7 @@ int atts_debug_score_unit(int64_t M, int64_t d, int64_t V, int32_t workers, int3
 
 /*
  * Bounded waits (diagnostic; the paper has no counterpart).  Every wait inside the kernels of atts_score_logprob,
- * atts_tree_attention and atts_cache_weights (for a shared-memory stage to fill or drain, for an accumulator to complete or be
+ * atts_tree_attention (and its windowed and packed kin) and atts_cache_weights (for a shared-memory stage to fill or drain, for an accumulator to complete or be
  * read) gives up after a number of SM cycles; the kernel then stops, lets copies in flight land, frees its tensor
  * memory and returns, ATTS_DEV_WAIT_EXPIRED is recorded and atts_last_device_status returns ATTS_ERR_TIMEOUT.  The
  * outputs of such a call are invalid; the context stays usable.

@@ -24,6 +24,8 @@ EXPORTS = (
     "atts_takeover_ids_workspace_bytes", "atts_takeover_ids", "atts_debug_set_wait", "atts_debug_score_form",
     "atts_tree_plan", "atts_rope_append", "atts_tree_attention_workspace_bytes", "atts_tree_attention",
     "atts_cache_weights", "atts_cache_select", "atts_cache_gather",
+    "atts_norm_rope_append", "atts_norm_rope", "atts_window_attention_workspace_bytes", "atts_window_attention",
+    "atts_packed_append", "atts_packed_read", "atts_packed_attention_workspace_bytes", "atts_packed_attention",
 )
 
 STAGE_DRAFT, STAGE_ACCEPTED, STAGE_TARGET = 1, 2, 3
@@ -104,6 +106,17 @@ def load(rebuild_if_stale: bool = True) -> ctypes.CDLL:
     lib.atts_cache_select.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_int64, c_int64, c_int64, c_void_p,
                                       c_void_p, c_void_p]
     lib.atts_cache_gather.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
+    turned = [c_void_p, c_void_p, c_int32, c_float, c_int32, c_void_p, c_void_p, c_float]
+    lib.atts_norm_rope_append.argtypes = rows * 3 + turned + [c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int64] + rows + [c_void_p]
+    lib.atts_norm_rope.argtypes = rows * 2 + turned + [c_int32, c_int64, c_int32, c_int32, c_int32] + rows * 2 + [c_void_p]
+    for name in ("window", "packed"):
+        getattr(lib, f"atts_{name}_attention_workspace_bytes").argtypes = [c_int64, c_int64, c_int32, c_int32, c_int32] + [c_int64] * 4 + [
+            POINTER(c_size_t)]
+    tail = [c_void_p] * 6 + [c_int64, c_int64, c_int64, c_int32, c_int64, c_int64, c_float] + rows + [c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.atts_window_attention.argtypes = rows + tail
+    lib.atts_packed_attention.argtypes = rows + [c_int32] + tail
+    lib.atts_packed_append.argtypes = rows * 2 + [c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_void_p]
+    lib.atts_packed_read.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
     lib.atts_profile_begin.argtypes = [c_int]
     lib.atts_profile_end.argtypes = [POINTER(ctypes.c_float), c_int, POINTER(c_int)]
     for name in EXPORTS[2:]:
@@ -409,10 +422,53 @@ class PagedCache:
         self._ref = ctypes.addressof(self._c)
 
 
-def _rows(t, name: str, M: int, heads: int, cache: PagedCache):
-    """(pointer, token stride, head stride) of a [M, heads, head_dim] tensor of the cache's type."""
-    if t.shape != (M, heads, cache.head_dim) or t.dtype is not cache.dtype or t.device != cache.device:
-        raise ValueError(f"{name}: has to be [{M}, {heads}, {cache.head_dim}], {cache.dtype}, on {cache.device} like the cache; got "
+class _PackedCache(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("block_table", c_void_p), ("num_seqs", c_int64), ("table_cols", c_int64),
+                ("table_stride", c_int64), ("num_pages", c_int64), ("page_size", c_int64), ("page_stride", c_int64),
+                ("head_stride", c_int64), ("heads", c_int32), ("head_dim", c_int32)]
+
+
+def packed_block_bytes(page_size: int, head_dim: int) -> int:
+    """Bytes of a page of one head in a packed cache: codes of 4 bits and a scale's byte for every 32 channels."""
+    return page_size * (head_dim // 2 + head_dim // 32)
+
+
+class PackedCache:
+    """Description of a paged key/value cache in 4 bits, made once and passed to every call (it holds pointers, not contents).
+
+    k, v: uint8 [num_pages, heads, packed_block_bytes(page_size, head_dim)] (any strides that are multiples of 16 bytes, the same
+    for both; blocks contiguous); block_table: int32 [num_seqs, pages]; head_dim 64, 128, 192 or 256."""
+
+    def __init__(self, k, v, block_table, page_size: int, head_dim: int):
+        import torch
+        if page_size < 8 or page_size > 4096 or page_size & (page_size - 1) or head_dim not in (64, 128, 192, 256):
+            raise ValueError("page_size has to be a power of two from 8 to 4096, head_dim 64, 128, 192 or 256")
+        block = packed_block_bytes(page_size, head_dim)
+        if k.dtype != torch.uint8 or v.dtype != torch.uint8:
+            raise ValueError("k and v have to be uint8")
+        if k.dim() != 3 or k.shape[2] != block or k.shape != v.shape or k.stride() != v.stride() or (k.numel() and k.stride(2) != 1):
+            raise ValueError(f"k and v: [num_pages, heads, {block}] with equal strides, blocks contiguous")
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+            raise ValueError("block_table: int32 [num_seqs, pages], rows contiguous")
+        if not (k.is_cuda and v.device == k.device and block_table.device == k.device):
+            raise ValueError("k, v and block_table have to be on one CUDA device")
+        self.k, self.v, self.block_table = k, v, block_table
+        self.page_size, self.head_dim = page_size, head_dim
+        self.num_pages, self.heads = k.shape[0], k.shape[1]
+        self.num_seqs, self.device = block_table.shape[0], k.device
+        # a dimension of one entry has a stride that means nothing
+        ps, hs = (k.stride(i) if k.shape[i] > 1 else block for i in range(2))
+        self._c = _PackedCache(_ptr(k), _ptr(v), _ptr(block_table), self.num_seqs, block_table.shape[1],
+                               block_table.stride(0) if self.num_seqs > 1 else block_table.shape[1], self.num_pages,
+                               page_size, ps, hs, self.heads, head_dim)
+        self._ref = ctypes.addressof(self._c)
+
+
+def _rows(t, name: str, M: int, heads: int, cache, dtype=None):
+    """(pointer, token stride, head stride) of a [M, heads, head_dim] tensor of the cache's type (of `dtype`, if given)."""
+    want = cache.dtype if dtype is None else dtype
+    if t.shape != (M, heads, cache.head_dim) or t.dtype is not want or t.device != cache.device:
+        raise ValueError(f"{name}: has to be [{M}, {heads}, {cache.head_dim}], {want}, on {cache.device} like the cache; got "
                          f"{list(t.shape)}, {t.dtype}, on {t.device}")
     token, head, channel = t.stride()
     if channel != 1 and t.numel():
@@ -570,3 +626,123 @@ def cache_gather(src: PagedCache, kept, counts, dst: PagedCache, weights_in=None
                                     None if weights_in is None else _vec(weights_in, "weights_in", torch.float32, src.num_seqs * src.heads * in_cols, dev),
                                     in_cols, None if weights_out is None else _vec(weights_out, "weights_out", torch.float32, n, dev),
                                     _stream_on(dev)), "atts_cache_gather")
+
+
+def _dtype_code(t, name: str) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return 0
+    if t.dtype is torch.float16:
+        return 1
+    raise ValueError(f"{name}: has to be bfloat16 or float16, not {t.dtype}")
+
+
+def norm_rope_append(q, k, v, positions, freqs, q_gain, k_gain, eps: float, cache: PagedCache, ctx_lens, cu_tokens, max_tokens: int, q_out,
+                     interleaved: bool = False, mscale: float = 1.0) -> None:
+    """:func:`rope_append` behind a norm of every head of q and k: x / sqrt(mean(x^2) + eps) * gain, then the rotation. q_gain and
+    k_gain [head_dim] of the cache's type (None: that side is only rotated)."""
+    import torch
+    M, dev, B, D = k.shape[0], cache.device, cache.num_seqs, cache.head_dim
+    kr, vr = _rows(k, "k", M, cache.heads, cache), _rows(v, "v", M, cache.heads, cache)
+    Hq = 0 if q is None else q.shape[1]
+    qr, outr = ((0, 0, 0), (0, 0, 0)) if q is None else (_rows(q, "q", M, Hq, cache), _rows(q_out, "q_out", M, Hq, cache))
+    n = freqs.numel()
+    _check(load().atts_norm_rope_append(*qr, *kr, *vr, _vec(positions, "positions", torch.int32, M, dev),
+                                        _vec(freqs, "freqs", torch.float64, n, dev), n, mscale, 1 if interleaved else 0,
+                                        None if q_gain is None else _vec(q_gain, "q_gain", cache.dtype, D, dev),
+                                        None if k_gain is None else _vec(k_gain, "k_gain", cache.dtype, D, dev), eps, cache._ref,
+                                        _vec(ctx_lens, "ctx_lens", torch.int32, B, dev),
+                                        _vec(cu_tokens, "cu_tokens", torch.int32, B + 1, dev), M, Hq, max_tokens, *outr, _stream_on(dev)),
+           "atts_norm_rope_append")
+
+
+def norm_rope(q, k, positions, freqs, q_gain, k_gain, eps: float, q_out, k_out, interleaved: bool = False, mscale: float = 1.0) -> None:
+    """The same from rows to rows: q [M, Hq, D] into q_out, k [M, Hk, D] into k_out (each may be written in place; q and q_out, or k
+    and k_out, may be None): what :func:`packed_append` takes."""
+    import torch
+    one = k if q is None else q
+    if one is None:
+        raise ValueError("q or k has to be given")
+    M, _, D = one.shape
+    dev, code = one.device, _dtype_code(one, "q" if q is not None else "k")
+
+    class Like:
+        head_dim, dtype, device = D, one.dtype, dev
+    Hq, Hk = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+    none = (0, 0, 0)
+    qr, qo = (none, none) if q is None else (_rows(q, "q", M, Hq, Like), _rows(q_out, "q_out", M, Hq, Like))
+    kr, ko = (none, none) if k is None else (_rows(k, "k", M, Hk, Like), _rows(k_out, "k_out", M, Hk, Like))
+    n = freqs.numel()
+    _check(load().atts_norm_rope(*qr, *kr, _vec(positions, "positions", torch.int32, M, dev), _vec(freqs, "freqs", torch.float64, n, dev), n,
+                                 mscale, 1 if interleaved else 0, None if q_gain is None else _vec(q_gain, "q_gain", one.dtype, D, dev),
+                                 None if k_gain is None else _vec(k_gain, "k_gain", one.dtype, D, dev), eps, code, M, Hq, Hk, D, *qo, *ko,
+                                 _stream_on(dev)), "atts_norm_rope")
+
+
+def window_attention_workspace_bytes(num_seqs: int, M: int, Hq: int, heads: int, head_dim: int, max_tokens: int, max_len: int, window: int,
+                                     sinks: int) -> int:
+    """Bytes that window_attention needs for these sizes. Ask for every batch: a smaller one may need more (more chunks)."""
+    out = c_size_t(0)
+    _check(load().atts_window_attention_workspace_bytes(num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, window, sinks, ctypes.byref(out)),
+           "atts_window_attention_workspace_bytes")
+    return out.value
+
+
+def packed_attention_workspace_bytes(num_seqs: int, M: int, Hq: int, heads: int, head_dim: int, max_tokens: int, max_len: int, window: int = 0,
+                                     sinks: int = 0) -> int:
+    """Bytes that packed_attention needs for these sizes. Ask for every batch: a smaller one may need more (more chunks)."""
+    out = c_size_t(0)
+    _check(load().atts_packed_attention_workspace_bytes(num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, window, sinks, ctypes.byref(out)),
+           "atts_packed_attention_workspace_bytes")
+    return out.value
+
+
+def _attention_tail(q, cache, dtype, ctx_lens, cu_tokens, pre, end, depth, window, sinks, max_tokens, max_len, scale, out, lse, workspace):
+    """Arguments of the windowed calls from the sequences' lengths on."""
+    import torch
+    M, Hq = q.shape[0], q.shape[1]
+    dev, B, i32 = cache.device, cache.num_seqs, torch.int32
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: has to be contiguous, on {dev}")
+    tree = (None if t is None else _vec(t, name, i32, M, dev) for t, name in ((pre, "pre"), (end, "end"), (depth, "depth")))
+    return (_vec(ctx_lens, "ctx_lens", i32, B, dev), _vec(cu_tokens, "cu_tokens", i32, B + 1, dev), *tree, window, sinks, M, Hq, max_tokens,
+            max_len, scale, *_rows(out, "out", M, Hq, cache, dtype), None if lse is None else _vec(lse, "lse", torch.float32, M * Hq, dev),
+            _ptr(workspace), _nbytes(workspace), _stream_on(dev))
+
+
+def window_attention(q, cache: PagedCache, ctx_lens, cu_tokens, pre, end, depth, window: int, sinks: int, max_tokens: int, max_len: int,
+                     scale: float, out, lse, workspace) -> None:
+    """:func:`tree_attention` through a window: of its line a token sees the last `window` places, its own among them, and the first
+    `sinks`. pre, end, depth int32 [M] (:func:`tree_plan`), all None: chains."""
+    _check(load().atts_window_attention(*_rows(q, "q", q.shape[0], q.shape[1], cache), cache._ref,
+                                        *_attention_tail(q, cache, cache.dtype, ctx_lens, cu_tokens, pre, end, depth, window, sinks, max_tokens,
+                                                         max_len, scale, out, lse, workspace)), "atts_window_attention")
+
+
+def packed_append(k, v, cache: PackedCache, ctx_lens, cu_tokens, max_tokens: int) -> None:
+    """Keys and values [M, heads, D] (bf16 or fp16, rotated already) into the packed cache's slots ctx_lens[b] + t."""
+    import torch
+    M, dev, B = k.shape[0], cache.device, cache.num_seqs
+    code = _dtype_code(k, "k")
+    _check(load().atts_packed_append(*_rows(k, "k", M, cache.heads, cache, k.dtype), *_rows(v, "v", M, cache.heads, cache, k.dtype), code, cache._ref,
+                                     _vec(ctx_lens, "ctx_lens", torch.int32, B, dev), _vec(cu_tokens, "cu_tokens", torch.int32, B + 1, dev), M,
+                                     max_tokens, _stream_on(dev)), "atts_packed_append")
+
+
+def packed_read(src: PackedCache, lens, max_len: int, dst: PagedCache) -> None:
+    """Slots below lens[b] of every sequence, as the values they stand for, into the same slots of the 16-bit cache dst."""
+    import torch
+    dev = src.device
+    if dst.device != dev:
+        raise ValueError(f"dst: has to be on {dev} like src, not on {dst.device}")
+    _check(load().atts_packed_read(src._ref, _vec(lens, "lens", torch.int32, src.num_seqs, dev), max_len, dst._ref, _stream_on(dev)), "atts_packed_read")
+
+
+def packed_attention(q, cache: PackedCache, ctx_lens, cu_tokens, pre, end, depth, window: int, sinks: int, max_tokens: int, max_len: int,
+                     scale: float, out, lse, workspace) -> None:
+    """Attention of q [M, Hq, D] (bf16 or fp16, out alike) over a packed cache: :func:`window_attention`, or with window 0 (depth may be
+    None) :func:`tree_attention`, on the values that it stands for."""
+    code = _dtype_code(q, "q")
+    _check(load().atts_packed_attention(*_rows(q, "q", q.shape[0], q.shape[1], cache, q.dtype), code, cache._ref,
+                                        *_attention_tail(q, cache, q.dtype, ctx_lens, cu_tokens, pre, end, depth, window, sinks, max_tokens,
+                                                         max_len, scale, out, lse, workspace)), "atts_packed_attention")

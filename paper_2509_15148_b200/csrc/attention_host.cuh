@@ -1,6 +1,8 @@
 // C-ABI entry points of the attention side (declared in include/atts.h): argument checks and launch geometry.
 // Included by atts.cu behind its own helpers.
 #pragma once
+#include "norm_rope.cuh"
+#include "packed_cache.cuh"
 #include "rope_cache.cuh"
 #include "tree_attention.cuh"
 
@@ -41,7 +43,37 @@ static int cache_view(const atts_kv_cache* c, CacheView* out) {
   return ATTS_OK;
 }
 
-// Checks shared by the two calls that read the cache against queries.
+// The same for a packed cache: strides in bytes, no slot stride.
+static int packed_view(const atts_packed_cache* c, CacheView* out) {
+  if (!c) return ATTS_ERR_NULL;
+  if (c->num_seqs < 0 || c->num_seqs > 65535 || c->heads < 1 || c->heads > 1024) return ATTS_ERR_SHAPE;
+  if (c->head_dim < 64 || c->head_dim > 256 || c->head_dim % 64 != 0) return ATTS_ERR_SHAPE;
+  if (c->page_size < 8 || c->page_size > 4096 || (c->page_size & (c->page_size - 1)) != 0) return ATTS_ERR_SHAPE;
+  if (c->num_pages < 0 || c->num_pages > 0x7FFFFFFF || c->table_cols < 0 || c->table_cols > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  if (c->table_stride < c->table_cols && c->num_seqs > 1) return ATTS_ERR_SHAPE;
+  const int64_t block = c->page_size / 8 * packed_eight(c->head_dim);
+  if (c->page_stride < 0 || c->head_stride < 0 || c->page_stride % 16 || c->head_stride % 16 ||
+      (c->num_pages > 1 && c->page_stride < block) || (c->heads > 1 && c->head_stride < block))
+    return ATTS_ERR_SHAPE;
+  if ((c->num_pages > 0 && (!c->k || !c->v)) || (c->num_seqs > 0 && c->table_cols > 0 && !c->block_table)) return ATTS_ERR_NULL;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->block_table, 4)) return ATTS_ERR_ALIGN;
+  out->k = static_cast<char*>(c->k);
+  out->v = static_cast<char*>(c->v);
+  out->table = c->block_table;
+  out->table_stride = c->table_stride;
+  out->page_stride = c->page_stride;
+  out->slot_stride = 0;
+  out->head_stride = c->head_stride;
+  out->table_cols = (int32_t)c->table_cols;
+  out->num_pages = (int32_t)c->num_pages;
+  out->heads = c->heads;
+  int lg = 0;
+  while ((1ll << lg) < c->page_size) ++lg;
+  out->page_log2 = lg;
+  return ATTS_OK;
+}
+
+// Checks shared by the calls that read a cache against queries.
 static int check_queries(const void* q, int64_t q_ts, int64_t q_hs, const atts_kv_cache* c, const int32_t* ctx,
                          const int32_t* cu, const int32_t* pre, const int32_t* end, int64_t M, int32_t Hq,
                          int64_t max_tokens, int64_t max_len, float scale) {
@@ -99,18 +131,26 @@ static int row_tile_tokens(int G, int64_t max_tokens) {
 // sequence has more than one.  Chunks: the number that makes the launch shortest by these measured times (us): a CTA's
 // start and end 9, a slot tile 1.2 (2.0 for two row tiles), a chunk's sums one per 45 KB of them, the second launch 3.
 // One row tile and more CTAs than SMs: kRowsBrief if its 8 + 3.5 a tile, two CTAs an SM, come out below that.
+// A window leaves a row tile with the tiles of the sinks, of the window before its tokens, and of the drafts, two of them cut;
+// a packed cache's tiles take as long as its codes take to expand and has no kRowsBrief (its raw tiles leave no room for two CTAs).
 struct AttnShape {
   AttnMode mode;
   AttnPlan p;
 };
-static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens, int64_t max_len) {
+constexpr int64_t kEndless = 0x7FFFFFFF;   // a window that leaves nothing out
+static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens, int64_t max_len,
+                            AttnForm form = kFormPlain, int64_t window = kEndless, int64_t sinks = 0) {
   AttnShape r{};
   const int G = Hq / heads;
   r.p.tpt = row_tile_tokens(G, max_tokens);
   r.mode = max_tokens > r.p.tpt ? kRowsTwo : kRowsOne;
   const int64_t per = r.p.tpt * (r.mode == kRowsTwo ? 2 : 1);
   r.p.nq = (int)((max_tokens + per - 1) / per);
-  const int64_t tiles = (max_len + kAttnTile - 1) / kAttnTile;
+  int64_t tiles = (max_len + kAttnTile - 1) / kAttnTile;
+  if (form != kFormPlain) {
+    const int64_t seen = (max_tokens + window + kAttnTile - 1) / kAttnTile + 2 + (sinks + kAttnTile - 1) / kAttnTile;
+    if (seen < tiles) tiles = seen;
+  }
   const int64_t base = num_seqs * heads * r.p.nq;
   const double tile = r.mode == kRowsTwo ? 2.0 : 1.2;
   const double part = (double)((max_tokens < per ? max_tokens : per) * G) * head_dim * 8 / (45 * 1024);
@@ -125,7 +165,7 @@ static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads
       best_n = n;
     }
   }
-  if (r.mode == kRowsOne && base > sms && (double)((base + 2 * sms - 1) / (2 * sms)) * (8.0 + 3.5 * (double)tiles) < best) {
+  if (form != kFormPacked && r.mode == kRowsOne && base > sms && (double)((base + 2 * sms - 1) / (2 * sms)) * (8.0 + 3.5 * (double)tiles) < best) {
     r.mode = kRowsBrief;
     best_n = 1;
   }
@@ -139,13 +179,82 @@ static size_t attn_workspace(const AttnShape& s, int64_t M, int32_t Hq, int32_t 
   return round_up(rows * 4, 256) + round_up(rows * head_dim * 4, 256);
 }
 
-template <typename T, int D, AttnMode MODE>
+template <typename T, int D, AttnMode MODE, AttnForm FORM>
 static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, const AttnPlan& p,
                             dim3 grid, unsigned* status, cudaStream_t stream) {
-  int st = launch_pdl(tree_attention_kernel<T, D, MODE>, grid, dim3(AttnCfg<D, MODE>::kThreads), AttnCfg<D, MODE>::kSmemBytes, stream, mq, mk, mv, a, p, status);
+  using Cfg = AttnCfg<D, MODE, FORM>;
+  int st = launch_pdl(tree_attention_kernel<T, D, MODE, FORM>, grid, dim3(Cfg::kThreads), Cfg::kSmemBytes, stream, mq, mk, mv, a, p, status);
   if (st != ATTS_OK || p.chunks <= 1) return st;
   const int64_t rows = (int64_t)a.max_tokens * a.Hq;
-  return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
+  return launch_pdl(attention_join_kernel<T, D, FORM != kFormPlain>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
+}
+
+// An attention call, its cache and queries checked (a.cache is filled): the remaining checks, the cut of the work, the launches.
+// `c` describes the cache for the tensor maps (of a packed one only type and sizes are used).
+template <AttnForm FORM>
+static int attend(AttnArgs& a, const atts_kv_cache* c, const void* q, int64_t q_ts, int64_t q_hs, const int32_t* ctx, const int32_t* cu,
+                  const int32_t* pre, const int32_t* end, const int32_t* depth, int64_t window, int64_t sinks, int64_t M, int32_t Hq,
+                  int64_t max_tokens, int64_t max_len, float scale, void* out, int64_t o_ts, int64_t o_hs, float* lse, void* workspace,
+                  size_t workspace_bytes, void* cuda_stream) {
+  if (o_ts < 0 || o_hs < 0 || o_ts % 8 || o_hs % 8) return ATTS_ERR_SHAPE;
+  if ((M > 0 && !out) || !workspace) return ATTS_ERR_NULL;
+  if (!aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, 256)) return ATTS_ERR_ALIGN;
+  const DeviceInfo* di;
+  const int st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  AttnShape sh = attn_shape(di->sm_count, c->num_seqs, Hq, c->heads, c->head_dim, max_tokens, max_len, FORM, window, sinks);
+  if (workspace_bytes < attn_workspace(sh, M, Hq, c->head_dim)) return ATTS_ERR_WORKSPACE;
+  if (M == 0 || c->num_seqs == 0 || max_tokens == 0) return ATTS_OK;
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.q_ts = q_ts; a.q_hs = q_hs; a.o_ts = o_ts; a.o_hs = o_hs;
+  a.ctx = ctx; a.cu = cu; a.pre = pre; a.end = end;
+  a.depth = depth; a.window = (int)window; a.sinks = (int)sinks;
+  a.M = (int)M; a.Hq = Hq; a.G = Hq / c->heads; a.max_tokens = (int)max_tokens; a.max_len = (int)max_len;
+  a.scale = scale;
+  sh.p.part_lse = static_cast<float*>(workspace);
+  sh.p.part_o = sh.p.part_lse + round_up((size_t)M * Hq * sh.p.chunks * 4, 256) / 4;
+  sh.p.wait_limit = wait_limit();
+  sh.p.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
+  const int64_t gx = (int64_t)sh.p.nq * sh.p.chunks;
+  if (gx > 0x7FFFFFFF || (int64_t)max_tokens * Hq > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
+  CUtensorMap mq, mk, mv;
+  if (encode_queries(di, &mq, c, q, q_ts, q_hs, M, Hq, sh.p.tpt) != ATTS_OK) return ATTS_ERR_CUDA;
+  if (FORM == kFormPacked) mk = mv = mq;   // not used
+  else if (encode_cache(di, &mk, c, c->k) != ATTS_OK || encode_cache(di, &mv, c, c->v) != ATTS_OK) return ATTS_ERR_CUDA;
+  const dim3 grid((unsigned)gx, (unsigned)c->heads, (unsigned)c->num_seqs);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const bool bf = c->dtype == ATTS_BF16;
+#define ATTS_ATTEND(D, MODE)                                                                                      \
+  (bf ? launch_attention<__nv_bfloat16, D, MODE, FORM>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream)         \
+      : launch_attention<__half, D, MODE, FORM>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream))
+  if (sh.mode == kRowsTwo) return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsTwo) : ATTS_ATTEND(64, kRowsTwo);
+  if constexpr (FORM != kFormPacked)
+    if (sh.mode == kRowsBrief) return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsBrief) : ATTS_ATTEND(64, kRowsBrief);
+  return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsOne) : ATTS_ATTEND(64, kRowsOne);
+#undef ATTS_ATTEND
+}
+
+// Arguments of a window: 1 .. 2^30 tokens (or 0, where that means none), 0 .. 2^30 sinks; trees bring their depths.
+static int check_window(int64_t window, int64_t sinks, bool may_be_none, const int32_t* pre, const int32_t* depth) {
+  if (window < (may_be_none ? 0 : 1) || window > kMaxSlots || sinks < 0 || sinks > kMaxSlots) return ATTS_ERR_ARG;
+  if (window > 0 && (pre != nullptr) != (depth != nullptr)) return ATTS_ERR_NULL;
+  if (!aligned(depth, 4)) return ATTS_ERR_ALIGN;
+  return ATTS_OK;
+}
+
+static int attention_workspace(AttnForm form, int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens,
+                               int64_t max_len, int64_t window, int64_t sinks, size_t* bytes) {
+  if (!bytes) return ATTS_ERR_NULL;
+  if (num_seqs < 0 || num_seqs > 65535 || M < 0 || M > (1ll << 30) || heads < 1 || heads > 1024 || Hq < 1 || Hq % heads != 0 ||
+      Hq / heads > 128 || (head_dim != 64 && head_dim != 128) || max_tokens < 0 || max_len < max_tokens || max_len > kMaxSlots)
+    return ATTS_ERR_SHAPE;
+  const DeviceInfo* di;
+  const int st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  *bytes = attn_workspace(attn_shape(di->sm_count, num_seqs, Hq, heads, head_dim, max_tokens, max_len, form, window, sinks), M, Hq, head_dim);
+  return ATTS_OK;
 }
 
 // launch_pdl with `cluster` blocks to a cluster; the grid counts clusters.
@@ -170,6 +279,62 @@ static int launch_pdl_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
     return ATTS_ERR_CUDA;
   }
   return ATTS_OK;
+}
+
+// Slots of a block of the packed append and of the call that reads back: enough blocks for every SM first.
+static int pack_tokens(int sms, int64_t slots) {
+  int n = kPackMaxTokens;
+  while (n > 1 && slots < 4 * (int64_t)n * sms) n /= 2;
+  return n;
+}
+
+// Checks and launch shared by the two normed rotations; the caller has filled what is its own.
+template <bool ROWS>
+static int norm_rope(NormRopeArgs& a, const void* q, int64_t q_ts, int64_t q_hs, const void* k, int64_t k_ts, int64_t k_hs,
+                     const int32_t* positions, const double* freqs, int32_t pairs, float mscale, int32_t interleaved, const void* q_gain,
+                     const void* k_gain, float eps, int32_t dtype, int64_t M, int32_t Hq, int32_t Hk, int32_t D, void* q_out, int64_t o_ts,
+                     int64_t o_hs, bool wide, bool none, int64_t num_seqs, void* cuda_stream) {
+  if (M < 0 || M > (1ll << 30) || Hq < 0 || Hq > (1 << 20)) return ATTS_ERR_SHAPE;
+  if (pairs < 0 || 2 * (int64_t)pairs > D) return ATTS_ERR_SHAPE;
+  if (q_ts < 0 || q_hs < 0 || k_ts < 0 || k_hs < 0 || o_ts < 0 || o_hs < 0) return ATTS_ERR_SHAPE;
+  if (interleaved != 0 && interleaved != 1) return ATTS_ERR_ARG;
+  if (!(mscale >= -3.402823466e38f && mscale <= 3.402823466e38f) || !(eps >= 0.f && eps <= 3.402823466e38f)) return ATTS_ERR_ARG;
+  if (M > 0 && ((Hk > 0 && !k) || (Hq > 0 && (!q || !q_out)) || (pairs > 0 && (!positions || !freqs)))) return ATTS_ERR_NULL;
+  if (!aligned(q, 2) || !aligned(k, 2) || !aligned(q_out, 2) || !aligned(q_gain, 2) || !aligned(k_gain, 2) || !aligned(positions, 4) ||
+      !aligned(freqs, 8))
+    return ATTS_ERR_ALIGN;
+  const DeviceInfo* di;
+  const int st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  if (M == 0 || none) return ATTS_OK;
+  a.q = static_cast<const char*>(q);
+  a.k = static_cast<const char*>(k);
+  a.q_gain = static_cast<const char*>(q_gain);
+  a.k_gain = static_cast<const char*>(k_gain);
+  a.q_out = static_cast<char*>(q_out);
+  a.q_ts = q_ts; a.q_hs = q_hs; a.k_ts = k_ts; a.k_hs = k_hs; a.o_ts = o_ts; a.o_hs = o_hs;
+  a.positions = positions; a.freqs = freqs;
+  a.pairs = pairs; a.D = D; a.Hq = Hq; a.Hk = Hk; a.M = (int)M; a.mscale = mscale; a.eps = eps;
+  const int64_t bits = (Hq > 0 ? q_ts | q_hs | o_ts | o_hs : 0) | (Hk > 0 ? k_ts | k_hs : 0);
+  wide = wide && bits % 8 == 0 && aligned(q, 16) && aligned(k, 16) && aligned(q_out, 16) && aligned(q_gain, 16) && aligned(k_gain, 16) &&
+         pairs % (interleaved ? 4 : 8) == 0;
+  a.lanes_log2 = 0;
+  while (a.lanes_log2 < 4 && 16 << a.lanes_log2 < D) ++a.lanes_log2;   // two pieces of eight channels a thread
+  const int64_t span = ROWS ? M : a.max_tokens;
+  a.tpb = M >= 4 * 8 * (int64_t)di->sm_count ? 4 : 1;
+  const dim3 grid((unsigned)((span + a.tpb - 1) / a.tpb), ROWS ? 1 : (unsigned)num_seqs);
+  const size_t smem = sizeof(float2) * a.tpb * (size_t)pairs;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+#define ATTS_NORM(T, I, W) return launch_pdl(norm_rope_kernel<T, I, W, ROWS>, grid, dim3(kRopeThreads), smem, stream, a, di->dev_status)
+#define ATTS_NORM_T(T)                                                                        \
+  do {                                                                                        \
+    if (interleaved) { if (wide) ATTS_NORM(T, true, true); else ATTS_NORM(T, true, false); }  \
+    else { if (wide) ATTS_NORM(T, false, true); else ATTS_NORM(T, false, false); }            \
+  } while (0)
+  if (dtype == ATTS_BF16) ATTS_NORM_T(__nv_bfloat16);
+  else ATTS_NORM_T(__half);
+#undef ATTS_NORM_T
+#undef ATTS_NORM
 }
 
 template <typename T, int D, bool MANY>
@@ -296,15 +461,7 @@ int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
 
 int atts_tree_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,
                                         int64_t max_tokens, int64_t max_len, size_t* bytes) {
-  if (!bytes) return ATTS_ERR_NULL;
-  if (num_seqs < 0 || num_seqs > 65535 || M < 0 || M > (1ll << 30) || heads < 1 || heads > 1024 || Hq < 1 || Hq % heads != 0 ||
-      Hq / heads > 128 || (head_dim != 64 && head_dim != 128) || max_tokens < 0 || max_len < max_tokens || max_len > kMaxSlots)
-    return ATTS_ERR_SHAPE;
-  const DeviceInfo* di;
-  const int st = device_info(&di);
-  if (st != ATTS_OK) return st;
-  *bytes = attn_workspace(attn_shape(di->sm_count, num_seqs, Hq, heads, head_dim, max_tokens, max_len), M, Hq, head_dim);
-  return ATTS_OK;
+  return attention_workspace(kFormPlain, num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, kEndless, 0, bytes);
 }
 
 int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
@@ -317,44 +474,154 @@ int atts_tree_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
   if (st != ATTS_OK) return st;
   st = check_queries(q, q_token_stride, q_head_stride, cache, ctx_lens, cu_tokens, pre, end, M, Hq, max_tokens, max_len, scale);
   if (st != ATTS_OK) return st;
-  if (out_token_stride < 0 || out_head_stride < 0 || out_token_stride % 8 || out_head_stride % 8) return ATTS_ERR_SHAPE;
-  if ((M > 0 && !out) || !workspace) return ATTS_ERR_NULL;
-  if (!aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, 256)) return ATTS_ERR_ALIGN;
+  return attend<kFormPlain>(a, cache, q, q_token_stride, q_head_stride, ctx_lens, cu_tokens, pre, end, nullptr, kEndless, 0, M, Hq, max_tokens,
+                            max_len, scale, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes, cuda_stream);
+}
+
+int atts_window_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens,
+                                          int64_t max_len, int64_t window, int64_t sinks, size_t* bytes) {
+  const int st = check_window(window, sinks, false, nullptr, nullptr);
+  if (st != ATTS_OK) return st;
+  return attention_workspace(kFormWindow, num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, window, sinks, bytes);
+}
+
+int atts_window_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,
+                          const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre, const int32_t* end,
+                          const int32_t* depth, int64_t window, int64_t sinks, int64_t M, int32_t Hq, int64_t max_tokens,
+                          int64_t max_len, float scale, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  AttnArgs a;
+  int st = cache_view(cache, &a.cache);
+  if (st != ATTS_OK) return st;
+  st = check_queries(q, q_token_stride, q_head_stride, cache, ctx_lens, cu_tokens, pre, end, M, Hq, max_tokens, max_len, scale);
+  if (st != ATTS_OK) return st;
+  if ((st = check_window(window, sinks, false, pre, depth)) != ATTS_OK) return st;
+  return attend<kFormWindow>(a, cache, q, q_token_stride, q_head_stride, ctx_lens, cu_tokens, pre, end, depth, window, sinks, M, Hq, max_tokens,
+                             max_len, scale, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes, cuda_stream);
+}
+
+int atts_packed_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens,
+                                          int64_t max_len, int64_t window, int64_t sinks, size_t* bytes) {
+  const int st = check_window(window, sinks, true, nullptr, nullptr);
+  if (st != ATTS_OK) return st;
+  return attention_workspace(kFormPacked, num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, window ? window : kEndless, sinks, bytes);
+}
+
+int atts_packed_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t dtype, const atts_packed_cache* cache,
+                          const int32_t* ctx_lens, const int32_t* cu_tokens, const int32_t* pre, const int32_t* end,
+                          const int32_t* depth, int64_t window, int64_t sinks, int64_t M, int32_t Hq, int64_t max_tokens,
+                          int64_t max_len, float scale, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  AttnArgs a;
+  int st = packed_view(cache, &a.cache);
+  if (st != ATTS_OK) return st;
+  if (dtype != ATTS_BF16 && dtype != ATTS_FP16) return ATTS_ERR_ARG;
+  const atts_kv_cache c = {cache->k, cache->v, cache->block_table, cache->num_seqs, cache->table_cols, cache->table_stride, cache->num_pages,
+                           cache->page_size, cache->page_stride, 1, cache->head_stride, cache->heads, cache->head_dim, dtype, 0};
+  st = check_queries(q, q_token_stride, q_head_stride, &c, ctx_lens, cu_tokens, pre, end, M, Hq, max_tokens, max_len, scale);
+  if (st != ATTS_OK) return st;
+  if ((st = check_window(window, sinks, true, pre, depth)) != ATTS_OK) return st;
+  return attend<kFormPacked>(a, &c, q, q_token_stride, q_head_stride, ctx_lens, cu_tokens, pre, end, depth, window ? window : kEndless, sinks, M,
+                             Hq, max_tokens, max_len, scale, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes,
+                             cuda_stream);
+}
+
+int atts_packed_append(const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                       int64_t v_head_stride, int32_t dtype, const atts_packed_cache* cache, const int32_t* ctx_lens,
+                       const int32_t* cu_tokens, int64_t M, int64_t max_tokens, void* cuda_stream) {
+  PackArgs a;
+  int st = packed_view(cache, &a.cache);
+  if (st != ATTS_OK) return st;
+  if (dtype != ATTS_BF16 && dtype != ATTS_FP16) return ATTS_ERR_ARG;
+  if (M < 0 || M > (1ll << 30) || max_tokens < 0 || max_tokens > kMaxSlots) return ATTS_ERR_SHAPE;
+  if (k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0) return ATTS_ERR_SHAPE;
+  if (cache->num_seqs > 0 && (!ctx_lens || !cu_tokens)) return ATTS_ERR_NULL;
+  if (M > 0 && (!k || !v)) return ATTS_ERR_NULL;
+  if (!aligned(k, 2) || !aligned(v, 2) || !aligned(ctx_lens, 4) || !aligned(cu_tokens, 4)) return ATTS_ERR_ALIGN;
   const DeviceInfo* di;
   st = device_info(&di);
   if (st != ATTS_OK) return st;
-  AttnShape sh = attn_shape(di->sm_count, cache->num_seqs, Hq, cache->heads, cache->head_dim, max_tokens, max_len);
-  if (workspace_bytes < attn_workspace(sh, M, Hq, cache->head_dim)) return ATTS_ERR_WORKSPACE;
   if (M == 0 || cache->num_seqs == 0 || max_tokens == 0) return ATTS_OK;
-  a.q = static_cast<const char*>(q);
-  a.out = static_cast<char*>(out);
-  a.lse = lse;
-  a.q_ts = q_token_stride; a.q_hs = q_head_stride; a.o_ts = out_token_stride; a.o_hs = out_head_stride;
-  a.ctx = ctx_lens; a.cu = cu_tokens; a.pre = pre; a.end = end;
-  a.M = (int)M; a.Hq = Hq; a.G = Hq / cache->heads; a.max_tokens = (int)max_tokens; a.max_len = (int)max_len;
-  a.scale = scale;
-  sh.p.part_lse = static_cast<float*>(workspace);
-  sh.p.part_o = sh.p.part_lse + round_up((size_t)M * Hq * sh.p.chunks * 4, 256) / 4;
-  sh.p.wait_limit = wait_limit();
-  sh.p.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
-  const int64_t gx = (int64_t)sh.p.nq * sh.p.chunks;
-  if (gx > 0x7FFFFFFF || (int64_t)max_tokens * Hq > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
-  CUtensorMap mq, mk, mv;
-  if (encode_queries(di, &mq, cache, q, q_token_stride, q_head_stride, M, Hq, sh.p.tpt) != ATTS_OK ||
-      encode_cache(di, &mk, cache, cache->k) != ATTS_OK || encode_cache(di, &mv, cache, cache->v) != ATTS_OK)
-    return ATTS_ERR_CUDA;
-  const dim3 grid((unsigned)gx, (unsigned)cache->heads, (unsigned)cache->num_seqs);
+  a.k = static_cast<const char*>(k);
+  a.v = static_cast<const char*>(v);
+  a.k_ts = k_token_stride; a.k_hs = k_head_stride; a.v_ts = v_token_stride; a.v_hs = v_head_stride;
+  a.ctx = ctx_lens; a.cu = cu_tokens;
+  a.D = cache->head_dim; a.M = (int)M; a.max_tokens = (int)max_tokens;
+  a.tpb = pack_tokens(di->sm_count, M);
+  const bool wide = (k_token_stride | k_head_stride | v_token_stride | v_head_stride) % 8 == 0 && aligned(k, 16) && aligned(v, 16);
+  const dim3 grid((unsigned)((max_tokens + a.tpb - 1) / a.tpb), (unsigned)cache->num_seqs);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const bool bf = cache->dtype == ATTS_BF16;
-#define ATTS_ATTEND(D, MODE)                                                                                      \
-  (bf ? launch_attention<__nv_bfloat16, D, MODE>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream)               \
-      : launch_attention<__half, D, MODE>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream))
-#define ATTS_ATTEND_D(D)                                  \
-  (sh.mode == kRowsTwo ? ATTS_ATTEND(D, kRowsTwo)         \
-                       : sh.mode == kRowsOne ? ATTS_ATTEND(D, kRowsOne) : ATTS_ATTEND(D, kRowsBrief))
-  return cache->head_dim == 128 ? ATTS_ATTEND_D(128) : ATTS_ATTEND_D(64);
-#undef ATTS_ATTEND_D
-#undef ATTS_ATTEND
+#define ATTS_PACK(T, W) return launch_pdl(packed_append_kernel<T, W>, grid, dim3(kPackThreads), 0, stream, a, di->dev_status)
+  if (dtype == ATTS_BF16) { if (wide) ATTS_PACK(__nv_bfloat16, true); else ATTS_PACK(__nv_bfloat16, false); }
+  if (wide) ATTS_PACK(__half, true);
+  ATTS_PACK(__half, false);
+#undef ATTS_PACK
+}
+
+int atts_packed_read(const atts_packed_cache* src, const int32_t* lens, int64_t max_len, const atts_kv_cache* dst, void* cuda_stream) {
+  ReadArgs a;
+  int st = packed_view(src, &a.src);
+  if (st != ATTS_OK) return st;
+  if ((st = cache_view(dst, &a.dst)) != ATTS_OK) return st;
+  if (src->heads != dst->heads || src->head_dim != dst->head_dim || src->num_seqs != dst->num_seqs) return ATTS_ERR_SHAPE;
+  if (max_len < 0 || max_len > kMaxSlots) return ATTS_ERR_SHAPE;
+  if (src->num_seqs > 0 && !lens) return ATTS_ERR_NULL;
+  if (!aligned(lens, 4)) return ATTS_ERR_ALIGN;
+  const DeviceInfo* di;
+  st = device_info(&di);
+  if (st != ATTS_OK) return st;
+  if (src->num_seqs == 0 || max_len == 0) return ATTS_OK;
+  a.lens = lens;
+  a.D = src->head_dim; a.max_len = (int)max_len;
+  a.tpb = pack_tokens(di->sm_count, src->num_seqs * max_len);
+  const dim3 grid((unsigned)((max_len + a.tpb - 1) / a.tpb), (unsigned)src->num_seqs);
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  if (dst->dtype == ATTS_BF16) return launch_pdl(packed_read_kernel<__nv_bfloat16>, grid, dim3(kPackThreads), 0, stream, a, di->dev_status);
+  return launch_pdl(packed_read_kernel<__half>, grid, dim3(kPackThreads), 0, stream, a, di->dev_status);
+}
+
+int atts_norm_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                          int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                          const int32_t* positions, const double* freqs, int32_t rotary_pairs, float mscale, int32_t interleaved,
+                          const void* q_gain, const void* k_gain, float eps, const atts_kv_cache* cache, const int32_t* ctx_lens,
+                          const int32_t* cu_tokens, int64_t M, int32_t Hq, int64_t max_tokens, void* q_out, int64_t out_token_stride,
+                          int64_t out_head_stride, void* cuda_stream) {
+  NormRopeArgs a;
+  int st = cache_view(cache, &a.cache);
+  if (st != ATTS_OK) return st;
+  if (max_tokens < 0 || max_tokens > kMaxSlots || v_token_stride < 0 || v_head_stride < 0) return ATTS_ERR_SHAPE;
+  if (cache->num_seqs > 0 && (!ctx_lens || !cu_tokens)) return ATTS_ERR_NULL;
+  if (M > 0 && !v) return ATTS_ERR_NULL;
+  if (!aligned(v, 2) || !aligned(ctx_lens, 4) || !aligned(cu_tokens, 4)) return ATTS_ERR_ALIGN;
+  a.v = static_cast<const char*>(v);
+  a.v_ts = v_token_stride; a.v_hs = v_head_stride;
+  a.ctx = ctx_lens; a.cu = cu_tokens; a.max_tokens = (int)max_tokens;
+  const bool none = cache->num_seqs == 0 || max_tokens == 0;
+  const bool wide = (v_token_stride | v_head_stride) % 8 == 0 && aligned(v, 16);
+  a.k_out = nullptr;
+  a.ko_ts = a.ko_hs = 0;
+  return norm_rope<false>(a, q, q_token_stride, q_head_stride, k, k_token_stride, k_head_stride, positions, freqs, rotary_pairs, mscale,
+                          interleaved, q_gain, k_gain, eps, cache->dtype, M, Hq, cache->heads, cache->head_dim, q_out, out_token_stride,
+                          out_head_stride, wide, none, cache->num_seqs, cuda_stream);
+}
+
+int atts_norm_rope(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* k, int64_t k_token_stride,
+                   int64_t k_head_stride, const int32_t* positions, const double* freqs, int32_t rotary_pairs, float mscale,
+                   int32_t interleaved, const void* q_gain, const void* k_gain, float eps, int32_t dtype, int64_t M, int32_t Hq,
+                   int32_t Hk, int32_t head_dim, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, void* k_out,
+                   int64_t k_out_token_stride, int64_t k_out_head_stride, void* cuda_stream) {
+  if (dtype != ATTS_BF16 && dtype != ATTS_FP16) return ATTS_ERR_ARG;
+  if (head_dim < 8 || head_dim > 256 || head_dim % 8 != 0 || Hk < 0 || Hk > (1 << 20)) return ATTS_ERR_SHAPE;
+  if (k_out_token_stride < 0 || k_out_head_stride < 0) return ATTS_ERR_SHAPE;
+  if (M > 0 && Hk > 0 && !k_out) return ATTS_ERR_NULL;
+  if (!aligned(k_out, 2)) return ATTS_ERR_ALIGN;
+  NormRopeArgs a = {};
+  a.k_out = static_cast<char*>(k_out);
+  a.ko_ts = k_out_token_stride; a.ko_hs = k_out_head_stride;
+  const bool wide = Hk == 0 || ((k_out_token_stride | k_out_head_stride) % 8 == 0 && aligned(k_out, 16));
+  return norm_rope<true>(a, q, q_token_stride, q_head_stride, k, k_token_stride, k_head_stride, positions, freqs, rotary_pairs, mscale,
+                         interleaved, q_gain, k_gain, eps, dtype, M, Hq, Hk, head_dim, q_out, q_out_token_stride, q_out_head_stride, wide,
+                         Hq + Hk == 0, 1, cuda_stream);
 }
 
 int atts_cache_weights(const void* q, int64_t q_token_stride, int64_t q_head_stride, const atts_kv_cache* cache,

@@ -4,6 +4,7 @@
 
 #include "conformal.cuh"
 #include "lmhead_lse.cuh"
+#include "packed_cache.cuh"
 #include "rope_cache.cuh"
 
 namespace atts {
@@ -16,7 +17,10 @@ struct AttnArgs {
   const int32_t *ctx, *cu, *pre, *end;
   int M, Hq, G, max_tokens, max_len;
   float scale;
-  CacheView cache;
+  CacheView cache;          // (a packed cache: strides in bytes, no slot stride)
+  // Windowed forms only.  A token's place on its line: a cached slot's number, or ctx + depth among the drafts.
+  const int32_t* depth;     // NULL: chains
+  int window, sinks;
 };
 
 // What a drafted token sees: the cached slots below ctx, and the drafted tokens j with lo(j) <= mine < hi(j).
@@ -151,22 +155,36 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // of the tiles that need them and clears the values of slots that hold nothing (whatever lies there, 0 * NaN must not reach
 // O), 4-7 and 8-11 are the two streams' rows.
 // ------------------------------------------------------------------------------------------------------------------
+//
+// Windowed form: a row sees, of all that the tree lets it see, the places nearer than `window` to its own and the first `sinks`.
+// The cached tiles between the sinks and the first place that any of the CTA's rows sees are left out of the count of tiles
+// (WindowView), so neither time nor chunks are spent on them; at the window's edge pairs are looked at one by one, as in a tree.
+// Packed form: the cache holds 4 bits a channel (packed_cache.cuh).  Warps 0 and 2 bring codes and scales into a ring of raw tiles
+// (one bulk copy a page), four more warps (12-15) expand them into the ring that the products read, with zeros for slots that hold
+// nothing; the expanded values are exact, so everything behind is the same arithmetic.
 enum AttnMode { kRowsTwo, kRowsOne, kRowsBrief };
+enum AttnForm { kFormPlain = 0, kFormWindow = 1, kFormPacked = 3 };   // (packed caches are attended to through a window, which may be endless)
 constexpr int kAttnTile = 128;          // rows of a tile, slots of a tile
 constexpr int kAttnTreeTiles = 1024;    // tiles behind the cached part that are listed; further ones are all looked at
 constexpr int kMaskRing = 4;
 
-template <int D, AttnMode MODE>
+template <int D, AttnMode MODE, AttnForm FORM = kFormPlain>
 struct AttnCfg {
+  static constexpr bool kWindow = (FORM & 1) != 0, kPacked = (FORM & 2) != 0;
   static constexpr int kStreams = MODE == kRowsBrief ? 1 : 2;
-  static constexpr int kThreads = 128 + 128 * kStreams;
+  static constexpr int kThreads = 128 + 128 * kStreams + (kPacked ? 128 : 0);
   static constexpr int kTmem = 256 * kStreams;                       // columns: scores (over them the probabilities), then O
   static constexpr int kTileBytes = kAttnTile * D * 2;
   static constexpr int kQBytes = (MODE == kRowsTwo ? 2 : 1) * kTileBytes;
-  static constexpr int kStages = D == 128 ? (MODE == kRowsTwo ? 4 : MODE == kRowsOne ? 5 : 2) : MODE == kRowsBrief ? 4 : 8;
+  static constexpr int kStages = kPacked ? (D == 128 ? (MODE == kRowsTwo ? 3 : 4) : 6)
+                                 : D == 128 ? (MODE == kRowsTwo ? 4 : MODE == kRowsOne ? 5 : 2) : MODE == kRowsBrief ? 4 : 8;
+  static constexpr int kRawStages = !kPacked ? 0 : D == 128 ? (MODE == kRowsTwo ? 4 : 6) : 8;
+  static constexpr int kRawBytes = kAttnTile / 8 * packed_eight(D);
   static constexpr int kRing = kQBytes;                              // byte offsets in (aligned) shared memory
   static constexpr int kMask = kRing + kStages * kTileBytes;         // [kMaskRing][128] int2
-  static constexpr int kList = kMask + kMaskRing * kAttnTile * 8;    // [kAttnTreeTiles] uint32
+  static constexpr int kPlaces = kMask + kMaskRing * kAttnTile * 8;  // [kMaskRing][128] int, windowed forms
+  static constexpr int kRaw = kPlaces + (kWindow ? kMaskRing * kAttnTile * 4 : 0);   // [kRawStages] raw tiles, packed form
+  static constexpr int kList = kRaw + kRawStages * kRawBytes;        // [kAttnTreeTiles] uint32
   static constexpr int kStats = kList + kAttnTreeTiles * 4;          // [128] float2: maximum and sum of the odd stream
   static constexpr int kBars = kStats + kAttnTile * 8;
   static constexpr int kSmemBytes = kBars + 512 + 1024;
@@ -213,6 +231,47 @@ __device__ __forceinline__ int2 slot_interval(const AttnArgs& a, const SeqView& 
   return (lo < 0 || hi <= lo) ? make_int2(0, 0) : make_int2(lo, hi - lo);
 }
 
+// Depth of drafted token j, and the place on its line of what a slot holds (any number where it holds nothing).  A depth that
+// no tree can have is cut to what one can, so that places stay below a sequence's length.
+__device__ __forceinline__ int draft_depth(const AttnArgs& a, const SeqView& s, int j) {
+  return a.depth ? max(0, min(a.depth[s.first + j], s.n - 1)) : j;
+}
+__device__ __forceinline__ int slot_place(const AttnArgs& a, const SeqView& s, int slot) {
+  const int j = slot - s.ctx;
+  return j < 0 || j >= s.n ? slot : s.ctx + draft_depth(a, s, j);
+}
+
+// What the window leaves of a sequence for rows whose depths span [dmin, dmax]: tiles are numbered without the `skip` ones from number
+// `sink_tiles` on, of which no row sees anything.
+struct WindowView {
+  int near_first, near_all;   // the shallowest row sees places from near_first on, every row those from near_all on
+  int sink_tiles, skip;
+  __device__ __forceinline__ int tile(int number) const { return number < sink_tiles ? number : number + skip; }
+};
+__device__ __forceinline__ WindowView window_view(const AttnArgs& a, const SeqView& s, int tok0, int ntok, int ntiles, int lane) {
+  int dmin = 0x7FFFFFFF, dmax = -1;
+  for (int t = tok0 + lane; t < tok0 + ntok; t += 32) {
+    if (a.pre && a.pre[s.first + t] < 0) continue;
+    const int d = draft_depth(a, s, t);
+    dmin = min(dmin, d);
+    dmax = max(dmax, d);
+  }
+  dmin = __reduce_min_sync(0xFFFFFFFFu, dmin);
+  dmax = __reduce_max_sync(0xFFFFFFFFu, dmax);
+  if (dmax < 0) dmin = dmax = 0;                          // nothing but padding
+  WindowView w;
+  w.near_first = s.ctx + dmin - a.window + 1;             // (at most 2^30 each: the sum fits)
+  w.near_all = s.ctx + dmax - a.window + 1;
+  // A drafted token's slot is never below its place, so the first places that rows see bound the slots too; but a token of a low
+  // place (a sink) may lie anywhere among the drafts, so where the drafts have sinks none of their tiles is left out.
+  int first = max(0, w.near_first) / kAttnTile;
+  if (s.ctx < a.sinks) first = min(first, s.ctx / kAttnTile);
+  first = min(first, ntiles);
+  w.sink_tiles = min((int)(((int64_t)a.sinks + kAttnTile - 1) / kAttnTile), first);
+  w.skip = first - w.sink_tiles;
+  return w;
+}
+
 // The same for a whole tile by one warp, slots e * 32 + lane, all loads under way at once.
 __device__ __forceinline__ void tile_intervals(const AttnArgs& a, const SeqView& s, int tile, int lane, int2 (&v)[kAttnTile / 32]) {
   constexpr int E = kAttnTile / 32;
@@ -236,8 +295,26 @@ __device__ __forceinline__ void tile_intervals(const AttnArgs& a, const SeqView&
   }
 }
 
+// The window's part of a slot's visibility: whether any row sees place x, whether every row does.
+__device__ __forceinline__ bool window_any(const AttnArgs& a, const WindowView& w, int x) { return x >= w.near_first || x < a.sinks; }
+__device__ __forceinline__ bool window_all(const AttnArgs& a, const WindowView& w, int x) { return x >= w.near_all || x < a.sinks; }
+
+// Flags of a tile of cached slots under a window.
+__device__ __forceinline__ uint32_t window_flags(const AttnArgs& a, const WindowView& w, int tile) {
+  uint32_t f = 0;
+#pragma unroll
+  for (int e = 0; e < kAttnTile / 32; ++e) {
+    const int x = tile * kAttnTile + e * 32, last = x + 31;
+    if (x >= w.near_all || last < a.sinks) f |= 2u << (2 * e);
+    else if (last >= w.near_first || x < a.sinks) f |= (1u << (2 * e)) | kTileMasked;
+  }
+  return f;
+}
+
 // Flags of one tile for rows whose places span [qmin, qmax] (whole warp); 0: nobody sees anything of it.
-__device__ __forceinline__ uint32_t tile_flags(const AttnArgs& a, const SeqView& s, int tile, int qmin, int qmax, int lane) {
+template <bool WINDOW = false>
+__device__ __forceinline__ uint32_t tile_flags(const AttnArgs& a, const SeqView& s, int tile, int qmin, int qmax, int lane,
+                                               const WindowView* w = nullptr) {
   uint32_t f = 0;
   int2 v[kAttnTile / 32];
   tile_intervals(a, s, tile, lane, v);
@@ -245,8 +322,14 @@ __device__ __forceinline__ uint32_t tile_flags(const AttnArgs& a, const SeqView&
   for (int e = 0; e < kAttnTile / 32; ++e) {
     const unsigned last = (unsigned)v[e].x + (unsigned)v[e].y;    // one past the interval
     const bool none = v[e].y == 0;
-    const bool any = __any_sync(0xFFFFFFFFu, !none && v[e].x <= qmax && (unsigned)qmin < last);
-    const bool all = __all_sync(0xFFFFFFFFu, !none && v[e].x <= qmin && (unsigned)qmax < last);
+    bool in = true, in_all = true;
+    if (WINDOW) {
+      const int x = slot_place(a, s, tile * kAttnTile + e * 32 + lane);
+      in = window_any(a, *w, x);
+      in_all = window_all(a, *w, x);
+    }
+    const bool any = __any_sync(0xFFFFFFFFu, !none && in && v[e].x <= qmax && (unsigned)qmin < last);
+    const bool all = __all_sync(0xFFFFFFFFu, !none && in_all && v[e].x <= qmin && (unsigned)qmax < last);
     if (any) f |= all ? 2u << (2 * e) : (1u << (2 * e)) | kTileMasked;
     if (__any_sync(0xFFFFFFFFu, none)) f |= kTileDead;
   }
@@ -256,9 +339,8 @@ __device__ __forceinline__ uint32_t tile_flags(const AttnArgs& a, const SeqView&
 // Loads a tile of slots, a lane per box (one page, 64 channels).  A TMA instruction costs its warp about 117 cycles when one
 // lane issues one after the other and 56 when lanes issue side by side, whatever its size, and warps do not disturb one
 // another (measured, boxes of 8 to 128 rows): so small pages are issued by many lanes, keys and values by two warps.
-template <int D>
+template <int D, int kHalves = D / 64>
 struct TileBoxes {
-  static constexpr int kHalves = D / 64;
   int page_log2, rows, boxes, slot;   // slots of a box, boxes of a tile (<= 32), this lane's first slot in the tile
   __device__ __forceinline__ TileBoxes(int page_log2_, int lane) : page_log2(page_log2_) {
     rows = min(1 << page_log2, kAttnTile);
@@ -288,12 +370,89 @@ __device__ __forceinline__ void rescale_o(uint32_t taddr, float f) {
   tmem_st_wait();
 }
 
-template <typename T, int D, AttnMode MODE>
-__global__ void __launch_bounds__(AttnCfg<D, MODE>::kThreads, MODE == kRowsBrief ? 2 : 1)
+// One bulk copy of a contiguous piece (addresses and size multiples of 16 bytes).
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar) : "memory");
+}
+
+// (x * s) in two 16-bit halves, exact: v = 16 + n in the top four fraction bits of each half, n = c + 8, and v s - 24 s = c s.
+template <typename T>
+struct Expand;
+template <>
+struct Expand<__nv_bfloat16> {
+  static constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
+  static constexpr int kShift = 3;      // nibble 0 to the top of the fraction
+  static __device__ __forceinline__ void scale(float s, uint32_t& s2, uint32_t& m2) {
+    s2 = Pack<__nv_bfloat16>::pack(s, s);
+    m2 = Pack<__nv_bfloat16>::pack(-24.f * s, -24.f * s);
+  }
+  static __device__ __forceinline__ uint32_t fma2(uint32_t v, uint32_t s, uint32_t m) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(s), "r"(m));
+    return r;
+  }
+};
+template <>
+struct Expand<__half> {
+  static constexpr uint32_t kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;
+  static constexpr int kShift = 6;
+  static __device__ __forceinline__ void scale(float s, uint32_t& s2, uint32_t& m2) {
+    s2 = Pack<__half>::pack(s, s);
+    m2 = Pack<__half>::pack(-24.f * s, -24.f * s);
+  }
+  static __device__ __forceinline__ uint32_t fma2(uint32_t v, uint32_t s, uint32_t m) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(s), "r"(m));
+    return r;
+  }
+};
+template <typename T, int I>
+__device__ __forceinline__ uint32_t expand_pair(uint32_t word, uint32_t s2, uint32_t m2) {
+  constexpr int by = Expand<T>::kShift - 4 * I;           // channel pair I sits in bits 4 I and 16 + 4 I
+  const uint32_t v = by >= 0 ? word << (by >= 0 ? by : 0) : word >> (by < 0 ? -by : 0);
+  return Expand<T>::fma2((v & Expand<T>::kMask) | Expand<T>::kSixteen, s2, m2);
+}
+
+// A quarter of a raw tile (32 slots) by one warp into the 16-bit tile that the products read: blocks of 64 channels, a row of 128
+// bytes a slot, 16-byte pieces swizzled by the row.  A thread takes a group of 32 channels; groups 2 and 3 write their pieces in
+// another order than groups 0 and 1, so that eight threads that store together never share a bank.  `dead`: bit per turn, slots that
+// hold nothing (zeros, whatever lies there).
+template <typename T, int D>
+__device__ __forceinline__ void expand_rows(const uint8_t* raw, uint8_t* tile, int quarter, int lane, uint32_t dead) {
+  constexpr int kPer = D / 32, kRows = 32 / kPer;         // threads a slot, slots a turn
+  const int g = lane % kPer;
+#pragma unroll
+  for (int it = 0; it < 32 / kRows; ++it) {
+    const int row = quarter * 32 + it * kRows + lane / kPer, r7 = row & 7;
+    const uint8_t* eight = raw + (row >> 3) * packed_eight(D);
+    uint4 w = *reinterpret_cast<const uint4*>(eight + r7 * (D / 2) + g * 16);
+    uint32_t byte = eight[4 * D + r7 * (D / 32) + g];
+    if ((dead >> it) & 1u) {
+      w = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+      byte = 0;
+    }
+    uint32_t s2, m2;
+    Expand<T>::scale(packed_scale(byte), s2, m2);
+    const bool swap = g >= 2;
+    const uint32_t word[4] = {swap ? w.z : w.x, swap ? w.w : w.y, swap ? w.x : w.z, swap ? w.y : w.w};
+    uint8_t* out = tile + (g >> 1) * (kAttnTile * 128) + row * 128;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int piece = (g & 1) * 4 + (swap ? i ^ 2 : i);
+      *reinterpret_cast<uint4*>(out + ((piece ^ r7) * 16)) = make_uint4(expand_pair<T, 0>(word[i], s2, m2), expand_pair<T, 1>(word[i], s2, m2),
+                                                                     expand_pair<T, 2>(word[i], s2, m2), expand_pair<T, 3>(word[i], s2, m2));
+    }
+  }
+}
+
+template <typename T, int D, AttnMode MODE, AttnForm FORM>
+__global__ void __launch_bounds__(AttnCfg<D, MODE, FORM>::kThreads, MODE == kRowsBrief ? 2 : 1)
 tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a,
                       const __grid_constant__ AttnPlan plan, unsigned* __restrict__ dev_status) {
-  using Cfg = AttnCfg<D, MODE>;
+  using Cfg = AttnCfg<D, MODE, FORM>;
+  constexpr bool WINDOW = Cfg::kWindow, PACKED = Cfg::kPacked;
   constexpr bool TWO = MODE != kRowsOne;                // a stream's rows are its own, and it takes every tile
   constexpr int kStreams = Cfg::kStreams;
   constexpr uint32_t kO = 128u * kStreams;              // first column of O
@@ -311,15 +470,29 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   const int tok0 = qt * per;
   if (tok0 >= s.n) return;
   const int ntok = min(per, s.n - tok0);
-  const int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
+  int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
+  int tree0 = min(s.ctx, s.len) / kAttnTile;          // first tile that is not all cached slots (a cache cut at max_len ends inside one)
+  WindowView win;
+  if (WINDOW) {                                       // tile numbers from here on leave out what no row sees
+    win = window_view(a, s, tok0, ntok, ntiles, threadIdx.x & 31);
+    const int first = win.sink_tiles + win.skip;
+    tree0 = tree0 >= first ? tree0 - win.skip : min(tree0, win.sink_tiles);
+    ntiles -= win.skip;
+  }
   const int tile0 = chunk * plan.chunk, tile1 = min(ntiles, tile0 + plan.chunk);
-  if (chunk > 0 && tile0 >= ntiles) return;
+  if (chunk > 0 && tile0 >= ntiles) {
+    // the join of a windowed batch does not know how many tiles a row tile had: it asks every chunk
+    if (WINDOW)
+      for (int i = threadIdx.x; i < ntok * a.G; i += Cfg::kThreads)
+        plan.part_lse[((int64_t)(s.first + tok0 + i / a.G) * a.Hq + hk * a.G + i % a.G) * plan.chunks + chunk] = -INFINITY;
+    return;
+  }
   const bool two = MODE == kRowsTwo && ntok > plan.tpt;
-  const int tree0 = min(s.ctx, s.len) / kAttnTile;    // first tile that is not all cached slots (a cache cut at max_len ends inside one)
 
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
   int2* mask = reinterpret_cast<int2*>(smem + Cfg::kMask);
+  int* places = reinterpret_cast<int*>(smem + Cfg::kPlaces);
   volatile uint32_t* list = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kList);
   float2* stats = reinterpret_cast<float2*>(smem + Cfg::kStats);
   const uint32_t bar0 = smem_base + Cfg::kBars;
@@ -334,7 +507,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   auto o_bar = [&](int i) { return q_bar + 64u + 8u * (uint32_t)i; };
   auto m_full = [&](int i) { return q_bar + 80u + 8u * (uint32_t)i; };
   auto m_empty = [&](int i) { return q_bar + 80u + 8u * (uint32_t)(kMaskRing + i); };
-  constexpr int kBarCount = 3 * kStages + 10 + 2 * kMaskRing;
+  auto raw_full = [&](int i) { return q_bar + 80u + 8u * (uint32_t)(2 * kMaskRing + i); };
+  auto raw_empty = [&](int i) { return q_bar + 80u + 8u * (uint32_t)(2 * kMaskRing + Cfg::kRawStages + i); };
+  constexpr int kBarCount = 3 * kStages + 10 + 2 * kMaskRing + 2 * Cfg::kRawStages;
   static_assert(8 * kBarCount + 32 <= 512, "room for the barriers");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + Cfg::kBars + 8 * kBarCount);
   volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -344,12 +519,18 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     prefetch_tmap(&map_q);
-    prefetch_tmap(&map_k);
-    prefetch_tmap(&map_v);
+    if (!PACKED) {
+      prefetch_tmap(&map_k);
+      prefetch_tmap(&map_v);
+    }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(full_bar(i), 1);
-      mbar_init(empty_bar(i), 2);     // the products that read the stage, and warp 3
+      mbar_init(full_bar(i), PACKED ? 4 : 1);     // the copies, or the warps that expand
+      mbar_init(empty_bar(i), PACKED ? 1 : 2);    // the products that read the stage, and warp 3
       mbar_init(clean_bar(i), 1);
+    }
+    for (int i = 0; i < Cfg::kRawStages; ++i) {
+      mbar_init(raw_full(i), 1);
+      mbar_init(raw_empty(i), 4);
     }
     mbar_init(q_bar, 1);
     mbar_init(join_bar, 4);
@@ -408,34 +589,46 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     }
     return i < ntile;
   };
+  auto tile_at = [&](int number) { return WINDOW ? win.tile(number) : number; };
   auto tile_of = [&](int i, uint32_t& f) -> int {
     f = kTileFull;
-    if (i < npre) return tile0 + i;
+    if (i < npre) {
+      const int t = tile_at(tile0 + i);
+      if (WINDOW) f = window_flags(a, win, t);
+      return t;
+    }
     if (i - npre < nlist) {
       const uint32_t e = list[i - npre];
       f = e & 0xFFFFu;
-      return t0 + (int)(e >> 16);
+      return tile_at(t0 + (int)(e >> 16));
     }
     f = kTileUnknown;
-    return t0 + kAttnTreeTiles + (i - npre - nlist);
+    return tile_at(t0 + kAttnTreeTiles + (i - npre - nlist));
+  };
+  // Where a tile of keys or values stands in the rings' order: K_0 .. K_{lead-1}, then V_i, K_{i+lead}.  Before V_i come i values
+  // and min(lead + i, ntile) keys.
+  auto place_of = [&](int i, bool value) {
+    return value ? (has(kLead + i - 1, false) ? kLead + 2 * i : ntile + i) : i < kLead ? i : 2 * i - kLead + 1;
   };
 
   pdl_launch_dependents();
 
-  // A row's 128 scores stay in registers: 224 (200) for the rows' warps and 56 for the others, 384 x 168 (256 x 128) in all as
-  // launched.
+  // A row's 128 scores stay in registers: 224 (200) for the rows' warps and 56 for the others, 384 x 168 (256 x 128, packed
+  // form: 512 x 128) in all as launched.
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0 || warp == 2) {
       // ---------------- loads: keys (and the queries) by warp 0, values by warp 2.  The ring's order is that of use:
       // K_0 .. K_{lead-1}, then V_i, K_{i+lead} ----------------
-      const TileBoxes<D> bx(a.cache.page_log2, lane);
-      constexpr int kNoSlot = -2;                               // behind the sequence: no page, filled with zeros
+      const TileBoxes<D, PACKED ? 1 : D / 64> bx(a.cache.page_log2, lane);
+      constexpr int kNoSlot = -2;                               // nothing that anybody sees: no page, filled with zeros
       auto look_up = [&](int i) -> int {                        // the table's entry for this lane's box, not looked at yet
         if (!has(i, false)) return kNoSlot;
         uint32_t f;
         const int slot = tile_of(i, f) * kAttnTile + bx.slot;
         if (lane >= bx.boxes || slot >= s.len) return kNoSlot;
+        // a page of which no row sees anything need not be there: what is behind a window may have been freed
+        if (WINDOW && slot + bx.rows <= min(s.ctx, win.near_first) && slot >= a.sinks) return kNoSlot;
         const int col = slot >> bx.page_log2;
         return col < a.cache.table_cols ? a.cache.table[(int64_t)seq * a.cache.table_stride + col] : -1;
       };
@@ -461,8 +654,34 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
           const int page = page_of(e0);
           e0 = e1;
           e1 = look_up(i + 2);
-          // place in the ring's order: before V_i come i values and min(lead + i, ntile) keys
-          const int pos = value ? (has(kLead + i - 1, false) ? kLead + 2 * i : ntile + i) : i < kLead ? i : 2 * i - kLead + 1;
+          const int pos = place_of(i, value);
+          if constexpr (PACKED) {
+            // Raw tiles: a page's piece of the tile is contiguous.  A missing page reads as zeros, and so does one that nobody sees;
+            // slots behind the sequence are left as they are (the warps that expand them look at the lengths).
+            const int stage = pos % Cfg::kRawStages;
+            ok = wait_warp(raw_empty(stage), ((uint32_t)(pos / Cfg::kRawStages) & 1u) ^ 1u);
+            if (!ok) break;
+            uint32_t f;
+            const int slot = tile_of(i, f) * kAttnTile + bx.slot;
+            const uint32_t bytes = (uint32_t)(bx.rows / 8) * packed_eight(D);
+            const uint32_t dst = smem_base + Cfg::kRaw + (uint32_t)stage * Cfg::kRawBytes + (uint32_t)(bx.slot / 8) * packed_eight(D);
+            const bool copied = page < a.cache.num_pages, missing = !copied && lane < bx.boxes && slot < s.len;
+            if (missing) {
+              for (uint32_t o = 0; o < bytes; o += 16)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(dst + o), "r"(0u) : "memory");
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            const uint32_t copies = __popc(__ballot_sync(0xFFFFFFFFu, copied));
+            __syncwarp();
+            if (lane == 0) mbar_expect_tx(raw_full(stage), copies * bytes);
+            __syncwarp();
+            if (copied)
+              bulk_load(dst, (value ? a.cache.v : a.cache.k) + (int64_t)page * a.cache.page_stride + (int64_t)hk * a.cache.head_stride +
+                                 (int64_t)((slot & ((1 << a.cache.page_log2) - 1)) / 8) * packed_eight(D),
+                        bytes, raw_full(stage));
+            __syncwarp();
+            continue;
+          }
           const int stage = pos % kStages;
           ok = wait_warp(empty_bar(stage), ((uint32_t)(pos / kStages) & 1u) ^ 1u);
           if (!ok) break;
@@ -508,7 +727,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         uint32_t f;
         tile_of(i, f);
         ok = wait_warp(full_bar(stage), phase);
-        if (ok && (f & kTileDead)) {
+        if (!PACKED && ok && (f & kTileDead)) {
           ok = wait_warp(clean_bar(stage), (clean_phase >> stage) & 1u);
           clean_phase ^= 1u << stage;
         }
@@ -576,7 +795,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         int2 v[kAttnTile / 32];
         tile_intervals(a, s, t, lane, v);
 #pragma unroll
-        for (int e = 0; e < kAttnTile / 32; ++e) mask[b * kAttnTile + e * 32 + lane] = v[e];
+        for (int e = 0; e < kAttnTile / 32; ++e) {
+          mask[b * kAttnTile + e * 32 + lane] = v[e];
+          if (WINDOW) places[b * kAttnTile + e * 32 + lane] = slot_place(a, s, t * kAttnTile + e * 32 + lane);
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(m_full(b));
         ++masked;
@@ -586,6 +808,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         if (lane == 0) mbar_arrive(empty_bar(stage));
         if (++stage == kStages) { stage = 0; phase ^= 1u; }
       };
+      if constexpr (PACKED) {                        // the ring is other warps' business
+        for (int i = 0; ok && has(i, false); ++i) intervals(i);
+      } else {
       int ik = 0;
       auto pass_key = [&]() {
         intervals(ik++);
@@ -617,15 +842,49 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         release();
         if (has(ik, false)) pass_key();
       }
+      }
+    }
+  } else if (PACKED && warp >= 4 + 4 * kStreams) {
+    // ---------------- raw tiles are expanded, in the rings' order ----------------
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if constexpr (PACKED) {
+      const int quarter = warp & 3;
+      int pos = 0;
+      bool ok = true;
+      auto expand = [&](int i) {
+        const int from = pos % Cfg::kRawStages, to = pos % kStages;
+        ok = wait_warp(raw_full(from), (uint32_t)(pos / Cfg::kRawStages) & 1u) && wait_warp(empty_bar(to), ((uint32_t)(pos / kStages) & 1u) ^ 1u);
+        if (!ok) return;
+        uint32_t f, dead = 0;
+        const int t = tile_of(i, f);
+        if (f & kTileDead) {
+          constexpr int kRows = 32 / (D / 32);
+          for (int it = 0; it < 32 / kRows; ++it)
+            dead |= (slot_interval(a, s, t * kAttnTile + quarter * 32 + it * kRows + lane / (D / 32)).y == 0 ? 1u : 0u) << it;
+        }
+        expand_rows<T, D>(smem + Cfg::kRaw + from * Cfg::kRawBytes, smem + Cfg::kRing + to * Cfg::kTileBytes, quarter, lane, dead);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(full_bar(to));
+          mbar_arrive(raw_empty(from));
+        }
+        ++pos;
+      };
+      for (int i = 0; i < kLead && ok && has(i, false); ++i) expand(i);
+      for (int i = 0; ok && has(i, false); ++i) {
+        expand(i);
+        if (ok && has(i + kLead, false)) expand(i + kLead);
+      }
     }
   } else {
     // ---------------- rows ----------------
-    if (MODE == kRowsBrief) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    if (MODE == kRowsBrief || PACKED) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     {
       const int qmin = range[0], qmax = range[1];    // all rows padding: qmax is -1 and no tile is visible
       for (int t = t0 + warp - 4; t < t_far; t += 4 * kStreams) {
-        const uint32_t f = qmax < 0 ? 0u : tile_flags(a, s, t, qmin, qmax, lane);
+        const uint32_t f = qmax < 0 ? 0u : tile_flags<WINDOW>(a, s, tile_at(t), qmin, qmax, lane, &win);
         if (lane == 0) list[t - t0] = f;
       }
       __syncwarp();
@@ -642,6 +901,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     const int64_t token = (int64_t)s.first + tok0 + tok;
     const int head = hk * a.G + row % a.G;
     const int mine = !in ? -1 : a.pre ? a.pre[token] : tok0 + tok;
+    const int near = WINDOW && in ? s.ctx + draft_depth(a, s, tok0 + tok) - a.window + 1 : 0;   // first place within this row's window
     const float c = a.scale * 1.4426950408889634f;
     float m = -INFINITY, l = 0.f;
     int done = 0;                                      // tiles of this stream so far
@@ -676,8 +936,14 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 #pragma unroll
               for (int j = 32 * g; j < 32 * g + 32; j += 2) {
                 const int4 w = *reinterpret_cast<const int4*>(mk + j);
-                if ((unsigned)(mine - w.x) >= (unsigned)w.y) v[j] = 0xFF800000u;
-                if ((unsigned)(mine - w.z) >= (unsigned)w.w) v[j + 1] = 0xFF800000u;
+                bool out0 = (unsigned)(mine - w.x) >= (unsigned)w.y, out1 = (unsigned)(mine - w.z) >= (unsigned)w.w;
+                if (WINDOW) {
+                  const int2 x = *reinterpret_cast<const int2*>(places + (masked % kMaskRing) * kAttnTile + j);
+                  out0 |= x.x < near && x.x >= a.sinks;
+                  out1 |= x.y < near && x.y >= a.sinks;
+                }
+                if (out0) v[j] = 0xFF800000u;
+                if (out1) v[j + 1] = 0xFF800000u;
               }
             }
           }
@@ -764,7 +1030,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       const bool empty = mine < 0 || sum == 0.f;     // (a NaN among a row's scores is not empty: it reaches out and lse)
       const float g0 = empty ? 0.f : f0 / sum, g1 = empty ? 0.f : f1 / sum;
       const float lse2 = empty ? -INFINITY : mm * c - AttnType<T>::shift + log2f(sum);
-      const int parts = (ntiles + plan.chunk - 1) / plan.chunk;
+      const int parts = WINDOW ? plan.chunks : (ntiles + plan.chunk - 1) / plan.chunk;
       const int64_t r = token * a.Hq + head;
       if (in) {
         if (parts > 1) plan.part_lse[r * plan.chunks + chunk] = lse2;
@@ -841,7 +1107,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 }
 
 // Joins the chunks of a row: o = sum_c o_c 2^(lse_c - max) / sum_c 2^(lse_c - max), one warp per row, chunks in order.
-template <typename T, int D>
+template <typename T, int D, bool WINDOW>
 __global__ void __launch_bounds__(256)
 attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnPlan plan) {
   pdl_wait();
@@ -853,7 +1119,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
   const int lane = threadIdx.x & 31;
   if (r >= (int64_t)s.n * a.Hq) return;
   const int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
-  const int parts = (ntiles + plan.chunk - 1) / plan.chunk;
+  const int parts = WINDOW ? plan.chunks : (ntiles + plan.chunk - 1) / plan.chunk;
   if (parts <= 1) return;
   const int64_t row = (int64_t)s.first * a.Hq + r;
   const float* lse = plan.part_lse + row * plan.chunks;
@@ -1313,13 +1579,21 @@ cache_weights_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 }
 
 // Opt-in shared memory of the kernels above (once per device).
+template <typename T, int D, AttnMode MODE, AttnForm FORM>
+static cudaError_t attention_attribute(cudaError_t before) {
+  return before != cudaSuccess ? before : cudaFuncSetAttribute(tree_attention_kernel<T, D, MODE, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                               AttnCfg<D, MODE, FORM>::kSmemBytes);
+}
 template <typename T, int D>
 static cudaError_t attention_attributes_of() {
-  cudaError_t e = cudaFuncSetAttribute(tree_attention_kernel<T, D, kRowsTwo>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, kRowsTwo>::kSmemBytes);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(tree_attention_kernel<T, D, kRowsOne>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, kRowsOne>::kSmemBytes);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(tree_attention_kernel<T, D, kRowsBrief>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnCfg<D, kRowsBrief>::kSmemBytes);
+  cudaError_t e = attention_attribute<T, D, kRowsTwo, kFormPlain>(cudaSuccess);
+  e = attention_attribute<T, D, kRowsOne, kFormPlain>(e);
+  e = attention_attribute<T, D, kRowsBrief, kFormPlain>(e);
+  e = attention_attribute<T, D, kRowsTwo, kFormWindow>(e);
+  e = attention_attribute<T, D, kRowsOne, kFormWindow>(e);
+  e = attention_attribute<T, D, kRowsBrief, kFormWindow>(e);
+  e = attention_attribute<T, D, kRowsTwo, kFormPacked>(e);
+  e = attention_attribute<T, D, kRowsOne, kFormPacked>(e);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(cache_weights_kernel<T, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightCfg<D>::kSmemBytes);
   if (e == cudaSuccess)
