@@ -14,7 +14,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libatts.so")
 SOURCES = [os.path.join(CSRC, "atts.cu")]
 HEADERS = [os.path.join(CSRC, "conformal.cuh"), os.path.join(CSRC, "lmhead_lse.cuh"),
            os.path.join(CSRC, "rope_cache.cuh"), os.path.join(CSRC, "tree_attention.cuh"), os.path.join(CSRC, "norm_rope.cuh"),
-           os.path.join(CSRC, "packed_cache.cuh"),
+           os.path.join(CSRC, "packed_cache.cuh"), os.path.join(CSRC, "packed_rows.cuh"),
            os.path.join(CSRC, "attention_host.cuh"), os.path.join(ROOT, "include", "atts.h")]
 
 

@@ -3,6 +3,7 @@
 #pragma once
 #include "norm_rope.cuh"
 #include "packed_cache.cuh"
+#include "packed_rows.cuh"
 #include "rope_cache.cuh"
 #include "tree_attention.cuh"
 
@@ -132,27 +133,61 @@ static int row_tile_tokens(int G, int64_t max_tokens) {
 // start and end 9, a slot tile 1.2 (2.0 for two row tiles), a chunk's sums one per 45 KB of them, the second launch 3.
 // One row tile and more CTAs than SMs: kRowsBrief if its 8 + 3.5 a tile, two CTAs an SM, come out below that.
 // A window leaves a row tile with the tiles of the sinks, of the window before its tokens, and of the drafts, two of them cut;
-// a packed cache's tiles take as long as its codes take to expand and has no kRowsBrief (its raw tiles leave no room for two CTAs).
+// a packed cache's tiles take 1.55 and 2.4, and it has no kRowsBrief (its raw tiles leave no room for two CTAs).
 struct AttnShape {
   AttnMode mode;
+  bool few;          // packed_rows_kernel
   AttnPlan p;
 };
 constexpr int64_t kEndless = 0x7FFFFFFF;   // a window that leaves nothing out
+
+// Slot tiles of which a row tile may see something.
+static int64_t seen_tiles(int64_t max_tokens, int64_t max_len, AttnForm form, int64_t window, int64_t sinks) {
+  const int64_t tiles = (max_len + kAttnTile - 1) / kAttnTile;
+  if (!(form & 1)) return tiles;
+  const int64_t seen = (max_tokens + window + kAttnTile - 1) / kAttnTile + 2 + (sinks + kAttnTile - 1) / kAttnTile;
+  return seen < tiles ? seen : tiles;
+}
+
+// packed_rows_kernel: all rows of a sequence's key head in one CTA.  The number of chunks that makes the launch shortest by these measured
+// times (us): a CTA's start and end 1, a tile 0.57 alone on an SM and 0.66 in company (0.75 and 0.9 beyond 8 rows), the
+// join of chunks 3 and 0.05 a chunk.
+static AttnShape few_shape(int sms, int64_t num_seqs, int G, int32_t heads, int64_t max_tokens, int64_t max_len, AttnForm form, int64_t window,
+                           int64_t sinks) {
+  AttnShape r{};
+  r.few = true;
+  r.p.tpt = max_tokens < 1 ? 1 : (int)max_tokens;
+  r.p.nq = 1;
+  const int64_t tiles = seen_tiles(max_tokens, max_len, form, window, sinks), base = num_seqs * heads;
+  const bool eight = max_tokens * G <= 8;
+  double best = 0.0;
+  int64_t best_n = 1;
+  for (int64_t n = 1; n <= tiles && n <= 256 && (n == 1 || base * n <= 64 * (int64_t)sms); ++n) {
+    const int64_t ct = (tiles + n - 1) / n, k = (base * n + sms - 1) / sms;
+    if ((tiles + ct - 1) / ct != n) continue;
+    const double tile = k <= 1 ? (eight ? 0.57 : 0.75) : eight ? 0.66 : 0.9;
+    const double cost = (double)k * (1.0 + tile * (double)ct) + (n > 1 ? 3.0 + 0.05 * (double)n : 0.0);
+    if (n == 1 || cost < best) {
+      best = cost;
+      best_n = n;
+    }
+  }
+  r.p.chunk = (int)(tiles > 0 ? (tiles + best_n - 1) / best_n : 1);
+  r.p.chunks = (int)(tiles > 0 ? (tiles + r.p.chunk - 1) / r.p.chunk : 1);
+  return r;
+}
 static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads, int32_t head_dim, int64_t max_tokens, int64_t max_len,
                             AttnForm form = kFormPlain, int64_t window = kEndless, int64_t sinks = 0) {
   AttnShape r{};
   const int G = Hq / heads;
+  if ((form & 2) && max_tokens * G <= kFewMaxRows) return few_shape(sms, num_seqs, G, heads, max_tokens, max_len, form, window, sinks);
   r.p.tpt = row_tile_tokens(G, max_tokens);
   r.mode = max_tokens > r.p.tpt ? kRowsTwo : kRowsOne;
   const int64_t per = r.p.tpt * (r.mode == kRowsTwo ? 2 : 1);
   r.p.nq = (int)((max_tokens + per - 1) / per);
-  int64_t tiles = (max_len + kAttnTile - 1) / kAttnTile;
-  if (form != kFormPlain) {
-    const int64_t seen = (max_tokens + window + kAttnTile - 1) / kAttnTile + 2 + (sinks + kAttnTile - 1) / kAttnTile;
-    if (seen < tiles) tiles = seen;
-  }
+  const int64_t tiles = seen_tiles(max_tokens, max_len, form, window, sinks);
   const int64_t base = num_seqs * heads * r.p.nq;
-  const double tile = r.mode == kRowsTwo ? 2.0 : 1.2;
+  const double tile = (form & 2) ? (r.mode == kRowsTwo ? 2.4 : 1.55) : r.mode == kRowsTwo ? 2.0 : 1.2;
   const double part = (double)((max_tokens < per ? max_tokens : per) * G) * head_dim * 8 / (45 * 1024);
   double best = 0.0;
   int64_t best_n = 1;
@@ -165,7 +200,7 @@ static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads
       best_n = n;
     }
   }
-  if (form != kFormPacked && r.mode == kRowsOne && base > sms && (double)((base + 2 * sms - 1) / (2 * sms)) * (8.0 + 3.5 * (double)tiles) < best) {
+  if (!(form & 2) && r.mode == kRowsOne && base > sms && (double)((base + 2 * sms - 1) / (2 * sms)) * (8.0 + 3.5 * (double)tiles) < best) {
     r.mode = kRowsBrief;
     best_n = 1;
   }
@@ -179,6 +214,13 @@ static size_t attn_workspace(const AttnShape& s, int64_t M, int32_t Hq, int32_t 
   return round_up(rows * 4, 256) + round_up(rows * head_dim * 4, 256);
 }
 
+template <typename T, int D>
+static int launch_parts_join(const AttnArgs& a, const AttnPlan& p, unsigned num_seqs, cudaStream_t stream) {
+  const int64_t rows = (int64_t)a.max_tokens * a.Hq;
+  if (p.chunks > kJoinFewParts) return launch_pdl(attention_parts_join_kernel<T, D, 4>, dim3((unsigned)((rows + 1) / 2), num_seqs), dim3(kJoinThreads), 0, stream, a, p);
+  return launch_pdl(attention_parts_join_kernel<T, D, 1>, dim3((unsigned)((rows + 7) / 8), num_seqs), dim3(kJoinThreads), 0, stream, a, p);
+}
+
 template <typename T, int D, AttnMode MODE, AttnForm FORM>
 static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, const AttnPlan& p,
                             dim3 grid, unsigned* status, cudaStream_t stream) {
@@ -186,7 +228,17 @@ static int launch_attention(const CUtensorMap& mq, const CUtensorMap& mk, const 
   int st = launch_pdl(tree_attention_kernel<T, D, MODE, FORM>, grid, dim3(Cfg::kThreads), Cfg::kSmemBytes, stream, mq, mk, mv, a, p, status);
   if (st != ATTS_OK || p.chunks <= 1) return st;
   const int64_t rows = (int64_t)a.max_tokens * a.Hq;
-  return launch_pdl(attention_join_kernel<T, D, FORM != kFormPlain>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
+  if (FORM & 1) return launch_parts_join<T, D>(a, p, grid.z, stream);
+  return launch_pdl(attention_join_kernel<T, D>, dim3((unsigned)((rows + 7) / 8), grid.z), dim3(256), 0, stream, a, p);
+}
+
+template <typename T, int D>
+static int launch_few(const AttnArgs& a, const AttnPlan& p, dim3 grid, unsigned* status, cudaStream_t stream) {
+  const int64_t most = (int64_t)a.max_tokens * a.G;
+  const int st = most <= 8 ? launch_pdl(packed_rows_kernel<T, D, 1>, grid, dim3(kFewThreads), FewCfg<D, 1>::kSmemBytes, stream, a, p, status)
+                           : launch_pdl(packed_rows_kernel<T, D, 2>, grid, dim3(kFewThreads), FewCfg<D, 2>::kSmemBytes, stream, a, p, status);
+  if (st != ATTS_OK || p.chunks <= 1) return st;
+  return launch_parts_join<T, D>(a, p, grid.z, stream);
 }
 
 // An attention call, its cache and queries checked (a.cache is filled): the remaining checks, the cut of the work, the launches.
@@ -219,18 +271,23 @@ static int attend(AttnArgs& a, const atts_kv_cache* c, const void* q, int64_t q_
   sh.p.withhold_loads = g_withhold_loads.load(std::memory_order_relaxed);
   const int64_t gx = (int64_t)sh.p.nq * sh.p.chunks;
   if (gx > 0x7FFFFFFF || (int64_t)max_tokens * Hq > 0x7FFFFFFF) return ATTS_ERR_SHAPE;
-  CUtensorMap mq, mk, mv;
-  if (encode_queries(di, &mq, c, q, q_ts, q_hs, M, Hq, sh.p.tpt) != ATTS_OK) return ATTS_ERR_CUDA;
-  if (FORM == kFormPacked) mk = mv = mq;   // not used
-  else if (encode_cache(di, &mk, c, c->k) != ATTS_OK || encode_cache(di, &mv, c, c->v) != ATTS_OK) return ATTS_ERR_CUDA;
   const dim3 grid((unsigned)gx, (unsigned)c->heads, (unsigned)c->num_seqs);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const bool bf = c->dtype == ATTS_BF16;
+  if constexpr ((FORM & 2) != 0)
+    if (sh.few) {
+      if (c->head_dim == 128) return bf ? launch_few<__nv_bfloat16, 128>(a, sh.p, grid, di->dev_status, stream) : launch_few<__half, 128>(a, sh.p, grid, di->dev_status, stream);
+      return bf ? launch_few<__nv_bfloat16, 64>(a, sh.p, grid, di->dev_status, stream) : launch_few<__half, 64>(a, sh.p, grid, di->dev_status, stream);
+    }
+  CUtensorMap mq, mk, mv;
+  if (encode_queries(di, &mq, c, q, q_ts, q_hs, M, Hq, sh.p.tpt) != ATTS_OK) return ATTS_ERR_CUDA;
+  if (FORM & 2) mk = mv = mq;   // not used
+  else if (encode_cache(di, &mk, c, c->k) != ATTS_OK || encode_cache(di, &mv, c, c->v) != ATTS_OK) return ATTS_ERR_CUDA;
 #define ATTS_ATTEND(D, MODE)                                                                                      \
   (bf ? launch_attention<__nv_bfloat16, D, MODE, FORM>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream)         \
       : launch_attention<__half, D, MODE, FORM>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream))
   if (sh.mode == kRowsTwo) return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsTwo) : ATTS_ATTEND(64, kRowsTwo);
-  if constexpr (FORM != kFormPacked)
+  if constexpr (!(FORM & 2))
     if (sh.mode == kRowsBrief) return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsBrief) : ATTS_ATTEND(64, kRowsBrief);
   return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsOne) : ATTS_ATTEND(64, kRowsOne);
 #undef ATTS_ATTEND
@@ -321,7 +378,9 @@ static int norm_rope(NormRopeArgs& a, const void* q, int64_t q_ts, int64_t q_hs,
   a.lanes_log2 = 0;
   while (a.lanes_log2 < 4 && 16 << a.lanes_log2 < D) ++a.lanes_log2;   // two pieces of eight channels a thread
   const int64_t span = ROWS ? M : a.max_tokens;
-  a.tpb = M >= 4 * 8 * (int64_t)di->sm_count ? 4 : 1;
+  a.inv_d = 1.f / (float)D;
+  a.tpb = 1;                        // as many tokens as leave two blocks to an SM: what a block sets up is shared by more rows
+  while (a.tpb < kNormRopeMaxTokens && M >= 4 * a.tpb * (int64_t)di->sm_count) a.tpb *= 2;
   const dim3 grid((unsigned)((span + a.tpb - 1) / a.tpb), ROWS ? 1 : (unsigned)num_seqs);
   const size_t smem = sizeof(float2) * a.tpb * (size_t)pairs;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
@@ -504,7 +563,7 @@ int atts_packed_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t H
                                           int64_t max_len, int64_t window, int64_t sinks, size_t* bytes) {
   const int st = check_window(window, sinks, true, nullptr, nullptr);
   if (st != ATTS_OK) return st;
-  return attention_workspace(kFormPacked, num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, window ? window : kEndless, sinks, bytes);
+  return attention_workspace(window ? kFormPackedWindow : kFormPacked, num_seqs, M, Hq, heads, head_dim, max_tokens, max_len, window ? window : kEndless, sinks, bytes);
 }
 
 int atts_packed_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t dtype, const atts_packed_cache* cache,
@@ -521,9 +580,12 @@ int atts_packed_attention(const void* q, int64_t q_token_stride, int64_t q_head_
   st = check_queries(q, q_token_stride, q_head_stride, &c, ctx_lens, cu_tokens, pre, end, M, Hq, max_tokens, max_len, scale);
   if (st != ATTS_OK) return st;
   if ((st = check_window(window, sinks, true, pre, depth)) != ATTS_OK) return st;
-  return attend<kFormPacked>(a, &c, q, q_token_stride, q_head_stride, ctx_lens, cu_tokens, pre, end, depth, window ? window : kEndless, sinks, M,
-                             Hq, max_tokens, max_len, scale, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes,
-                             cuda_stream);
+  if (window)
+    return attend<kFormPackedWindow>(a, &c, q, q_token_stride, q_head_stride, ctx_lens, cu_tokens, pre, end, depth, window, sinks, M, Hq,
+                                     max_tokens, max_len, scale, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes,
+                                     cuda_stream);
+  return attend<kFormPacked>(a, &c, q, q_token_stride, q_head_stride, ctx_lens, cu_tokens, pre, end, nullptr, kEndless, 0, M, Hq, max_tokens,
+                             max_len, scale, out, out_token_stride, out_head_stride, lse, workspace, workspace_bytes, cuda_stream);
 }
 
 int atts_packed_append(const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,

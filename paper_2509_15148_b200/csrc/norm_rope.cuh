@@ -9,8 +9,10 @@ namespace atts {
 // A block takes `tpb` consecutive tokens: first their cosines and sines (the angle reduced in 64 bits, as in rope_append_kernel) and
 // the places of their slots, each looked up once for all heads, then the rows [query heads | key heads | value heads].
 // `lanes` neighbouring threads share a row and hold it in registers, two 16-byte pieces each, so that it is read once although
-// the sum of its squares (in fp32, by a fixed tree) has to be known before the first channel can be written.  A thread's pieces
-// are the same in every row, so the gains of both kinds are loaded once and stay in registers too.
+// the sum of its squares (in fp32, by a fixed tree) has to be known before the first channel can be written.  A group of them takes
+// one token's heads, first queries, then keys, then values, with the products of its channels' gains and cosines and sines in
+// registers: a row then costs two packed multiply-adds a pair and a scaling (with cosines from shared memory and gains by the row
+// 16,000 tokens of 40 + 8 + 8 heads of 128 took 96 us, bound by instructions).
 // ROWS: keys go to rows of their own instead of a cache, and there are no values (what a cache in 4 bits is filled from).
 // ------------------------------------------------------------------------------------------------------------------
 struct NormRopeArgs {
@@ -21,21 +23,25 @@ struct NormRopeArgs {
   const double* freqs;
   int pairs, D, Hq, Hk, M, tpb, max_tokens;
   int lanes_log2;  // threads that share a row
-  float mscale, eps;
+  float mscale, eps, inv_d;
   CacheView cache;
 };
-constexpr int kNormRopeMaxTokens = 8;   // of a block
+constexpr int kNormRopeMaxTokens = 16;   // of a block
 
+// 16 bytes of a row as four pairs of neighbouring channels in fp32.
 template <typename T>
-__device__ __forceinline__ float square_sum(const uint32_t (&w)[4]) {
-  float s = 0.f;
+__device__ __forceinline__ void unpack_piece(const uint4& x, uint64_t (&v)[4]) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float2 f = Pack<T>::unpack(w[e]);
-    s = fmaf(f.x, f.x, s);
-    s = fmaf(f.y, f.y, s);
+    v[e] = pair2(f.x, f.y);
   }
-  return s;
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack_piece(const uint64_t (&v)[4]) {
+  return make_uint4(Pack<T>::pack(low2(v[0]), high2(v[0])), Pack<T>::pack(low2(v[1]), high2(v[1])), Pack<T>::pack(low2(v[2]), high2(v[2])),
+                    Pack<T>::pack(low2(v[3]), high2(v[3])));
 }
 // Sum over the threads that share a row; every thread of the warp takes part.
 __device__ __forceinline__ float row_sum(float s, int lanes) {
@@ -44,7 +50,7 @@ __device__ __forceinline__ float row_sum(float s, int lanes) {
 }
 
 template <typename T, bool INTERLEAVED, bool WIDE, bool ROWS>
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, WIDE ? 3 : 1)
 norm_rope_kernel(const __grid_constant__ NormRopeArgs a, unsigned* __restrict__ dev_status) {
   extern __shared__ float2 rope_cs[];                 // [tpb][pairs]
   __shared__ int64_t slot_at[kNormRopeMaxTokens];     // element offset of a token's slot in the cache, -1: none
@@ -76,120 +82,145 @@ norm_rope_kernel(const __grid_constant__ NormRopeArgs a, unsigned* __restrict__ 
     const int page = cache_page(a.cache, blockIdx.y, slot, dev_status);
     slot_at[threadIdx.x] = page < 0 ? -1 : cache_offset(a.cache, page, slot);
   }
-
-  const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
-  const int pieces = a.D / 8, turned = a.pairs / 4;      // 16-byte pieces of a row, and those that are rotated
-  const int half = INTERLEAVED ? 0 : turned / 2, rest = INTERLEAVED ? 0 : turned;
-  // This thread's pieces of every row: the two halves of eight rotated pairs, or neighbours; -1: none.
-  const bool halves = lane < half;
-  const int pa = WIDE ? (halves ? lane : rest + 2 * (lane - half)) : 0, pb = halves ? lane + half : pa + 1;
-  const bool has_a = WIDE && pa < pieces, has_b = WIDE && pb < pieces;
-  uint4 gain[2][2] = {};                                  // of queries, of keys
-  if (WIDE) {
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const uint4* from = reinterpret_cast<const uint4*>(g ? a.k_gain : a.q_gain);
-      if (from && has_a) gain[g][0] = from[pa];
-      if (from && has_b) gain[g][1] = from[pb];
-    }
-  }
   __syncthreads();
 
-  const int rows = a.Hq + (ROWS ? 1 : 2) * a.Hk, stride = kRopeThreads >> a.lanes_log2;
-  for (int r0 = 0; r0 < nt * rows; r0 += stride) {        // as many turns for every thread: rows are summed by whole warps
-    const int r = r0 + (threadIdx.x >> a.lanes_log2);
-    bool live = r < nt * rows;
-    const int t = live ? r / rows : 0, h = r - t * rows;
-    const int64_t token = first + t0 + t;
-    const T* src = nullptr;
-    T* dst = nullptr;
-    int kind = 0;                                         // 0 query, 1 key, 2 value
-    if (live) {
-      if (h < a.Hq) {
-        src = reinterpret_cast<const T*>(a.q) + token * a.q_ts + h * a.q_hs;
-        dst = reinterpret_cast<T*>(a.q_out) + token * a.o_ts + h * a.o_hs;
-      } else {
-        kind = h < a.Hq + a.Hk ? 1 : 2;
-        const int hk = h - a.Hq - (kind == 2 ? a.Hk : 0);
-        src = kind == 1 ? reinterpret_cast<const T*>(a.k) + token * a.k_ts + hk * a.k_hs : reinterpret_cast<const T*>(a.v) + token * a.v_ts + hk * a.v_hs;
-        if (ROWS) {
-          dst = reinterpret_cast<T*>(a.k_out) + token * a.ko_ts + hk * a.ko_hs;
-        } else {
-          live = slot_at[t] >= 0;
-          dst = reinterpret_cast<T*>(kind == 1 ? a.cache.k : a.cache.v) + slot_at[t] + hk * a.cache.head_stride;
+  // `lanes` threads are a group; group g takes heads g / tpb, g / tpb + subs, .. of token g % tpb.
+  const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.lanes_log2;
+  const int t = group % a.tpb, sub = group / a.tpb, subs = (kRopeThreads >> a.lanes_log2) / a.tpb;
+  const bool token_in = t < nt;
+  const int64_t token = first + t0 + t, at = !ROWS && token_in ? slot_at[t] : -1;
+  const float2* cs = rope_cs + (token_in ? t * a.pairs : 0);
+  if (WIDE) {
+    const int pieces = a.D / 8, turned = a.pairs / 4;    // 16-byte pieces of a row, and those that are rotated
+    const int half = INTERLEAVED ? 0 : turned / 2, rest = INTERLEAVED ? 0 : turned;
+    // This thread's pieces of every row: the two halves of eight rotated pairs, or neighbours.
+    const bool halves = lane < half;
+    const int pa = halves ? lane : rest + 2 * (lane - half), pb = halves ? lane + half : pa + 1;
+    const bool has_a = pa < pieces, has_b = pb < pieces;
+#pragma unroll 1
+    for (int kind = 0; kind < (ROWS ? 2 : 3); ++kind) {  // queries, keys, values
+      const int heads = kind == 0 ? a.Hq : a.Hk;
+      const T* src = reinterpret_cast<const T*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v) + token * (kind == 0 ? a.q_ts : kind == 1 ? a.k_ts : a.v_ts);
+      const int64_t src_hs = kind == 0 ? a.q_hs : kind == 1 ? a.k_hs : a.v_hs, dst_hs = kind == 0 ? a.o_hs : ROWS ? a.ko_hs : a.cache.head_stride;
+      T* dst = kind == 0 ? reinterpret_cast<T*>(a.q_out) + token * a.o_ts
+               : ROWS    ? reinterpret_cast<T*>(a.k_out) + token * a.ko_ts
+                         : reinterpret_cast<T*>(kind == 1 ? a.cache.k : a.cache.v) + at;
+      const bool token_live = token_in && (kind == 0 || ROWS || at >= 0);
+      const char* gains = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
+      // (x, y) of a pair becomes f (x cx + y sx, y cy + x sy): cosines and sines with the channels' gains in them, for this
+      // token and kind of row.  Pieces that are not rotated have their gains in cx and cy.
+      uint64_t cx[4], cy[4], sx[4], sy[4];
+      bool turn_a = false, turn_b = false;
+      if (kind < 2) {
+        uint64_t ga[4], gb[4];
+        const uint64_t ones = pair2(1.f, 1.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ga[e] = gb[e] = ones;
+        if (gains && has_a) unpack_piece<T>(reinterpret_cast<const uint4*>(gains)[pa], ga);
+        if (gains && has_b) unpack_piece<T>(reinterpret_cast<const uint4*>(gains)[pb], gb);
+        turn_a = INTERLEAVED ? pa < turned : halves;
+        turn_b = INTERLEAVED ? pb < turned : halves;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          cx[e] = ga[e];
+          cy[e] = gb[e];
+          sx[e] = sy[e] = 0;
+          if (INTERLEAVED) {                             // both pieces hold pairs of their own: (c g0, c g1) and (-s g1, s g0)
+            if (turn_a) {
+              const float2 r = cs[4 * pa + e];
+              cx[e] = mul2(pair2(r.x, r.x), ga[e]);
+              sx[e] = mul2(pair2(-r.y, r.y), pair2(high2(ga[e]), low2(ga[e])));
+            }
+            if (turn_b) {
+              const float2 r = cs[4 * pb + e];
+              cy[e] = mul2(pair2(r.x, r.x), gb[e]);
+              sy[e] = mul2(pair2(-r.y, r.y), pair2(high2(gb[e]), low2(gb[e])));
+            }
+          } else if (halves) {
+            const float2 r0 = cs[8 * lane + 2 * e], r1 = cs[8 * lane + 2 * e + 1];
+            const uint64_t c = pair2(r0.x, r1.x);
+            cx[e] = mul2(c, ga[e]);
+            cy[e] = mul2(c, gb[e]);
+            sx[e] = mul2(pair2(-r0.y, -r1.y), gb[e]);
+            sy[e] = mul2(pair2(r0.y, r1.y), ga[e]);
+          }
+        }
+      }
+      constexpr int kAtOnce = 2;                         // rows of a thread whose loads are on their way together
+#pragma unroll 1
+      for (int h0 = 0; h0 < heads; h0 += kAtOnce * subs) {   // as many turns for every thread: rows are summed by whole warps
+        uint4 x[kAtOnce], y[kAtOnce];
+        bool live[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int h = h0 + u * subs + sub;
+          live[u] = token_live && h < heads;
+          x[u] = y[u] = make_uint4(0, 0, 0, 0);
+          const uint4* from = reinterpret_cast<const uint4*>(src + h * src_hs);
+          if (live[u] && has_a) x[u] = from[pa];
+          if (live[u] && has_b) y[u] = from[pb];
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          if (kind < 2) {
+            uint64_t p[4], q[4];
+            unpack_piece<T>(x[u], p);
+            unpack_piece<T>(y[u], q);
+            float f = 1.f;
+            if (gains) {
+              uint64_t sum = 0;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum = fma2(q[e], q[e], fma2(p[e], p[e], sum));
+              f = rsqrtf(row_sum(low2(sum) + high2(sum), lanes) * a.inv_d + a.eps);
+            }
+            const uint64_t ff = pair2(f, f);
+            uint64_t v[4], w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = mul2(p[e], cx[e]);
+              w[e] = mul2(q[e], cy[e]);
+              if (turn_a) v[e] = fma2(INTERLEAVED ? pair2(high2(p[e]), low2(p[e])) : q[e], sx[e], v[e]);
+              if (turn_b) w[e] = fma2(INTERLEAVED ? pair2(high2(q[e]), low2(q[e])) : p[e], sy[e], w[e]);
+              v[e] = mul2(v[e], ff);
+              w[e] = mul2(w[e], ff);
+            }
+            x[u] = pack_piece<T>(v);
+            y[u] = pack_piece<T>(w);
+          }
+          uint4* to = reinterpret_cast<uint4*>(dst + (h0 + u * subs + sub) * dst_hs);
+          if (live[u] && has_a) to[pa] = x[u];
+          if (live[u] && has_b) to[pb] = y[u];
         }
       }
     }
-    const char* gains = kind == 0 ? a.q_gain : a.k_gain;
-    const bool norm = kind < 2 && gains;
-    const float2* cs = rope_cs + t * a.pairs;
-    if (WIDE) {
-      uint4 x = make_uint4(0, 0, 0, 0), y = x;
-      if (live && has_a) x = reinterpret_cast<const uint4*>(src)[pa];
-      if (live && has_b) y = reinterpret_cast<const uint4*>(src)[pb];
-      uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
-      const float f = rsqrtf(row_sum(square_sum<T>(xw) + square_sum<T>(yw), lanes) / (float)a.D + a.eps);
-      if (live && kind < 2) {
-        const uint4 gx = kind ? gain[1][0] : gain[0][0], gy = kind ? gain[1][1] : gain[0][1];
-        const uint32_t gxw[4] = {gx.x, gx.y, gx.z, gx.w}, gyw[4] = {gy.x, gy.y, gy.z, gy.w};
-        float u[8], v[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 p = Pack<T>::unpack(xw[e]), q = Pack<T>::unpack(yw[e]), g = Pack<T>::unpack(gxw[e]), k = Pack<T>::unpack(gyw[e]);
-          u[2 * e] = norm ? p.x * f * g.x : p.x;
-          u[2 * e + 1] = norm ? p.y * f * g.y : p.y;
-          v[2 * e] = norm ? q.x * f * k.x : q.x;
-          v[2 * e + 1] = norm ? q.y * f * k.y : q.y;
-        }
-        if (INTERLEAVED) {
-          auto rotate = [&](float (&w)[8], int piece) {
-            if (piece >= turned) return;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 g = cs[4 * piece + e];
-              const float x0 = w[2 * e];
-              w[2 * e] = x0 * g.x - w[2 * e + 1] * g.y;
-              w[2 * e + 1] = w[2 * e + 1] * g.x + x0 * g.y;
-            }
-          };
-          rotate(u, pa);
-          rotate(v, pb);
-        } else if (halves) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float2 g = cs[8 * lane + e];
-            const float x0 = u[e];
-            u[e] = x0 * g.x - v[e] * g.y;
-            v[e] = v[e] * g.x + x0 * g.y;
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          xw[e] = Pack<T>::pack(u[2 * e], u[2 * e + 1]);
-          yw[e] = Pack<T>::pack(v[2 * e], v[2 * e + 1]);
-        }
-      }
-      if (live && has_a) reinterpret_cast<uint4*>(dst)[pa] = make_uint4(xw[0], xw[1], xw[2], xw[3]);
-      if (live && has_b) reinterpret_cast<uint4*>(dst)[pb] = make_uint4(yw[0], yw[1], yw[2], yw[3]);
-    } else {
+  } else {
+    for (int h0 = 0; h0 < a.Hq + (ROWS ? 1 : 2) * a.Hk; h0 += subs) {
+      const int h = h0 + sub, kind = h < a.Hq ? 0 : h < a.Hq + a.Hk ? 1 : 2, hk = h - a.Hq - (kind == 2 ? a.Hk : 0);
+      const bool live = token_in && h < a.Hq + (ROWS ? 1 : 2) * a.Hk && (kind == 0 || ROWS || at >= 0);
+      const T* src = kind == 0   ? reinterpret_cast<const T*>(a.q) + token * a.q_ts + h * a.q_hs
+                     : kind == 1 ? reinterpret_cast<const T*>(a.k) + token * a.k_ts + hk * a.k_hs
+                                 : reinterpret_cast<const T*>(a.v) + token * a.v_ts + hk * a.v_hs;
+      T* dst = kind == 0 ? reinterpret_cast<T*>(a.q_out) + token * a.o_ts + h * a.o_hs
+               : ROWS    ? reinterpret_cast<T*>(a.k_out) + token * a.ko_ts + hk * a.ko_hs
+                         : reinterpret_cast<T*>(kind == 1 ? a.cache.k : a.cache.v) + at + hk * a.cache.head_stride;
+      const T* g = reinterpret_cast<const T*>(kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr);
       float s = 0.f;
-      if (live && norm)
+      if (live && g)
         for (int i = lane; i < a.D; i += lanes) {
           const float x = Pack<T>::get(src[i]);
           s = fmaf(x, x, s);
         }
-      const float f = rsqrtf(row_sum(s, lanes) / (float)a.D + a.eps);
+      const float f = rsqrtf(row_sum(s, lanes) * a.inv_d + a.eps);
       if (!live) continue;                                // (no warp-wide step follows in this turn)
-      const T* g = reinterpret_cast<const T*>(gains);
-      auto at = [&](int i) { return norm ? Pack<T>::get(src[i]) * f * Pack<T>::get(g[i]) : Pack<T>::get(src[i]); };
+      auto value = [&](int i) { return g ? Pack<T>::get(src[i]) * f * Pack<T>::get(g[i]) : Pack<T>::get(src[i]); };
       const int pairs = kind < 2 ? a.pairs : 0;
       for (int i = lane; i < pairs; i += lanes) {
         const int i0 = INTERLEAVED ? 2 * i : i, i1 = INTERLEAVED ? 2 * i + 1 : i + a.pairs;
-        const float x = at(i0), y = at(i1);
+        const float x = value(i0), y = value(i1);
         dst[i0] = Pack<T>::put(x * cs[i].x - y * cs[i].y);
         dst[i1] = Pack<T>::put(y * cs[i].x + x * cs[i].y);
       }
-      for (int i = 2 * pairs + lane; i < a.D; i += lanes) dst[i] = norm ? Pack<T>::put(at(i)) : src[i];
+      for (int i = 2 * pairs + lane; i < a.D; i += lanes) dst[i] = g ? Pack<T>::put(value(i)) : src[i];
     }
   }
 }

@@ -23,36 +23,74 @@ __host__ __device__ constexpr int packed_eight(int D) { return 4 * D + D / 4; } 
 __device__ __forceinline__ int packed_codes(int entry, int D) { return (entry >> 3) * packed_eight(D) + (entry & 7) * (D / 2); }
 __device__ __forceinline__ int packed_scales(int entry, int D) { return (entry >> 3) * packed_eight(D) + 4 * D + (entry & 7) * (D / 32); }
 
-// Scale's byte of a group whose largest magnitude has these bits (sign cleared): max / 7 to fp16, then to three fraction bits,
-// to nearest even both times.  (The fp32 product by 1 / 7 is off by 2^-23 of itself at most, max / 7, with 11 bits of max, by 2^-15
-// from where fp16 would round the other way, unless it is an fp16 number itself: the first rounding is that of the quotient.)
-__device__ __forceinline__ uint32_t packed_scale_byte(uint32_t top) {
-  if (top >= 0x7F800000u) return 255u;
-  const uint32_t h = __half_as_ushort(__float2half_rn(fminf(__uint_as_float(top) * (1.f / 7.f), kPackedMaxScale)));
+// Scale's byte of a group whose largest magnitude is `top`: max / 7 to fp16, then to three fraction bits, to nearest even both
+// times.  (The fp32 product by 1 / 7 is off by 2^-23 of itself at most, max / 7, with 11 bits of max, by 2^-15 from where fp16 would
+// round the other way, unless it is an fp16 number itself: the first rounding is that of the quotient.)
+__device__ __forceinline__ uint32_t packed_scale_byte(float top) {
+  if (!(top < INFINITY)) return 255u;
+  const uint32_t h = __half_as_ushort(__float2half_rn(fminf(top * (1.f / 7.f), kPackedMaxScale)));
   return (h + 63u + ((h >> 7) & 1u)) >> 7;
 }
 __device__ __forceinline__ float packed_scale(uint32_t byte) { return __half2float(__ushort_as_half((unsigned short)(byte << 7))); }
 
-// The word of eight channels under their group's scale (inverse: 1 / s, 0 for no scale).  x / s to the nearest whole number, ties to
-// even: x * (1 / s) is off by 2^-20 at most, while x / s, a quotient of 11 and 4 bits, is a tie or 2^-13 away from one, so the
-// product goes to a multiple of 2^-18 first, which makes a tie a tie again.
+// The word of eight channels under their group's scale (inverse: 1 / s, 0 for no scale); |x / s| at most 15.  x / s to the nearest whole
+// number, ties to even: x * (1 / s) is off by 2^-20 at most, while x / s, a quotient of 11 and 4 bits, is a tie or 2^-13 away from one,
+// so 48 + x / s goes to a multiple of 2^-18 first, which makes a tie a tie again, and then to 1.5 * 2^23 + 8 + c, whose low bits are
+// c + 8.  The upper bits of the eight, shifted alike, are a constant that the last step takes off.
 __device__ __forceinline__ uint32_t packed_word(const float (&x)[8], float inverse) {
   uint32_t w = 0;
+  constexpr uint32_t kUpper = 0x4B400000u;
+  constexpr uint32_t kTaken = kUpper * (0x1111u + 0x11110000u);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float c = __fsub_rn(__fadd_rn(x[j] * inverse, 48.f), 48.f);
-    c = fminf(fmaxf(c, -7.f), 7.f);
-    const uint32_t whole = __float_as_uint(__fadd_rn(c, 12582920.f));   // 1.5 * 2^23 + 8: the low bits are c + 8
-    w |= (whole & 15u) << (4 * (j / 2) + 16 * (j % 2));
+  for (int j = 0; j < 8; ++j) w += __float_as_uint(__fadd_rn(fmaf(x[j], inverse, 48.f), 12582920.f - 48.f)) << (4 * (j / 2) + 16 * (j % 2));
+  return w - kTaken;
+}
+
+// (x * s) in two 16-bit halves, exact: v = 16 + n in the top four fraction bits of each half, n = c + 8, and v s - 24 s = c s.
+template <typename T>
+struct Expand;
+template <>
+struct Expand<__nv_bfloat16> {
+  static constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
+  static constexpr int kShift = 3;      // nibble 0 to the top of the fraction
+  static __device__ __forceinline__ void scale(float a, float b, uint32_t& s2, uint32_t& m2) {   // of the low and the high half
+    s2 = Pack<__nv_bfloat16>::pack(a, b);
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(m2) : "r"(s2), "r"(0xC1C0C1C0u));
   }
-  return w;
+  static __device__ __forceinline__ uint32_t fma2(uint32_t v, uint32_t s, uint32_t m) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(s), "r"(m));
+    return r;
+  }
+};
+template <>
+struct Expand<__half> {
+  static constexpr uint32_t kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;
+  static constexpr int kShift = 6;
+  static __device__ __forceinline__ void scale(float a, float b, uint32_t& s2, uint32_t& m2) {   // of the low and the high half
+    s2 = Pack<__half>::pack(a, b);
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(m2) : "r"(s2), "r"(0xCE00CE00u));
+  }
+  static __device__ __forceinline__ uint32_t fma2(uint32_t v, uint32_t s, uint32_t m) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(s), "r"(m));
+    return r;
+  }
+};
+template <typename T, int I>
+__device__ __forceinline__ uint32_t expand_pair(uint32_t word, uint32_t s2, uint32_t m2) {
+  constexpr int by = Expand<T>::kShift - 4 * I;           // channel pair I sits in bits 4 I and 16 + 4 I
+  const uint32_t v = by >= 0 ? word << (by >= 0 ? by : 0) : word >> (by < 0 ? -by : 0);
+  uint32_t x;   // (v & mask) | sixteen in one instruction: from C it becomes two, each with a constant of its own (60.6 against 54.8 us)
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(x) : "r"(v), "r"(Expand<T>::kMask), "r"(Expand<T>::kSixteen));
+  return Expand<T>::fma2(x, s2, m2);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
 // Append.  A thread takes eight channels of a key and the same of a value, four threads a group; loads of 16 bytes and stores of 4
 // are contiguous over a warp.  Bound: HBM (2 D bytes of a row in, D / 2 + D / 32 out).
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kPackThreads = 256, kPackMaxTokens = 16;
+constexpr int kPackThreads = 256, kPackMaxTokens = 32;
 
 struct PackArgs {
   const char *k, *v;
@@ -63,19 +101,14 @@ struct PackArgs {
 };
 
 template <typename T, bool WIDE>
-__device__ __forceinline__ void load_eight(const T* src, float (&x)[8]) {
+__device__ __forceinline__ void load_eight(const T* src, uint32_t (&w)[4]) {
   if (WIDE) {
-    const uint4 w = *reinterpret_cast<const uint4*>(src);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = Pack<T>::unpack(u[e]);
-      x[2 * e] = f.x;
-      x[2 * e + 1] = f.y;
-    }
+    const uint4 u = *reinterpret_cast<const uint4*>(src);
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
   } else {
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(src);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = Pack<T>::get(src[e]);
+    for (int e = 0; e < 4; ++e) w[e] = (uint32_t)p[2 * e] | ((uint32_t)p[2 * e + 1] << 16);
   }
 }
 
@@ -104,35 +137,57 @@ packed_append_kernel(const __grid_constant__ PackArgs a, unsigned* __restrict__ 
     entry_at[threadIdx.x] = slot & ((1 << a.cache.page_log2) - 1);
   }
   __syncthreads();
+  // A thread keeps its head and channels (u) and goes over tokens; a group's four threads go together.
   const int per_row = a.D / 8, per_token = a.cache.heads * per_row;
-  const int total = nt * per_token;              // a multiple of 4: a group's four threads are in it or not together
-  for (int e0 = 0; e0 < total; e0 += kPackThreads) {
-    const int e = e0 + threadIdx.x;
-    const bool in = e < total;
-    const int t = in ? e / per_token : 0, u = in ? e - t * per_token : 0;
+  const int side = min(per_token, kPackThreads), tokens = kPackThreads / side, t_first = threadIdx.x / side;
+  if (t_first >= tokens) return;
+  const unsigned quad = 0xFu << (threadIdx.x & 28);
+  for (int u = threadIdx.x - t_first * side; u < per_token; u += side) {
     const int head = u / per_row, c8 = u - head * per_row;
-    const int64_t token = first + t0 + t;
-    const bool live = in && page_at[t] >= 0;
-    float x[2][8] = {};
-    if (live) {
-      load_eight<T, WIDE>(reinterpret_cast<const T*>(a.k) + token * a.k_ts + head * a.k_hs + 8 * c8, x[0]);
-      load_eight<T, WIDE>(reinterpret_cast<const T*>(a.v) + token * a.v_ts + head * a.v_hs + 8 * c8, x[1]);
-    }
+    const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)(first + t0) * a.k_ts + head * a.k_hs + 8 * c8;
+    const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)(first + t0) * a.v_ts + head * a.v_hs + 8 * c8;
+    for (int t = t_first; t < nt; t += 2 * tokens) {     // two tokens' loads on their way together
+      uint32_t x[2][2][4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t top = 0;                          // magnitudes compare as their bits do, NaN above all
+      for (int w = 0; w < 2; ++w)
+        if (t + w * tokens < nt) {
+          load_eight<T, WIDE>(k + (t + w * tokens) * a.k_ts, x[w][0]);
+          load_eight<T, WIDE>(v + (t + w * tokens) * a.v_ts, x[w][1]);
+        }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[i][j]) & 0x7FFFFFFFu);
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-      top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-      if (!live) continue;
-      const uint32_t byte = packed_scale_byte(top);
-      const float s = packed_scale(byte);
-      uint32_t word = 0x88888888u;
-      if (byte != 255u) word = packed_word(x[i], s > 0.f ? 1.f / s : 0.f);
-      char* base = (i ? a.cache.v : a.cache.k) + page_at[t] + head * a.cache.head_stride;
-      *reinterpret_cast<uint32_t*>(base + packed_codes(entry_at[t], a.D) + 4 * c8) = word;
-      if ((c8 & 3) == 0) base[packed_scales(entry_at[t], a.D) + c8 / 4] = (char)byte;
+      for (int w = 0; w < 2; ++w) {
+        const int tt = t + w * tokens;
+        if (tt >= nt || page_at[tt] < 0) continue;       // (all four threads of a group)
+        const int codes = packed_codes(entry_at[tt], a.D) + 4 * c8, scales = packed_scales(entry_at[tt], a.D) + c8 / 4;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t tops = 0;                             // magnitudes compare as their bits do, NaN above all: two at a time
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tops = __vmaxu2(tops, x[w][i][e] & 0x7FFF7FFFu);
+          tops = __vmaxu2(tops, __shfl_xor_sync(quad, tops, 1));
+          tops = __vmaxu2(tops, __shfl_xor_sync(quad, tops, 2));
+          const uint32_t byte = packed_scale_byte(Pack<T>::unpack(max(tops & 0xFFFFu, tops >> 16)).x);
+          const float s = packed_scale(byte);
+          uint32_t word = 0x88888888u;
+          if (byte != 255u) {
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = Pack<T>::unpack(x[w][i][e]);
+              y[2 * e] = f.x;
+              y[2 * e + 1] = f.y;
+            }
+            // A scale is max / 7 to 1 / 16 of itself, so no quotient passes 7.5, unless the scale is the largest or below 2^-14.
+            if (byte < 8u || s == kPackedMaxScale)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = fminf(fmaxf(y[e], -7.f * s), 7.f * s);
+            word = packed_word(y, s > 0.f ? 1.f / s : 0.f);
+          }
+          char* base = (i ? a.cache.v : a.cache.k) + page_at[tt] + head * a.cache.head_stride;
+          *reinterpret_cast<uint32_t*>(base + codes) = word;
+          if ((c8 & 3) == 0) base[scales] = (char)byte;
+        }
+      }
     }
   }
 }
@@ -148,11 +203,9 @@ struct ReadArgs {
 
 template <typename T>
 __device__ __forceinline__ uint4 packed_values(uint32_t word, float s) {
-  uint32_t r[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r[i] = Pack<T>::pack((float)((int)((word >> (4 * i)) & 15u) - 8) * s, (float)((int)((word >> (16 + 4 * i)) & 15u) - 8) * s);
-  return make_uint4(r[0], r[1], r[2], r[3]);
+  uint32_t s2, m2;
+  Expand<T>::scale(s, s, s2, m2);
+  return make_uint4(expand_pair<T, 0>(word, s2, m2), expand_pair<T, 1>(word, s2, m2), expand_pair<T, 2>(word, s2, m2), expand_pair<T, 3>(word, s2, m2));
 }
 
 template <typename T>
@@ -175,19 +228,33 @@ packed_read_kernel(const __grid_constant__ ReadArgs a, unsigned* __restrict__ de
   }
   __syncthreads();
   const int per_row = a.D / 8, per_token = a.src.heads * per_row;
-  for (int e = threadIdx.x; e < n * per_token; e += kPackThreads) {
-    const int t = e / per_token, u = e - t * per_token;
+  const int side = min(per_token, kPackThreads), slots = kPackThreads / side, t_first = threadIdx.x / side;
+  if (t_first >= slots) return;
+  for (int u = threadIdx.x - t_first * side; u < per_token; u += side) {
     const int head = u / per_row, c8 = u - head * per_row;
-    if (from[t] < 0) continue;
-    const int entry = (s0 + t) & ((1 << a.src.page_log2) - 1);
-    const int codes = packed_codes(entry, a.D) + 4 * c8, scales = packed_scales(entry, a.D) + c8 / 4;
-    const char* k = a.src.k + from[t] + head * a.src.head_stride;
-    const char* v = a.src.v + from[t] + head * a.src.head_stride;
-    const uint32_t kw = *reinterpret_cast<const uint32_t*>(k + codes), vw = *reinterpret_cast<const uint32_t*>(v + codes);
-    const uint32_t kb = (uint8_t)k[scales], vb = (uint8_t)v[scales];
-    const int64_t at = to[t] + head * a.dst.head_stride + 8 * c8;
-    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.dst.k) + at) = packed_values<T>(kw, packed_scale(kb));
-    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.dst.v) + at) = packed_values<T>(vw, packed_scale(vb));
+    const int64_t src_head = head * a.src.head_stride, dst_at = head * a.dst.head_stride + 8 * c8;
+    for (int t = t_first; t < n; t += 2 * slots) {       // two slots' loads on their way together
+      uint32_t word[2][2], byte[2][2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int tt = t + w * slots;
+        if (tt >= n || from[tt] < 0) continue;
+        const int entry = (s0 + tt) & ((1 << a.src.page_log2) - 1);
+        const int64_t at = from[tt] + src_head;
+        const int codes = packed_codes(entry, a.D) + 4 * c8, scales = packed_scales(entry, a.D) + c8 / 4;
+        word[w][0] = *reinterpret_cast<const uint32_t*>(a.src.k + at + codes);
+        word[w][1] = *reinterpret_cast<const uint32_t*>(a.src.v + at + codes);
+        byte[w][0] = *reinterpret_cast<const uint8_t*>(a.src.k + at + scales);
+        byte[w][1] = *reinterpret_cast<const uint8_t*>(a.src.v + at + scales);
+      }
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int tt = t + w * slots;
+        if (tt >= n || from[tt] < 0) continue;
+        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.dst.k) + to[tt] + dst_at) = packed_values<T>(word[w][0], packed_scale(byte[w][0]));
+        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.dst.v) + to[tt] + dst_at) = packed_values<T>(word[w][1], packed_scale(byte[w][1]));
+      }
+    }
   }
 }
 

@@ -101,24 +101,6 @@ __device__ __forceinline__ void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint32
         "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])                            \
       : "r"(taddr)                                                                                                         \
       : "memory")
-// Two fp32 values in one 64-bit register pair: one instruction for two multiply-adds or additions.
-__device__ __forceinline__ uint64_t pair2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float low2(uint64_t x) { return __uint_as_float((uint32_t)x); }
-__device__ __forceinline__ float high2(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -160,10 +142,10 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // The cached tiles between the sinks and the first place that any of the CTA's rows sees are left out of the count of tiles
 // (WindowView), so neither time nor chunks are spent on them; at the window's edge pairs are looked at one by one, as in a tree.
 // Packed form: the cache holds 4 bits a channel (packed_cache.cuh).  Warps 0 and 2 bring codes and scales into a ring of raw tiles
-// (one bulk copy a page), four more warps (12-15) expand them into the ring that the products read, with zeros for slots that hold
+// (one bulk copy a page), eight more warps (12-19) expand them into the ring that the products read, with zeros for slots that hold
 // nothing; the expanded values are exact, so everything behind is the same arithmetic.
 enum AttnMode { kRowsTwo, kRowsOne, kRowsBrief };
-enum AttnForm { kFormPlain = 0, kFormWindow = 1, kFormPacked = 3 };   // (packed caches are attended to through a window, which may be endless)
+enum AttnForm { kFormPlain = 0, kFormWindow = 1, kFormPacked = 2, kFormPackedWindow = 3 };
 constexpr int kAttnTile = 128;          // rows of a tile, slots of a tile
 constexpr int kAttnTreeTiles = 1024;    // tiles behind the cached part that are listed; further ones are all looked at
 constexpr int kMaskRing = 4;
@@ -172,7 +154,8 @@ template <int D, AttnMode MODE, AttnForm FORM = kFormPlain>
 struct AttnCfg {
   static constexpr bool kWindow = (FORM & 1) != 0, kPacked = (FORM & 2) != 0;
   static constexpr int kStreams = MODE == kRowsBrief ? 1 : 2;
-  static constexpr int kThreads = 128 + 128 * kStreams + (kPacked ? 128 : 0);
+  static constexpr int kExpand = 8;                                  // warps that expand a packed cache's tiles
+  static constexpr int kThreads = 128 + 128 * kStreams + (kPacked ? 32 * kExpand : 0);
   static constexpr int kTmem = 256 * kStreams;                       // columns: scores (over them the probabilities), then O
   static constexpr int kTileBytes = kAttnTile * D * 2;
   static constexpr int kQBytes = (MODE == kRowsTwo ? 2 : 1) * kTileBytes;
@@ -246,6 +229,7 @@ __device__ __forceinline__ int slot_place(const AttnArgs& a, const SeqView& s, i
 struct WindowView {
   int near_first, near_all;   // the shallowest row sees places from near_first on, every row those from near_all on
   int sink_tiles, skip;
+  int full_from;              // every row sees the whole of cached tiles from this one on
   __device__ __forceinline__ int tile(int number) const { return number < sink_tiles ? number : number + skip; }
 };
 __device__ __forceinline__ WindowView window_view(const AttnArgs& a, const SeqView& s, int tok0, int ntok, int ntiles, int lane) {
@@ -269,6 +253,7 @@ __device__ __forceinline__ WindowView window_view(const AttnArgs& a, const SeqVi
   first = min(first, ntiles);
   w.sink_tiles = min((int)(((int64_t)a.sinks + kAttnTile - 1) / kAttnTile), first);
   w.skip = first - w.sink_tiles;
+  w.full_from = (max(0, w.near_all) + kAttnTile - 1) / kAttnTile;
   return w;
 }
 
@@ -301,6 +286,7 @@ __device__ __forceinline__ bool window_all(const AttnArgs& a, const WindowView& 
 
 // Flags of a tile of cached slots under a window.
 __device__ __forceinline__ uint32_t window_flags(const AttnArgs& a, const WindowView& w, int tile) {
+  if (tile >= w.full_from) return kTileFull;              // nearly all of them
   uint32_t f = 0;
 #pragma unroll
   for (int e = 0; e < kAttnTile / 32; ++e) {
@@ -376,73 +362,42 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar) : "memory");
 }
 
-// (x * s) in two 16-bit halves, exact: v = 16 + n in the top four fraction bits of each half, n = c + 8, and v s - 24 s = c s.
-template <typename T>
-struct Expand;
-template <>
-struct Expand<__nv_bfloat16> {
-  static constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
-  static constexpr int kShift = 3;      // nibble 0 to the top of the fraction
-  static __device__ __forceinline__ void scale(float s, uint32_t& s2, uint32_t& m2) {
-    s2 = Pack<__nv_bfloat16>::pack(s, s);
-    m2 = Pack<__nv_bfloat16>::pack(-24.f * s, -24.f * s);
-  }
-  static __device__ __forceinline__ uint32_t fma2(uint32_t v, uint32_t s, uint32_t m) {
-    uint32_t r;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(s), "r"(m));
-    return r;
-  }
-};
-template <>
-struct Expand<__half> {
-  static constexpr uint32_t kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;
-  static constexpr int kShift = 6;
-  static __device__ __forceinline__ void scale(float s, uint32_t& s2, uint32_t& m2) {
-    s2 = Pack<__half>::pack(s, s);
-    m2 = Pack<__half>::pack(-24.f * s, -24.f * s);
-  }
-  static __device__ __forceinline__ uint32_t fma2(uint32_t v, uint32_t s, uint32_t m) {
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(v), "r"(s), "r"(m));
-    return r;
-  }
-};
-template <typename T, int I>
-__device__ __forceinline__ uint32_t expand_pair(uint32_t word, uint32_t s2, uint32_t m2) {
-  constexpr int by = Expand<T>::kShift - 4 * I;           // channel pair I sits in bits 4 I and 16 + 4 I
-  const uint32_t v = by >= 0 ? word << (by >= 0 ? by : 0) : word >> (by < 0 ? -by : 0);
-  return Expand<T>::fma2((v & Expand<T>::kMask) | Expand<T>::kSixteen, s2, m2);
-}
-
-// A quarter of a raw tile (32 slots) by one warp into the 16-bit tile that the products read: blocks of 64 channels, a row of 128
+// A part of a raw tile (16 slots) by one warp into the 16-bit tile that the products read: blocks of 64 channels, a row of 128
 // bytes a slot, 16-byte pieces swizzled by the row.  A thread takes a group of 32 channels; groups 2 and 3 write their pieces in
 // another order than groups 0 and 1, so that eight threads that store together never share a bank.  `dead`: bit per turn, slots that
 // hold nothing (zeros, whatever lies there).
 template <typename T, int D>
-__device__ __forceinline__ void expand_rows(const uint8_t* raw, uint8_t* tile, int quarter, int lane, uint32_t dead) {
-  constexpr int kPer = D / 32, kRows = 32 / kPer;         // threads a slot, slots a turn
-  const int g = lane % kPer;
+__device__ __forceinline__ void expand_rows(uint32_t raw, uint32_t tile, int first, int lane, uint32_t dead) {
+  constexpr int kPer = D / 32, kRows = 32 / kPer, kTurns = 16 / kRows;    // threads a slot, slots a turn
+  const int g = lane % kPer, row = first + lane / kPer, r7 = row & 7;   // of the first turn; r7 is every turn's
+  const bool swap = g >= 2;
+  const uint32_t codes = raw + (uint32_t)((row >> 3) * packed_eight(D) + r7 * (D / 2) + g * 16);
+  const uint32_t scales = raw + (uint32_t)((row >> 3) * packed_eight(D) + 4 * D + r7 * (D / 32) + g);
+  uint32_t out[4];
 #pragma unroll
-  for (int it = 0; it < 32 / kRows; ++it) {
-    const int row = quarter * 32 + it * kRows + lane / kPer, r7 = row & 7;
-    const uint8_t* eight = raw + (row >> 3) * packed_eight(D);
-    uint4 w = *reinterpret_cast<const uint4*>(eight + r7 * (D / 2) + g * 16);
-    uint32_t byte = eight[4 * D + r7 * (D / 32) + g];
+  for (int i = 0; i < 4; ++i) out[i] = tile + (uint32_t)((g >> 1) * (kAttnTile * 128) + row * 128 + ((((g & 1) * 4 + (swap ? i ^ 2 : i)) ^ r7) * 16));
+  uint4 w[kTurns];
+  uint32_t byte[kTurns];
+#pragma unroll
+  for (int it = 0; it < kTurns; ++it) {                   // every load is on its way before the first store
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[it].x), "=r"(w[it].y), "=r"(w[it].z), "=r"(w[it].w)
+                 : "r"(codes + it * (kRows / 8) * packed_eight(D)));
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(byte[it]) : "r"(scales + it * (kRows / 8) * packed_eight(D)));
+  }
+#pragma unroll
+  for (int it = 0; it < kTurns; ++it) {
     if ((dead >> it) & 1u) {
-      w = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
-      byte = 0;
+      w[it] = make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
+      byte[it] = 0;
     }
     uint32_t s2, m2;
-    Expand<T>::scale(packed_scale(byte), s2, m2);
-    const bool swap = g >= 2;
-    const uint32_t word[4] = {swap ? w.z : w.x, swap ? w.w : w.y, swap ? w.x : w.z, swap ? w.y : w.w};
-    uint8_t* out = tile + (g >> 1) * (kAttnTile * 128) + row * 128;
+    const float sc = packed_scale(byte[it]);
+    Expand<T>::scale(sc, sc, s2, m2);
+    const uint32_t word[4] = {swap ? w[it].z : w[it].x, swap ? w[it].w : w[it].y, swap ? w[it].x : w[it].z, swap ? w[it].y : w[it].w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int piece = (g & 1) * 4 + (swap ? i ^ 2 : i);
-      *reinterpret_cast<uint4*>(out + ((piece ^ r7) * 16)) = make_uint4(expand_pair<T, 0>(word[i], s2, m2), expand_pair<T, 1>(word[i], s2, m2),
-                                                                     expand_pair<T, 2>(word[i], s2, m2), expand_pair<T, 3>(word[i], s2, m2));
-    }
+    for (int i = 0; i < 4; ++i)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(out[i] + it * kRows * 128), "r"(expand_pair<T, 0>(word[i], s2, m2)),
+                   "r"(expand_pair<T, 1>(word[i], s2, m2)), "r"(expand_pair<T, 2>(word[i], s2, m2)), "r"(expand_pair<T, 3>(word[i], s2, m2)) : "memory");
   }
 }
 
@@ -524,13 +479,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       prefetch_tmap(&map_v);
     }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(full_bar(i), PACKED ? 4 : 1);     // the copies, or the warps that expand
+      mbar_init(full_bar(i), PACKED ? Cfg::kExpand : 1);     // the copies, or the warps that expand
       mbar_init(empty_bar(i), PACKED ? 1 : 2);    // the products that read the stage, and warp 3
       mbar_init(clean_bar(i), 1);
     }
     for (int i = 0; i < Cfg::kRawStages; ++i) {
       mbar_init(raw_full(i), 1);
-      mbar_init(raw_empty(i), 4);
+      mbar_init(raw_empty(i), Cfg::kExpand);
     }
     mbar_init(q_bar, 1);
     mbar_init(join_bar, 4);
@@ -613,8 +568,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 
   pdl_launch_dependents();
 
-  // A row's 128 scores stay in registers: 224 (200) for the rows' warps and 56 for the others, 384 x 168 (256 x 128, packed
-  // form: 512 x 128) in all as launched.
+  // A row's 128 scores stay in registers: 224 (200) for the rows' warps and 56 for the others, 384 x 168 (256 x 128) in all as
+  // launched; packed form 168, 56 and 40 for those that expand, of 640 x 96.
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0 || warp == 2) {
@@ -846,9 +801,9 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     }
   } else if (PACKED && warp >= 4 + 4 * kStreams) {
     // ---------------- raw tiles are expanded, in the rings' order ----------------
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if constexpr (PACKED) {
-      const int quarter = warp & 3;
+      const int first = 16 * (warp - 4 - 4 * kStreams);     // of this warp's slots in a tile
       int pos = 0;
       bool ok = true;
       auto expand = [&](int i) {
@@ -859,10 +814,10 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const int t = tile_of(i, f);
         if (f & kTileDead) {
           constexpr int kRows = 32 / (D / 32);
-          for (int it = 0; it < 32 / kRows; ++it)
-            dead |= (slot_interval(a, s, t * kAttnTile + quarter * 32 + it * kRows + lane / (D / 32)).y == 0 ? 1u : 0u) << it;
+          for (int it = 0; it < 16 / kRows; ++it)
+            dead |= (slot_interval(a, s, t * kAttnTile + first + it * kRows + lane / (D / 32)).y == 0 ? 1u : 0u) << it;
         }
-        expand_rows<T, D>(smem + Cfg::kRaw + from * Cfg::kRawBytes, smem + Cfg::kRing + to * Cfg::kTileBytes, quarter, lane, dead);
+        expand_rows<T, D>(smem_base + Cfg::kRaw + (uint32_t)(from * Cfg::kRawBytes), smem_base + Cfg::kRing + (uint32_t)(to * Cfg::kTileBytes), first, lane, dead);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
@@ -879,7 +834,8 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     }
   } else {
     // ---------------- rows ----------------
-    if (MODE == kRowsBrief || PACKED) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    if (PACKED) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    else if (MODE == kRowsBrief) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     {
       const int qmin = range[0], qmax = range[1];    // all rows padding: qmax is -1 and no tile is visible
@@ -1107,7 +1063,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
 }
 
 // Joins the chunks of a row: o = sum_c o_c 2^(lse_c - max) / sum_c 2^(lse_c - max), one warp per row, chunks in order.
-template <typename T, int D, bool WINDOW>
+template <typename T, int D>
 __global__ void __launch_bounds__(256)
 attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnPlan plan) {
   pdl_wait();
@@ -1119,7 +1075,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
   const int lane = threadIdx.x & 31;
   if (r >= (int64_t)s.n * a.Hq) return;
   const int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
-  const int parts = WINDOW ? plan.chunks : (ntiles + plan.chunk - 1) / plan.chunk;
+  const int parts = (ntiles + plan.chunk - 1) / plan.chunk;
   if (parts <= 1) return;
   const int64_t row = (int64_t)s.first * a.Hq + r;
   const float* lse = plan.part_lse + row * plan.chunks;
@@ -1145,6 +1101,65 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
   uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + token * a.o_ts + (int64_t)head * a.o_hs + lane * E);
 #pragma unroll
   for (int e = 0; e < E; e += 2) out[e / 2] = Pack<T>::pack(o[e] * inv, o[e + 1] * inv);
+  if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+// The same where every chunk of every row has written its part (a part with lse = -inf no sums): windowed and packed forms.  WARPS
+// a row, each with its share of the parts and four of them on their way.  Many parts take four: one warp that goes over 33 of them one
+// by one takes 11 us.  A few take one: with four, 15,000 rows of two parts are four times the blocks, 25 us instead of 5.
+constexpr int kJoinThreads = 256, kJoinFewParts = 8;
+template <typename T, int D, int WARPS>
+__global__ void __launch_bounds__(kJoinThreads)
+attention_parts_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AttnPlan plan) {
+  constexpr int kRows = kJoinThreads / 32 / WARPS;
+  __shared__ float sums[kRows][WARPS][D];
+  pdl_wait();
+  SeqView s;
+  unsigned none;
+  if (!seq_view(a.cu, a.ctx, blockIdx.y, a.M, a.max_tokens, a.max_len, s, &none, false)) return;
+  const int which = threadIdx.x / (32 * WARPS), warp = threadIdx.x / 32 % WARPS, lane = threadIdx.x & 31;
+  const int64_t r = (int64_t)blockIdx.x * kRows + which, row = (int64_t)s.first * a.Hq + r;
+  if (r - which >= (int64_t)s.n * a.Hq) return;                       // none of the block's rows exists
+  const bool in = r < (int64_t)s.n * a.Hq;
+  constexpr int E = D / 32;
+  float o[E] = {}, top = -INFINITY, sum = 0.f;
+  if (in) {
+    const float* lse = plan.part_lse + row * plan.chunks;
+    for (int i = lane; i < plan.chunks; i += 32) top = fmaxf(top, lse[i]);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+    for (int i = lane; i < plan.chunks; i += 32) sum += lse[i] == -INFINITY ? 0.f : ex2_approx(lse[i] - top);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+#pragma unroll 4
+    for (int i = warp; i < plan.chunks; i += WARPS) {
+      const float w = lse[i] == -INFINITY ? 0.f : ex2_approx(lse[i] - top);
+      const float* p = plan.part_o + (row * plan.chunks + i) * D + lane * E;
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = p[e];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += w == 0.f ? 0.f : w * v[e];   // (an empty part's sums are not there)
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[which][warp][lane * E + e] = o[e];
+  }
+  __syncthreads();
+  if (!in || warp != 0) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;    // (NaN stays NaN)
+  const int64_t token = row / a.Hq;
+  const int head = (int)(row - token * a.Hq);
+  uint32_t* out = reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(a.out) + token * a.o_ts + (int64_t)head * a.o_hs + lane * E);
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    float x = 0.f, y = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      x += sums[which][w][lane * E + e];
+      y += sums[which][w][lane * E + e + 1];
+    }
+    out[e / 2] = Pack<T>::pack(x * inv, y * inv);
+  }
   if (a.lse && lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
@@ -1594,6 +1609,8 @@ static cudaError_t attention_attributes_of() {
   e = attention_attribute<T, D, kRowsBrief, kFormWindow>(e);
   e = attention_attribute<T, D, kRowsTwo, kFormPacked>(e);
   e = attention_attribute<T, D, kRowsOne, kFormPacked>(e);
+  e = attention_attribute<T, D, kRowsTwo, kFormPackedWindow>(e);
+  e = attention_attribute<T, D, kRowsOne, kFormPackedWindow>(e);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(cache_weights_kernel<T, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, WeightCfg<D>::kSmemBytes);
   if (e == cudaSuccess)

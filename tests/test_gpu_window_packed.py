@@ -306,6 +306,26 @@ def test_packed_over_longer_caches_through_a_window(case, window, sinks):
     run(*case, window=window, sinks=sinks, packed=True)
 
 
+FEW = [  # numbers of rows at and around what a form for few rows takes
+    ([1, 0, 1], [4000, 5, 129], 8, 1, 64, 16, BF, "chain", 0.0),
+    ([2, 1], [1300, 126], 16, 2, 128, 8, FP, "random", 0.0),
+    ([3, 3], [513, 128], 6, 2, 128, 16, BF, "random", 0.0),
+    ([5], [20000], 12, 2, 64, 64, FP, "random", 0.2),
+    ([8, 2], [900, 30], 16, 4, 128, 32, BF, "random", 0.1),
+    ([11, 1, 0], [3000, 0, 7], 12, 4, 128, 128, FP, "random", 0.1),
+    ([17, 40], [700, 260], 2, 2, 64, 16, BF, "fan", 0.0),
+    ([16], [300], 32, 8, 128, 256, BF, "chain", 0.0),
+    ([65], [140], 2, 2, 128, 16, BF, "random", 0.1),
+    ([6] * 40, [100 + 9 * i for i in range(40)], 24, 4, 128, 16, FP, "random", 0.1),
+]
+
+
+@pytest.mark.parametrize("window, sinks", [(0, 0), (1, 2), (150, 4), (1000, 0)])
+@pytest.mark.parametrize("case", FEW)
+def test_packed_with_few_rows(case, window, sinks):
+    run(*case, window=window, sinks=sinks, packed=True)
+
+
 def test_packed_with_large_pages_loose_bounds_and_scattered_rows():
     b = Windowed(5, [11, 30], [5000, 700], 8, 2, 128, 512, BF, "random", 0.1, packed=True)
     want = b.dense()
