@@ -133,7 +133,7 @@ static int row_tile_tokens(int G, int64_t max_tokens) {
 // start and end 9, a slot tile 1.2 (2.0 for two row tiles), a chunk's sums one per 45 KB of them, the second launch 3.
 // One row tile and more CTAs than SMs: kRowsBrief if its 8 + 3.5 a tile, two CTAs an SM, come out below that.
 // A window leaves a row tile with the tiles of the sinks, of the window before its tokens, and of the drafts, two of them cut;
-// a packed cache's tiles take 1.55 and 2.4, and it has no kRowsBrief (its raw tiles leave no room for two CTAs).
+// a packed cache's tiles take 1.55 (1.35 for half the rows) and 2.4, and it has no kRowsBrief (its raw tiles leave no room for two CTAs).
 struct AttnShape {
   AttnMode mode;
   bool few;          // packed_rows_kernel
@@ -150,8 +150,8 @@ static int64_t seen_tiles(int64_t max_tokens, int64_t max_len, AttnForm form, in
 }
 
 // packed_rows_kernel: all rows of a sequence's key head in one CTA.  The number of chunks that makes the launch shortest by these measured
-// times (us): a CTA's start and end 1, a tile 0.57 alone on an SM and 0.66 in company (0.75 and 0.9 beyond 8 rows), the
-// join of chunks 3 and 0.05 a chunk.
+// times (us): a CTA's start and end 2, a tile 1.0 alone on an SM and 0.66 in company (1.4 and 0.9 beyond 8 rows), the join of
+// chunks 4 and 0.05 a chunk.
 static AttnShape few_shape(int sms, int64_t num_seqs, int G, int32_t heads, int64_t max_tokens, int64_t max_len, AttnForm form, int64_t window,
                            int64_t sinks) {
   AttnShape r{};
@@ -165,8 +165,8 @@ static AttnShape few_shape(int sms, int64_t num_seqs, int G, int32_t heads, int6
   for (int64_t n = 1; n <= tiles && n <= 256 && (n == 1 || base * n <= 64 * (int64_t)sms); ++n) {
     const int64_t ct = (tiles + n - 1) / n, k = (base * n + sms - 1) / sms;
     if ((tiles + ct - 1) / ct != n) continue;
-    const double tile = k <= 1 ? (eight ? 0.57 : 0.75) : eight ? 0.66 : 0.9;
-    const double cost = (double)k * (1.0 + tile * (double)ct) + (n > 1 ? 3.0 + 0.05 * (double)n : 0.0);
+    const double tile = k <= 1 ? (eight ? 1.0 : 1.4) : eight ? 0.66 : 0.9;
+    const double cost = (double)k * (2.0 + tile * (double)ct) + (n > 1 ? 4.0 + 0.05 * (double)n : 0.0);
     if (n == 1 || cost < best) {
       best = cost;
       best_n = n;
@@ -182,12 +182,12 @@ static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads
   const int G = Hq / heads;
   if ((form & 2) && max_tokens * G <= kFewMaxRows) return few_shape(sms, num_seqs, G, heads, max_tokens, max_len, form, window, sinks);
   r.p.tpt = row_tile_tokens(G, max_tokens);
-  r.mode = max_tokens > r.p.tpt ? kRowsTwo : kRowsOne;
+  r.mode = max_tokens > r.p.tpt ? kRowsTwo : form != kFormPlain && max_tokens * G <= 64 ? kRowsHalf : kRowsOne;
   const int64_t per = r.p.tpt * (r.mode == kRowsTwo ? 2 : 1);
   r.p.nq = (int)((max_tokens + per - 1) / per);
   const int64_t tiles = seen_tiles(max_tokens, max_len, form, window, sinks);
   const int64_t base = num_seqs * heads * r.p.nq;
-  const double tile = (form & 2) ? (r.mode == kRowsTwo ? 2.4 : 1.55) : r.mode == kRowsTwo ? 2.0 : 1.2;
+  const double tile = (form & 2) ? (r.mode == kRowsTwo ? 2.4 : r.mode == kRowsHalf ? 1.35 : 1.55) : r.mode == kRowsTwo ? 2.0 : 1.2;
   const double part = (double)((max_tokens < per ? max_tokens : per) * G) * head_dim * 8 / (45 * 1024);
   double best = 0.0;
   int64_t best_n = 1;
@@ -200,7 +200,7 @@ static AttnShape attn_shape(int sms, int64_t num_seqs, int32_t Hq, int32_t heads
       best_n = n;
     }
   }
-  if (!(form & 2) && r.mode == kRowsOne && base > sms && (double)((base + 2 * sms - 1) / (2 * sms)) * (8.0 + 3.5 * (double)tiles) < best) {
+  if (!(form & 2) && r.mode != kRowsTwo && base > sms && (double)((base + 2 * sms - 1) / (2 * sms)) * (8.0 + 3.5 * (double)tiles) < best) {
     r.mode = kRowsBrief;
     best_n = 1;
   }
@@ -287,6 +287,8 @@ static int attend(AttnArgs& a, const atts_kv_cache* c, const void* q, int64_t q_
   (bf ? launch_attention<__nv_bfloat16, D, MODE, FORM>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream)         \
       : launch_attention<__half, D, MODE, FORM>(mq, mk, mv, a, sh.p, grid, di->dev_status, stream))
   if (sh.mode == kRowsTwo) return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsTwo) : ATTS_ATTEND(64, kRowsTwo);
+  if constexpr (FORM != kFormPlain)
+    if (sh.mode == kRowsHalf) return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsHalf) : ATTS_ATTEND(64, kRowsHalf);
   if constexpr (!(FORM & 2))
     if (sh.mode == kRowsBrief) return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsBrief) : ATTS_ATTEND(64, kRowsBrief);
   return c->head_dim == 128 ? ATTS_ATTEND(128, kRowsOne) : ATTS_ATTEND(64, kRowsOne);

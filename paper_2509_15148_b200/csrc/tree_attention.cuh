@@ -144,7 +144,11 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // Packed form: the cache holds 4 bits a channel (packed_cache.cuh).  Warps 0 and 2 bring codes and scales into a ring of raw tiles
 // (one bulk copy a page), eight more warps (12-19) expand them into the ring that the products read, with zeros for slots that hold
 // nothing; the expanded values are exact, so everything behind is the same arithmetic.
-enum AttnMode { kRowsTwo, kRowsOne, kRowsBrief };
+// At most 64 rows (windowed and packed forms): kRowsHalf is kRowsOne with every row there twice, in the upper and in the lower half of the
+// row tile.  The upper one takes the first 64 slots of each tile and the lower one the others (zeros for the rest in the products with
+// V), each with maxima and sums of its own, so that a tile's chain of maximum and exponentials is half as long and all four
+// schedulers work on it, where otherwise the warps of the lower half had no rows; the halves are joined with the streams at the end.
+enum AttnMode { kRowsTwo, kRowsOne, kRowsBrief, kRowsHalf };
 enum AttnForm { kFormPlain = 0, kFormWindow = 1, kFormPacked = 2, kFormPackedWindow = 3 };
 constexpr int kAttnTile = 128;          // rows of a tile, slots of a tile
 constexpr int kAttnTreeTiles = 1024;    // tiles behind the cached part that are listed; further ones are all looked at
@@ -160,7 +164,7 @@ struct AttnCfg {
   static constexpr int kTileBytes = kAttnTile * D * 2;
   static constexpr int kQBytes = (MODE == kRowsTwo ? 2 : 1) * kTileBytes;
   static constexpr int kStages = kPacked ? (D == 128 ? (MODE == kRowsTwo ? 3 : 4) : 6)
-                                 : D == 128 ? (MODE == kRowsTwo ? 4 : MODE == kRowsOne ? 5 : 2) : MODE == kRowsBrief ? 4 : 8;
+                                 : D == 128 ? (MODE == kRowsTwo ? 4 : MODE == kRowsBrief ? 2 : 5) : MODE == kRowsBrief ? 4 : 8;
   static constexpr int kRawStages = !kPacked ? 0 : D == 128 ? (MODE == kRowsTwo ? 4 : 6) : 8;
   static constexpr int kRawBytes = kAttnTile / 8 * packed_eight(D);
   static constexpr int kRing = kQBytes;                              // byte offsets in (aligned) shared memory
@@ -168,12 +172,13 @@ struct AttnCfg {
   static constexpr int kPlaces = kMask + kMaskRing * kAttnTile * 8;  // [kMaskRing][128] int, windowed forms
   static constexpr int kRaw = kPlaces + (kWindow ? kMaskRing * kAttnTile * 4 : 0);   // [kRawStages] raw tiles, packed form
   static constexpr int kList = kRaw + kRawStages * kRawBytes;        // [kAttnTreeTiles] uint32
-  static constexpr int kStats = kList + kAttnTreeTiles * 4;          // [128] float2: maximum and sum of the odd stream
-  static constexpr int kBars = kStats + kAttnTile * 8;
+  static constexpr int kStats = kList + kAttnTreeTiles * 4;          // [128] float2: maximum and sum of the odd stream; kRowsHalf [3][64]
+  static constexpr int kBars = kStats + (MODE == kRowsHalf ? 192 : kAttnTile) * 8;
   static constexpr int kSmemBytes = kBars + 512 + 1024;
-  static constexpr int kLead = MODE == kRowsOne ? 2 : 1;             // key tiles loaded ahead of the first value tile
+  static constexpr int kLead = MODE == kRowsOne || MODE == kRowsHalf ? 2 : 1;             // key tiles loaded ahead of the first value tile
   static_assert(kSmemBytes <= 232448, "shared memory of one SM");
   static_assert(MODE != kRowsBrief || 2 * (kSmemBytes + 1024) <= 233472, "two CTAs share an SM");
+  static_assert(MODE != kRowsHalf || kStages * kTileBytes >= 192 * (D + 4) * 4, "the other sums of a row are joined through the ring");
   static_assert(MODE != kRowsOne || kStages * kTileBytes >= kAttnTile * (D + 4) * 4, "the odd stream's sums are joined through the ring");
 };
 
@@ -408,7 +413,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                       const __grid_constant__ AttnPlan plan, unsigned* __restrict__ dev_status) {
   using Cfg = AttnCfg<D, MODE, FORM>;
   constexpr bool WINDOW = Cfg::kWindow, PACKED = Cfg::kPacked;
-  constexpr bool TWO = MODE != kRowsOne;                // a stream's rows are its own, and it takes every tile
+  constexpr bool HALF = MODE == kRowsHalf, TWO = MODE != kRowsOne && !HALF;   // TWO: a stream's rows are its own, and it takes every tile
   constexpr int kStreams = Cfg::kStreams;
   constexpr uint32_t kO = 128u * kStreams;              // first column of O
   constexpr int kStages = Cfg::kStages;
@@ -488,7 +493,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       mbar_init(raw_empty(i), Cfg::kExpand);
     }
     mbar_init(q_bar, 1);
-    mbar_init(join_bar, 4);
+    mbar_init(join_bar, HALF ? 6 : 4);
     mbar_init(flag_bar, 4 * kStreams);
     mbar_init(list_bar, 1);
     for (int i = 0; i < 2; ++i) {
@@ -596,11 +601,11 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const bool value = warp == 2;
         int e0 = look_up(0);                                    // entries of the next two tiles
         if (!value && lane == 0 && has(0, true)) {              // nothing is loaded that nothing waits for
-          mbar_expect_tx(q_bar, (uint32_t)((two ? 2 : 1) * a.G * plan.tpt * D * 2));
-          for (int i = 0; i < (two ? 2 : 1); ++i)
+          mbar_expect_tx(q_bar, (uint32_t)((two || HALF ? 2 : 1) * a.G * plan.tpt * D * 2));
+          for (int i = 0; i < (two || HALF ? 2 : 1); ++i)
             for (int c = 0; c < D / 64; ++c)
-              tma_load_3d(smem_base + (uint32_t)i * Cfg::kTileBytes + (uint32_t)c * (kAttnTile * 128), &map_q, q_bar, c * 64, hk * a.G,
-                          s.first + tok0 + i * plan.tpt);
+              tma_load_3d(smem_base + (uint32_t)i * (HALF ? 64 * 128 : Cfg::kTileBytes) + (uint32_t)c * (kAttnTile * 128), &map_q, q_bar, c * 64, hk * a.G,
+                          s.first + tok0 + (HALF ? 0 : i * plan.tpt));
         }
         __syncwarp();
         int e1 = look_up(1);
@@ -851,11 +856,13 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     const int row = quarter * 32 + lane;
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
     const uint32_t t_s = tmem_base + lane_base + (uint32_t)st * kAttnTile, t_o = tmem_base + lane_base + kO + (uint32_t)st * D;
-    const int tok = (TWO ? st * plan.tpt : 0) + row / a.G;           // within the CTA's tokens
-    const bool in = row < plan.tpt * a.G && tok < ntok;
+    constexpr int kCols = HALF ? 64 : 128;                           // of a tile's slots that this thread takes
+    const int own = HALF ? row & 63 : row, col0 = HALF ? row & 64 : 0;
+    const int tok = (TWO ? st * plan.tpt : 0) + own / a.G;           // within the CTA's tokens
+    const bool in = own < plan.tpt * a.G && tok < ntok;
     const bool warp_in = __any_sync(0xFFFFFFFFu, in);
     const int64_t token = (int64_t)s.first + tok0 + tok;
-    const int head = hk * a.G + row % a.G;
+    const int head = hk * a.G + own % a.G;
     const int mine = !in ? -1 : a.pre ? a.pre[token] : tok0 + tok;
     const int near = WINDOW && in ? s.ctx + draft_depth(a, s, tok0 + tok) - a.window + 1 : 0;   // first place within this row's window
     const float c = a.scale * 1.4426950408889634f;
@@ -876,15 +883,15 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       if (!ok) break;
       tc_fence_after();
       if (warp_in) {
-        uint32_t v[128];
+        uint32_t v[kCols];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) ATTS_TMEM_LD_32(t_s + 32u * j, (&v[32 * j]));
+        for (int j = 0; j < kCols / 32; ++j) ATTS_TMEM_LD_32(t_s + (uint32_t)col0 + 32u * j, (&v[32 * j]));
         tmem_ld_wait();
         if ((f & 0xFFu) != kTileFull) {
-          const int2* mk = mask + (masked % kMaskRing) * kAttnTile;
+          const int2* mk = mask + (masked % kMaskRing) * kAttnTile + col0;
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const uint32_t kind = (f >> (2 * g)) & 3u;
+          for (int g = 0; g < kCols / 32; ++g) {
+            const uint32_t kind = (f >> (2 * g + col0 / 16)) & 3u;
             if (kind == 0u) {
 #pragma unroll
               for (int j = 32 * g; j < 32 * g + 32; ++j) v[j] = 0xFF800000u;
@@ -894,7 +901,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
                 const int4 w = *reinterpret_cast<const int4*>(mk + j);
                 bool out0 = (unsigned)(mine - w.x) >= (unsigned)w.y, out1 = (unsigned)(mine - w.z) >= (unsigned)w.w;
                 if (WINDOW) {
-                  const int2 x = *reinterpret_cast<const int2*>(places + (masked % kMaskRing) * kAttnTile + j);
+                  const int2 x = *reinterpret_cast<const int2*>(places + (masked % kMaskRing) * kAttnTile + col0 + j);
                   out0 |= x.x < near && x.x >= a.sinks;
                   out1 |= x.y < near && x.y >= a.sinks;
                 }
@@ -906,7 +913,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < 128; j += 8)
+        for (int j = 0; j < kCols; j += 8)
 #pragma unroll
           for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], __uint_as_float(v[j + e]), __uint_as_float(v[j + 4 + e]));
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
@@ -927,7 +934,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         const uint64_t c2 = pair2(c, c), off2 = pair2(off, off);
         uint64_t sum2[2] = {0, 0};
 #pragma unroll
-        for (int j = 0; j < 128; j += 32) {
+        for (int j = 0; j < kCols; j += 32) {
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
@@ -936,7 +943,14 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
             sum2[(e >> 1) & 1] = add2(sum2[(e >> 1) & 1], pair2(p0, p1));
             w[e / 2] = Pack<T>::pack(p0, p1);
           }
-          ATTS_TMEM_ST_16(t_s + (uint32_t)(j / 2), w);
+          ATTS_TMEM_ST_16(t_s + (uint32_t)((col0 + j) / 2), w);
+        }
+        if (HALF) {                                    // the other half's slots are not this row's
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e] = 0u;
+          ATTS_TMEM_ST_16(t_s + (uint32_t)((64 - col0) / 2), w);
+          ATTS_TMEM_ST_16(t_s + (uint32_t)((64 - col0) / 2 + 16), w);
         }
         const uint64_t sum = add2(sum2[0], sum2[1]);
         l += low2(sum) + high2(sum);
@@ -956,7 +970,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
     // ---- join of the two streams (one row tile): the odd one hands its sums over through the ring, which is free once
     // every product has finished: this stream's last one has; the other's last but one has, and its last is waited for ----
     float2 other = make_float2(-INFINITY, 0.f);
-    const bool joined = !TWO && ntile > 1;
+    const bool joined = !TWO && !HALF && ntile > 1;
     float* pass = reinterpret_cast<float*>(smem + Cfg::kRing);
     if (joined && st == 1) {
       if (ok) ok = wait_warp(o_bar(0), (uint32_t)((ntile + 1) / 2 - 1) & 1u);
@@ -978,13 +992,52 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       ok = wait_warp(join_bar, 0);
       if (ok && warp_in) other = stats[row];
     }
-    if (ok && active && warp_in && (TWO || st == 0)) {
+    // kRowsHalf: three others (1 the lower half of this stream, 2 and 3 the halves of the odd one) hand theirs over, none of which
+    // may have seen a tile.
+    const int part = HALF ? 2 * st + (col0 >> 6) : 0;
+    float2 others[3] = {other, other, other};
+    if (HALF && part > 0) {
+      const int theirs = st == 0 ? ntile / 2 : (ntile + 1) / 2;      // the other stream's tiles
+      if (ok && theirs > 0) ok = wait_warp(o_bar(1 - st), (uint32_t)(theirs - 1) & 1u);
+      if (ok && warp_in) {
+        stats[(part - 1) * 64 + own] = done > 0 ? make_float2(m, l) : other;
+        if (done > 0)
+#pragma unroll 1
+          for (int j = 0; j < D; j += 32) {
+            uint32_t v[32];
+            ATTS_TMEM_LD_32(t_o + (uint32_t)j, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              *reinterpret_cast<uint4*>(pass + ((part - 1) * 64 + own) * (D + 4) + j + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+          }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(join_bar);
+    }
+    if (HALF && part == 0 && ok) {
+      ok = wait_warp(join_bar, 0);
+      if (ok && warp_in)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) others[i] = stats[i * 64 + own];
+    }
+    if (ok && active && warp_in && (TWO || st == 0) && part == 0) {
       // o = (O_0 f0 + O_1 f1) / (l_0 f0 + l_1 f1), fk = 2^(c (m_k - max))
-      const float mm = fmaxf(m, other.x);
+      float mm = fmaxf(m, other.x);
+      if (HALF) mm = fmaxf(m, max3(others[0].x, others[1].x, others[2].x));
       const float f0 = m == -INFINITY ? 0.f : ex2_approx((m - mm) * c), f1 = other.x == -INFINITY ? 0.f : ex2_approx((other.x - mm) * c);
-      const float sum = l * f0 + other.y * f1;
+      float sum = l * f0 + other.y * f1, fh[3] = {0.f, 0.f, 0.f};
+      if (HALF)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          fh[i] = others[i].x == -INFINITY ? 0.f : ex2_approx((others[i].x - mm) * c);
+          sum += others[i].y * fh[i];
+        }
       const bool empty = mine < 0 || sum == 0.f;     // (a NaN among a row's scores is not empty: it reaches out and lse)
       const float g0 = empty ? 0.f : f0 / sum, g1 = empty ? 0.f : f1 / sum;
+      if (HALF)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) fh[i] = empty ? 0.f : fh[i] / sum;
       const float lse2 = empty ? -INFINITY : mm * c - AttnType<T>::shift + log2f(sum);
       const int parts = WINDOW ? plan.chunks : (ntiles + plan.chunk - 1) / plan.chunk;
       const int64_t r = token * a.Hq + head;
@@ -1028,6 +1081,19 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
           for (int e = 0; e < 32; e += 4) {
             const float4 x = *reinterpret_cast<const float4*>(pass + row * (D + 4) + j + e);
             o[e] += x.x * g1; o[e + 1] += x.y * g1; o[e + 2] += x.z * g1; o[e + 3] += x.w * g1;
+          }
+        }
+        if (HALF && !empty) {
+#pragma unroll 1
+          for (int i = 0; i < 3; ++i) {
+            const float g = i == 0 ? fh[0] : i == 1 ? fh[1] : fh[2];
+            if (g == 0.f) continue;                    // (nothing was handed over where no tile was seen)
+            const float* from = pass + (i * 64 + own) * (D + 4) + j;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 x = *reinterpret_cast<const float4*>(from + e);
+              o[e] += x.x * g; o[e + 1] += x.y * g; o[e + 2] += x.z * g; o[e + 3] += x.w * g;
+            }
           }
         }
         if (parts > 1) {
@@ -1607,6 +1673,9 @@ static cudaError_t attention_attributes_of() {
   e = attention_attribute<T, D, kRowsTwo, kFormWindow>(e);
   e = attention_attribute<T, D, kRowsOne, kFormWindow>(e);
   e = attention_attribute<T, D, kRowsBrief, kFormWindow>(e);
+  e = attention_attribute<T, D, kRowsHalf, kFormWindow>(e);
+  e = attention_attribute<T, D, kRowsHalf, kFormPacked>(e);
+  e = attention_attribute<T, D, kRowsHalf, kFormPackedWindow>(e);
   e = attention_attribute<T, D, kRowsTwo, kFormPacked>(e);
   e = attention_attribute<T, D, kRowsOne, kFormPacked>(e);
   e = attention_attribute<T, D, kRowsTwo, kFormPackedWindow>(e);
