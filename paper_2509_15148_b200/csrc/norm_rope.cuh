@@ -13,6 +13,9 @@ namespace atts {
 // one token's heads, first queries, then keys, then values, with the products of its channels' gains and cosines and sines in
 // registers: a row then costs two packed multiply-adds a pair and a scaling (with cosines from shared memory and gains by the row
 // 16,000 tokens of 40 + 8 + 8 heads of 128 took 96 us, bound by instructions).
+// Bound: HBM from some thousand tokens on: 16,000 tokens of 40 + 8 + 8 heads of 128 71 us = 5.1 TB/s, 0.78 of a plain copy (rope_append_kernel
+// 67.5).  Tokens of a block, as many as leave two blocks to an SM: 16 / 8 / 4 tokens 71 / 76 / 95 us there, 16 / 4 / 1 at 1,449 tokens
+// 16.3 / 11.4 / 23.7.  Two rows' loads on their way and at most 80 registers (three blocks an SM); one row and four blocks 85 us.
 // ROWS: keys go to rows of their own instead of a cache, and there are no values (what a cache in 4 bits is filled from).
 // ------------------------------------------------------------------------------------------------------------------
 struct NormRopeArgs {

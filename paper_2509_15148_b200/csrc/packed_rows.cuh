@@ -5,22 +5,26 @@
 namespace atts {
 
 // ------------------------------------------------------------------------------------------------------------------
-// With few rows the products are small and what costs is bringing the codes in and expanding them.  tree_attention_kernel expands
-// through shared memory, because its products read both operands there, and computes 128 rows whatever their number: 4 x 13 tokens x 4
-// heads over 131,071 slots take it 588 us, more than the same slots in 16 bits.  Here a thread expands the codes in registers, in just the
-// order in which the warp-level product (16 x 8 x 16) takes its first operand, and nothing is written back:
+// At most 16 rows: the products are small, and what costs is bringing the codes in and expanding them.  tree_attention_kernel expands
+// through shared memory, because its products read both operands there, and computes 128 rows whatever their number.  Here a thread
+// expands the codes in registers, in just the order in which the warp-level product (16 x 8 x 16) takes its first operand, and
+// nothing is written back:
 //   S^T = K Q^T   16 slots x 8 rows a product: a thread's 8 bytes (D = 64) or 16 bytes of a slot's codes are the channels of its K operands;
 //                 which channels a step of the product takes is free as long as Q's operand is laid out alike (once, in shared memory).
 //   O^T += V^T P^T  pairs of neighbouring slots of one channel: the halves of two slots' words change places (two byte permutations a
 //                 pair of words), then they expand as K's do, each half under its own slot's scale.  P^T comes out of S^T's registers, two
 //                 8 x 8 transposes for 16 slots and 8 rows.
 // The warps take turns at loading: warp t % 8 brings tile t, two tiles after the one that had its place was used up, so that it hardly
-// ever waits for the others (a ninth warp that only loads leaves the others 168 registers instead of 255, and 48 rows would not fit).
-// Every warp goes over its own slots of each tile with its own maxima and sums; they are joined at the end through shared memory, and
-// over CTAs by attention_join_kernel.  The running maximum is a warp's and moves when a row passes it by 2^8, as in tree_attention_kernel;
-// so do the rounding of probabilities and everything that masks.
-// Bound: shifts and masks (two instructions a channel pair at 16 lanes a clock and scheduler: 512 cycles a tile of keys and values of
-// 128 channels) and, from 16 rows on, the products (8.2 cycles a scheduler each, 128 a tile and 8 rows).
+// ever waits for the others.  Every warp goes over its own slots of each tile (32 with up to 8 rows, where two sets of warps then take
+// turns at tiles, 56 against 59.5 us; 16 beyond, whose sums need the registers) with its own maxima and sums; they are joined at the
+// end through shared memory, and over CTAs by attention_parts_join_kernel.  The running maximum is a warp's and moves when a row
+// passes it by 2^8, as in tree_attention_kernel; so do the rounding of probabilities and everything that masks.
+// Bound: instructions.  16 slots of 128 channels are 402, of which 64 channel pairs of a shift (16 lanes a clock and scheduler), a mask
+// (16) and a multiply-add (16), and 16 products (8.2 cycles of the tensor pipe each): 804 issue slots a scheduler and tile, where
+// an SM with two CTAs takes about 1,200 cycles.  4 sequences of 20,000 to 32,768 slots, 8 key heads of 128 (17 us at HBM's rate): 8 rows
+// 47 us, 16 rows 63 (tree_attention_kernel 114 and 118, and from 24 rows on 88 to 98, where a form for 32 rows here took 105).
+// Loads placed a step ahead of their products: 60 against 49 us (more instructions, and latency is covered by the four warps of a
+// scheduler as it is); constants of the mask out of shared memory, products that the compiler may move: no difference.
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kFewWarps = 8, kFewThreads = 32 * kFewWarps, kFewMaxRows = 16;
 
@@ -56,8 +60,8 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-// Slot of row k of a product's 16: k with its neighbours of odd pairs exchanged, so that neither the keys' nor (beyond two at a time)
-// the values' loads share banks.
+// Slot of row k of a product's 16: the two of every odd pair exchanged, so that a keys' load hits every bank once and a values' load,
+// whose four slots are two rows of 64 bytes apart, each bank twice instead of four times.
 __device__ __forceinline__ int few_slot(int k) { return k ^ ((k >> 1) & 1); }
 
 template <int WORDS>

@@ -143,11 +143,15 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // (WindowView), so neither time nor chunks are spent on them; at the window's edge pairs are looked at one by one, as in a tree.
 // Packed form: the cache holds 4 bits a channel (packed_cache.cuh).  Warps 0 and 2 bring codes and scales into a ring of raw tiles
 // (one bulk copy a page), eight more warps (12-19) expand them into the ring that the products read, with zeros for slots that hold
-// nothing; the expanded values are exact, so everything behind is the same arithmetic.
+// nothing; the expanded values are exact, so everything behind is the same arithmetic.  A warp takes about 1,400 cycles to expand 32
+// slots of a tile beside the rows' warps (shifts, masks and multiply-adds at half rate): with four of them expanding set the pace
+// (16 trees of up to 24 tokens over 1500 to 2500 slots 67 us, 8 drafts of 500 over 1013 256; with eight 39 and 192, in 16 bits 38
+// and 165).  What is left against 16 bits is the expanded tiles' way through shared memory and registers: 168 a row instead of 224.
 // At most 64 rows (windowed and packed forms): kRowsHalf is kRowsOne with every row there twice, in the upper and in the lower half of the
 // row tile.  The upper one takes the first 64 slots of each tile and the lower one the others (zeros for the rest in the products with
 // V), each with maxima and sums of its own, so that a tile's chain of maximum and exponentials is half as long and all four
 // schedulers work on it, where otherwise the warps of the lower half had no rows; the halves are joined with the streams at the end.
+// 4 x 13 tokens over 131,071 packed slots: 305 us (kRowsOne 353); one token of 8 samples through a window of 1024: 22.6 (24.2).
 enum AttnMode { kRowsTwo, kRowsOne, kRowsBrief, kRowsHalf };
 enum AttnForm { kFormPlain = 0, kFormWindow = 1, kFormPacked = 2, kFormPackedWindow = 3 };
 constexpr int kAttnTile = 128;          // rows of a tile, slots of a tile

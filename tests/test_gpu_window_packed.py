@@ -473,4 +473,67 @@ def test_norm_append_attend_and_read_back_as_a_layer_uses_them():
     assert binding.last_device_status() == 0
 
 
+def test_example_of_a_layer_whose_cache_stops_growing():
+    """examples/packed_step.py, every step against the definitions on what the cache has to hold."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "packed_step.py")
+    spec = importlib.util.spec_from_file_location("packed_step", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    torch.manual_seed(3)
+    B, line = 3, 9
+    layer = ex.PackedLayer(samples=B, slots=256, pages=24, hidden=128, heads=4, kv_heads=2, head_dim=64, window=40, sinks=3)
+    parent = list(range(-1, line - 1)) + [4, line]
+    T = len(parent)
+    held = [torch.zeros(B, 256, 2, 64, dtype=torch.float64) for _ in range(2)]
+    for turn in range(16):
+        ctx = layer.lens.tolist()
+        _, q, k, v, out, lse = layer.step(torch.randn(B * T, 128, device="cuda").bfloat16(), parent * B, [T * b for b in range(B + 1)])
+        for b in range(B):
+            rows = slice(b * T, (b + 1) * T)
+            for i, x in enumerate((k, v)):
+                held[i][b, ctx[b]:ctx[b] + T] = pack_pool(x[rows][:, None].repeat(1, 8, 1, 1))[1][:, 0].cpu()
+            see = torch.from_numpy(orc.sees(parent, ctx[b], 40, 3))
+            n = see.shape[1]
+            for h in range(4):
+                kk, vv = held[0][b, :n, h // 2], held[1][b, :n, h // 2]
+                s = ((q[rows, h].double().cpu() @ kk.T) * layer.scale).masked_fill(~see, -float("inf"))
+                want = torch.softmax(s, -1) @ vv
+                assert ((out[rows, h].double().cpu() - want).abs() <= 2.0 ** -8 * (vv.abs().max() + want.abs()) + 1e-4 * vv.abs().max()).all()
+                want_lse = torch.logsumexp(s, -1)
+                assert ((lse[rows, h].double().cpu() - want_lse).abs() <= 5e-5 + 1e-5 * want_lse.abs()).all()
+        layer.lens += line
+        layer.release()
+    assert 24 - len(layer.free) <= B * 5 and binding.last_device_status() == 0
+
+
+def test_append_and_read_back_of_more_heads_than_a_block_has_threads_for():
+    """24 heads of 128 and 3 of 64: more channels a token than threads, and a number of threads that does not divide a block."""
+    for heads, D in ((24, 128), (3, 64), (40, 256)):
+        g = torch.Generator(device="cuda").manual_seed(heads)
+        k, v = (torch.randn(70, heads, D, generator=g, device="cuda").half() for _ in range(2))
+        pools = [torch.zeros(5, heads, binding.packed_block_bytes(16, D), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        cache = binding.PackedCache(*pools, i32([[4, 0, 2, 1, 3]]), 16, D)
+        binding.packed_append(k, v, cache, i32([3]), i32([0, 70]), 70)
+        back = [torch.zeros(5, 16, heads, D, dtype=FP, device="cuda") for _ in range(2)]
+        binding.packed_read(cache, i32([73]), 80, binding.PagedCache(*back, i32([[4, 0, 2, 1, 3]])))
+        for x, y in zip((k, v), back):
+            want = pack_pool(x[:, None].repeat(1, 8, 1, 1))[1][:, 0]
+            got = y[torch.tensor([4, 0, 2, 1, 3], device="cuda")].flatten(0, 1)[3:73].double()
+            assert torch.equal(got, want)
+    assert binding.last_device_status() == 0
+
+
+@pytest.mark.parametrize("rows", [4, 40, 200])
+def test_infinite_scores_and_values_reach_the_rows_that_see_them(rows):
+    """+inf among a row's scores makes its out and lse NaN, as in the attention over 16 bits, in every form that takes a packed cache."""
+    b = Windowed(5, [rows], [300], 2, 2, 64, 16, BF, "chain", 0.0, packed=True)
+    b.q[1, 0, :] = float("inf")
+    out, lse = b.call()
+    assert torch.isnan(lse[1, 0]) and torch.isnan(out[1, 0]).all()
+    assert not torch.isnan(lse[0]).any() and not torch.isnan(lse[2:]).any() and not torch.isnan(out[2:]).any()
+
+
 EPS = 1e-6
