@@ -146,7 +146,7 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // nothing; the expanded values are exact, so everything behind is the same arithmetic.  A warp takes about 1,400 cycles to expand 32
 // slots of a tile beside the rows' warps (shifts, masks and multiply-adds at half rate): with four of them expanding set the pace
 // (16 trees of up to 24 tokens over 1500 to 2500 slots 67 us, 8 drafts of 500 over 1013 256; with eight 39 and 192, in 16 bits 38
-// and 165).  What is left against 16 bits is the expanded tiles' way through shared memory and registers: 168 a row instead of 224.
+// and 165).
 // At most 64 rows (windowed and packed forms): kRowsHalf is kRowsOne with every row there twice, in the upper and in the lower half of the
 // row tile.  The upper one takes the first 64 slots of each tile and the lower one the others (zeros for the rest in the products with
 // V), each with maxima and sums of its own, so that a tile's chain of maximum and exponentials is half as long and all four
