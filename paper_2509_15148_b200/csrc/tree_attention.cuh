@@ -775,37 +775,37 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
       if constexpr (PACKED) {                        // the ring is other warps' business
         for (int i = 0; ok && has(i, false); ++i) intervals(i);
       } else {
-      int ik = 0;
-      auto pass_key = [&]() {
-        intervals(ik++);
-        ok = ok && wait_warp(full_bar(stage), phase);
-        if (ok) release();
-      };
-      while (ik < kLead && ok && has(ik, false)) pass_key();
-      for (int i = 0; ok && has(i, false); ++i) {
-        ok = wait_warp(full_bar(stage), phase);
-        if (!ok) break;
-        uint32_t f;
-        const int t = tile_of(i, f);
-        if (f & kTileDead) {
-          uint8_t* v = smem + Cfg::kRing + stage * Cfg::kTileBytes;
-          int2 iv[kAttnTile / 32];
-          tile_intervals(a, s, t, lane, iv);
+        int ik = 0;
+        auto pass_key = [&]() {
+          intervals(ik++);
+          ok = ok && wait_warp(full_bar(stage), phase);
+          if (ok) release();
+        };
+        while (ik < kLead && ok && has(ik, false)) pass_key();
+        for (int i = 0; ok && has(i, false); ++i) {
+          ok = wait_warp(full_bar(stage), phase);
+          if (!ok) break;
+          uint32_t f;
+          const int t = tile_of(i, f);
+          if (f & kTileDead) {
+            uint8_t* v = smem + Cfg::kRing + stage * Cfg::kTileBytes;
+            int2 iv[kAttnTile / 32];
+            tile_intervals(a, s, t, lane, iv);
 #pragma unroll 1
-          for (int e = 0; e < kAttnTile / 32; ++e) {
-            if (iv[e].y != 0) continue;
-            uint8_t* at = v + (e * 32 + lane) * 128;
-            for (int c = 0; c < D / 64; ++c)
+            for (int e = 0; e < kAttnTile / 32; ++e) {
+              if (iv[e].y != 0) continue;
+              uint8_t* at = v + (e * 32 + lane) * 128;
+              for (int c = 0; c < D / 64; ++c)
 #pragma unroll
-              for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(at + c * (kAttnTile * 128) + x * 16) = make_uint4(0, 0, 0, 0);
+                for (int x = 0; x < 8; ++x) *reinterpret_cast<uint4*>(at + c * (kAttnTile * 128) + x * 16) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(clean_bar(stage));
           }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(clean_bar(stage));
+          release();
+          if (has(ik, false)) pass_key();
         }
-        release();
-        if (has(ik, false)) pass_key();
-      }
       }
     }
   } else if (PACKED && warp >= 4 + 4 * kStreams) {
