@@ -96,7 +96,7 @@ packed_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ A
   int ntiles = (s.len + kAttnTile - 1) / kAttnTile;
   const WindowView win = window_view(a, s, 0, s.n, ntiles, lane);
   const int tree0 = min(s.ctx, s.len) / kAttnTile;         // first tile that is not all cached slots
-  ntiles -= win.skip;
+  ntiles = win.live ? ntiles - win.skip : 0;               // padding alone sees nothing: no page is looked up
   const int tile0 = chunk * plan.chunk, tile1 = min(ntiles, tile0 + plan.chunk);
   const int64_t row0 = (int64_t)s.first * a.Hq + hk * a.G;
   auto row_of = [&](int r) { return row0 + (int64_t)(r / a.G) * a.Hq + r % a.G; };

@@ -239,6 +239,7 @@ struct WindowView {
   int near_first, near_all;   // the shallowest row sees places from near_first on, every row those from near_all on
   int sink_tiles, skip;
   int full_from;              // every row sees the whole of cached tiles from this one on
+  bool live;                  // some row is not padding
   __device__ __forceinline__ int tile(int number) const { return number < sink_tiles ? number : number + skip; }
 };
 __device__ __forceinline__ WindowView window_view(const AttnArgs& a, const SeqView& s, int tok0, int ntok, int ntiles, int lane) {
@@ -251,8 +252,9 @@ __device__ __forceinline__ WindowView window_view(const AttnArgs& a, const SeqVi
   }
   dmin = __reduce_min_sync(0xFFFFFFFFu, dmin);
   dmax = __reduce_max_sync(0xFFFFFFFFu, dmax);
-  if (dmax < 0) dmin = dmax = 0;                          // nothing but padding
   WindowView w;
+  w.live = dmax >= 0;
+  if (!w.live) dmin = dmax = 0;
   w.near_first = s.ctx + dmin - a.window + 1;             // (at most 2^30 each: the sum fits)
   w.near_all = s.ctx + dmax - a.window + 1;
   // A drafted token's slot is never below its place, so the first places that rows see bound the slots too; but a token of a low
