@@ -280,7 +280,7 @@ packed_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ A
               const float keep = t == m[r][e] ? 1.f : ex2_approx((m[r][e] - t) * c);      // 0 for m = -inf
               m[r][e] = t;
               off[r][e] = (t == -INFINITY ? 0.f : -t * c) + AttnType<T>::shift;
-              bound[r][e] = t + 8.f / c;
+              bound[r][e] = t == -INFINITY ? t : t + 8.f / c;                              // (8 / c is inf for the smallest scales)
               l[r][e] *= keep;
 #pragma unroll
               for (int i2 = 0; i2 < D / 16; ++i2) {

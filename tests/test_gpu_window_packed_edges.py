@@ -33,3 +33,17 @@ def test_a_sequence_of_padding_alone_needs_no_page(rows, ctx, packed, window, si
     assert binding.last_device_status() == 0
     b.check(out, lse, *want)
     assert (out[n:2 * n] == 0).all() and (lse[n:2 * n] == -float("inf")).all()
+
+
+# ---- the smallest scales ----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("scale", [1e-38, 1e-40])
+@pytest.mark.parametrize("tokens, Hq, Hk", [(4, 4, 4), (4, 16, 4), (20, 8, 4), (100, 4, 4), (200, 4, 4)])
+def test_smallest_scales_weigh_all_that_is_seen_alike(tokens, Hq, Hk, scale, packed):
+    """The window's edge lies so that the first 32 slots of which token 0 sees one show the others none."""
+    B = 75 if tokens == 4 else 2
+    b = Windowed(17, [tokens] * B, [1000] * B, Hq, Hk, 64, 16, BF, "chain", 0.0, window=1000 + 1 - 159, sinks=0, packed=packed)
+    b.scale = scale
+    out, lse = b.call()
+    assert binding.last_device_status() == 0
+    b.check(out, lse, *b.dense())
