@@ -443,7 +443,7 @@ int atts_rope_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
  * head h / (Hq / heads):
  *   out[i, h] = sum_s p_s v_s,  p = softmax over the visible slots of scale * q . k_s,   lse[i, h] = log sum_s exp(...)
  * A row that sees nothing (padding, pre < 0) gets out = 0 and lse = -inf.  A NaN or +inf among the scores that a row sees makes
- * that row's out and lse NaN.
+ * that row's out and lse NaN; a score that passes fp32's range is one.
  *   q             dev  rows [M, Hq, head_dim], 16-byte aligned, strides multiples of 8 elements; Hq a multiple of the cache's
  *                      heads, at most 128 query heads per key head; head_dim 64 or 128
  *   pre, end      dev  [M] int32 (atts_tree_plan); both NULL: every sequence's drafts are one chain (causal)

@@ -1039,12 +1039,14 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
           fh[i] = others[i].x == -INFINITY ? 0.f : ex2_approx((others[i].x - mm) * c);
           sum += others[i].y * fh[i];
         }
-      const bool empty = mine < 0 || sum == 0.f;     // (a NaN among a row's scores is not empty: it reaches out and lse)
+      // A NaN among a row's scores is not empty: it reaches out and lse.  Nor is a score that the scale takes beyond fp32, which makes
+      // every exponential 0: out and lse become the NaN that +inf makes of them.
+      const bool empty = mine < 0 || (sum == 0.f && mm * c < INFINITY);
       const float g0 = empty ? 0.f : f0 / sum, g1 = empty ? 0.f : f1 / sum;
       if (HALF)
 #pragma unroll
         for (int i = 0; i < 3; ++i) fh[i] = empty ? 0.f : fh[i] / sum;
-      const float lse2 = empty ? -INFINITY : mm * c - AttnType<T>::shift + log2f(sum);
+      const float lse2 = empty ? -INFINITY : sum == 0.f ? NAN : mm * c - AttnType<T>::shift + log2f(sum);
       const int parts = WINDOW ? plan.chunks : (ntiles + plan.chunk - 1) / plan.chunk;
       const int64_t r = token * a.Hq + head;
       if (in) {

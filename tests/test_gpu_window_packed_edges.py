@@ -4,16 +4,41 @@ A call's form goes by the rows that a sequence's key head can have (drafted toke
 cache up to 8 and up to 16, in both up to 64, up to 128, more; over 16 bits also many short sequences.  ROWS has a batch of each.
 Tolerances are those of test_gpu_attention.py."""
 import pytest
+import torch
 
 from paper_2509_15148_b200 import binding
 from tests.test_gpu_attention import BF
-from tests.test_gpu_window_packed import Windowed
+from tests.test_gpu_window_packed import Windowed, pack_pool
 
 pytestmark = pytest.mark.gpu
 
 ROWS = {  # tokens of the longest sequence, Hq, Hk
     "8": (4, 4, 2), "16": (4, 8, 2), "64": (20, 4, 2), "128": (100, 2, 2), "more": (200, 4, 2),
 }
+
+
+def made(packed, change, *args, **kw):
+    """A batch whose cache `change` has altered before it is packed."""
+    b = Windowed(*args, **kw)
+    change(b)
+    if packed:
+        b.packed, b.pools = True, []
+        for name in ("k", "v"):
+            pool, value = pack_pool(getattr(b, name))
+            b.pools.append(pool)
+            setattr(b, name, value)
+        b.handle = binding.PackedCache(*b.pools, b.table, b.page, b.D)
+    return b
+
+
+def others(b, out, lse, want, hit):
+    """Rows outside `hit` (truth values [M, Hq]) are right; those in it are NaN."""
+    assert torch.isnan(lse[hit]).all() and torch.isnan(out[hit]).all()
+    fine = ~hit
+    out, lse = out.clone(), lse.clone()
+    out[hit], lse[hit] = want[0][hit].to(out.dtype), want[1][hit].float()
+    assert fine.any()
+    b.check(out, lse, *want)
 
 
 # ---- sequences of padding alone -----------------------------------------------------------------------------------------
@@ -47,3 +72,28 @@ def test_smallest_scales_weigh_all_that_is_seen_alike(tokens, Hq, Hk, scale, pac
     out, lse = b.call()
     assert binding.last_device_status() == 0
     b.check(out, lse, *b.dense())
+
+
+# ---- scores beyond fp32 -------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("ctx", [300, 20000])
+@pytest.mark.parametrize("form", ["tree", "window", "packed", "packed window"])
+@pytest.mark.parametrize("rows", ROWS)
+def test_scores_that_the_scale_takes_beyond_fp32_are_not_an_empty_row(rows, form, ctx):
+    """One query's products are 1.5e18 to 3e18 in size, of either sign, times a scale of 1e21: +inf in fp32, so out and lse are NaN as for
+    any +inf.  The other queries are zeros: every slot that they see weighs alike."""
+    n, Hq, Hk = ROWS[rows]
+
+    def change(b):
+        live = ~torch.isnan(b.k[..., 0])
+        sign = torch.randn(b.k[..., 0].shape, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").sign()
+        b.k[..., 0] = torch.where(live, 3 * sign, b.k[..., 0].float()).to(b.dtype)
+    b = made("packed" in form, change, 19, [n, 1], [ctx, 130], Hq, Hk, 64, 32, BF, "chain", 0.0, window=200 if "window" in form else 0, sinks=1)
+    b.q.zero_()
+    b.scale = 1e21
+    want = b.dense()[:2]
+    b.q[1, 1, 0] = 1e18
+    out, lse = b.attend() if form == "tree" else b.call()
+    assert binding.last_device_status() == 0
+    hit = torch.zeros(b.M, b.Hq, dtype=torch.bool, device="cuda")
+    hit[1, 1] = True
+    others(b, out, lse, want, hit)
