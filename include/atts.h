@@ -557,7 +557,9 @@ int atts_window_attention(const void* q, int64_t q_token_stride, int64_t q_head_
  *      to even); held as the byte of its five exponent and three fraction bits: byte << 7 is s in fp16 (208 the largest).  A group that has a
  *      NaN or an infinity gets the byte 255, which is NaN and makes every channel of the group one.
  *   c: x / s to the nearest whole number, ties to even, cut to -7 .. 7 (0 where s is 0: magnitudes below 7 * 2^-18).
- * Values up to 14,336 are held to half a scale; 4.25 bits a channel.  c * s is exact in bf16 and fp16.
+ * Channels of at most 14,336 are held to half a scale where the group's largest magnitude is 7 * 2^-14 (4.3e-4) or more.  In smaller
+ * groups, whose scales have fewer digits, every channel is held to 2^-15 (the largest may be off by 3.5 scales: 7.5e-5 is held as 5.3e-5).
+ * 4.25 bits a channel.  c * s is exact in bf16 and fp16.
  * A page of a head is a contiguous block of page_size / 8 * 4.25 * head_dim bytes (page_size / 8 pieces of
  * 4 * head_dim bytes of codes of eight slots, then head_dim / 4 bytes of their scales).  A slot has head_dim / 2 bytes of codes:
  * eight channels to a little-endian word, c + 8 of channel 2 i in bits 4 i .. and of channel 2 i + 1 in bits 16 + 4 i ..

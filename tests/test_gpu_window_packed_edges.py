@@ -3,11 +3,13 @@
 A call's form goes by the rows that a sequence's key head can have (drafted tokens times the query heads that share it): over a packed
 cache up to 8 and up to 16, in both up to 64, up to 128, more; over 16 bits also many short sequences.  ROWS has a batch of each.
 Tolerances are those of test_gpu_attention.py."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import window_packed_oracle as orc
 from paper_2509_15148_b200 import binding
-from tests.test_gpu_attention import BF
+from tests.test_gpu_attention import BF, FP, i32
 from tests.test_gpu_window_packed import Windowed, pack_pool
 
 pytestmark = pytest.mark.gpu
@@ -97,3 +99,33 @@ def test_scores_that_the_scale_takes_beyond_fp32_are_not_an_empty_row(rows, form
     hit = torch.zeros(b.M, b.Hq, dtype=torch.bool, device="cuda")
     hit[1, 1] = True
     others(b, out, lse, want, hit)
+
+
+# ---- the format ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_append_of_small_groups_is_the_format_to_the_byte(dtype):
+    """Scales below 2^-14 have fewer digits: every largest magnitude up to 7 * 2^-13 in one group or another."""
+    top = torch.arange(1 << 15, dtype=torch.int32).to(torch.int16).view(dtype)
+    top = top[(top > 0) & (top < 7 * 2.0 ** -13)]
+    top = top[-(16 * 2048):]
+    n = -(-top.numel() // 16) * 16
+    g = torch.Generator().manual_seed(3)
+    x = (2 * torch.rand(n, 32, generator=g) - 1)
+    x[: top.numel()] *= top.float()[:, None]
+    x = x.to(dtype)
+    x[torch.arange(top.numel()), torch.randint(0, 32, (top.numel(),), generator=g)] = top
+    x = x.view(n // 2, 1, 64).cuda()
+    page, slots = 256, n // 2
+    pages = -(-slots // page)
+    pools = [torch.full((pages, 1, binding.packed_block_bytes(page, 64)), 0xAA, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    binding.packed_append(x, -x, binding.PackedCache(*pools, i32(np.arange(pages)[None]), page, 64), i32([0]), i32([0, slots]), slots)
+    for new, pool in ((x, pools[0]), (-x, pools[1])):
+        full = torch.zeros(pages * page, 1, 64, dtype=dtype, device="cuda")
+        full[:slots] = new
+        want = pack_pool(full.view(pages, page, 1, 64))[0]
+        whole = slots // page
+        assert torch.equal(pool[:whole], want[:whole])
+        for s in range(whole * page, slots):
+            c0, s0 = orc.slot_bytes(s % page, 64)
+            assert torch.equal(pool[whole, 0, c0:c0 + 32], want[whole, 0, c0:c0 + 32]) and torch.equal(pool[whole, 0, s0:s0 + 2], want[whole, 0, s0:s0 + 2])
+    assert binding.last_device_status() == 0
