@@ -390,7 +390,7 @@ packed_rows_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ A
       y.x += v.x * f; y.y += v.y * f; y.z += v.z * f; y.w += v.w * f;
     }
     const int tok = r / a.G;
-    const bool empty = (a.pre && a.pre[s.first + tok] < 0) || (sum == 0.f && top * c < INFINITY);   // (NaN and scores beyond fp32 are not)
+    const bool empty = (a.pre && a.pre[s.first + tok] < 0) || (sum == 0.f && top == -INFINITY);   // (NaN and scores beyond fp32 are not)
     const float g = empty ? 0.f : 1.f / sum;
     y = empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(y.x * g, y.y * g, y.z * g, y.w * g);
     const float lse2 = empty ? -INFINITY : sum == 0.f ? NAN : top * c - AttnType<T>::shift + log2f(sum);

@@ -1041,7 +1041,7 @@ tree_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_co
         }
       // A NaN among a row's scores is not empty: it reaches out and lse.  Nor is a score that the scale takes beyond fp32, which makes
       // every exponential 0: out and lse become the NaN that +inf makes of them.
-      const bool empty = mine < 0 || (sum == 0.f && mm * c < INFINITY);
+      const bool empty = mine < 0 || (sum == 0.f && mm == -INFINITY);
       const float g0 = empty ? 0.f : f0 / sum, g1 = empty ? 0.f : f1 / sum;
       if (HALF)
 #pragma unroll
