@@ -513,7 +513,8 @@ int atts_cache_gather(const atts_kv_cache* src, const int32_t* kept, int64_t kep
  * then pairs of y are turned as in atts_rope_append, and the row is rounded once.
  *   q_gain, k_gain  dev  [head_dim] in the rows' type, shared by the heads; NULL: that side is only rotated
  *   eps             finite, >= 0 (a row of zeros with eps = 0 gives NaN)
- * atts_norm_rope_append: everything else as atts_rope_append.  Mean squares are taken in fp32: magnitudes up to 1e18.
+ * Mean squares are taken in fp32: magnitudes up to 1e18, and where eps is below 1e-34 rows whose largest magnitude is 1e-17 or more.
+ * atts_norm_rope_append: everything else as atts_rope_append.
  * atts_norm_rope: rows to rows, no cache (what atts_packed_append takes): q [M, Hq, head_dim] into q_out, k [M, Hk, head_dim]
  * into k_out; either may be written in place (same strides).  Hq or Hk may be 0, its pointers then NULL.  dtype ATTS_BF16 or
  * ATTS_FP16; head_dim a multiple of 8, <= 256.
@@ -540,8 +541,9 @@ int atts_norm_rope(const void* q, int64_t q_token_stride, int64_t q_head_stride,
  *                      number of ancestors, the outputs of its sequence are undefined
  *   window        1 <= window <= 2^30;  sinks  0 <= sinks <= 2^30
  * Everything else as atts_tree_attention; the workspace is asked for with the same window and sinks.  What lies behind the
- * window costs nothing, and a page none of whose slots any drafted token of the sequence sees need not be there any more (its
- * table entry may be -1).
+ * window costs nothing, and a page of nothing but cached slots that no drafted token of the sequence sees need not be there any
+ * more (its table entry may be -1).  Pages that hold drafted tokens have to be there, those of padding too where the sequence has other
+ * tokens.  A sequence whose drafted tokens are all padding needs no page at all.
  */
 int atts_window_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,
                                           int64_t max_tokens, int64_t max_len, int64_t window, int64_t sinks, size_t* bytes);
@@ -596,8 +598,9 @@ int atts_packed_read(const atts_packed_cache* src, const int32_t* lens, int64_t 
  * Attention over a packed cache: atts_window_attention, or with window = 0 (then depth may be NULL and sinks mean nothing)
  * atts_tree_attention, on the values that the cache stands for; q and out of type dtype, head_dim 64 or 128.  Those values go to
  * the tensor cores exactly, so the arithmetic behind them is that of the calls over 16 bits.  A missing page's slots
- * read as zeros; a NaN group makes out and lse of the rows that see its key NaN, and out of all rows of its head that see its value's
- * tile (a masked product is 0 * v, as with 16 bits).
+ * read as zeros.  A NaN group of a key makes out and lse of the rows that see it NaN, one of a value its 32 channels of out of the rows that
+ * see it; other rows of that sequence and key head may get NaN in those channels too, also where their window does not hold the slot (a
+ * masked product is 0 * v, as with 16 bits, where values have to be finite).  Padding's slots are as if they were not there.
  */
 int atts_packed_attention_workspace_bytes(int64_t num_seqs, int64_t M, int32_t Hq, int32_t heads, int32_t head_dim,
                                           int64_t max_tokens, int64_t max_len, int64_t window, int64_t sinks, size_t* bytes);

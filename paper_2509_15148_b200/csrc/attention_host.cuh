@@ -381,7 +381,7 @@ static int norm_rope(NormRopeArgs& a, const void* q, int64_t q_ts, int64_t q_hs,
   while (a.lanes_log2 < 4 && 16 << a.lanes_log2 < D) ++a.lanes_log2;   // two pieces of eight channels a thread
   const int64_t span = ROWS ? M : a.max_tokens;
   a.inv_d = 1.f / (float)D;
-  a.tpb = 1;                        // as many tokens as leave two blocks to an SM: what a block sets up is shared by more rows
+  a.tpb = 1;                        // as many tokens as leave two blocks to an SM if sequences fill them: what a block sets up is shared by more rows
   while (a.tpb < kNormRopeMaxTokens && M >= 4 * a.tpb * (int64_t)di->sm_count) a.tpb *= 2;
   const dim3 grid((unsigned)((span + a.tpb - 1) / a.tpb), ROWS ? 1 : (unsigned)num_seqs);
   const size_t smem = sizeof(float2) * a.tpb * (size_t)pairs;

@@ -12,11 +12,16 @@ namespace atts {
 // the sum of its squares (in fp32, by a fixed tree) has to be known before the first channel can be written.  A group of them takes
 // one token's heads, first queries, then keys, then values, with the products of its channels' gains and cosines and sines in
 // registers: a row then costs two packed multiply-adds a pair and a scaling (with cosines from shared memory and gains by the row
-// 16,000 tokens of 40 + 8 + 8 heads of 128 took 96 us, bound by instructions).
-// Bound: HBM from some thousand tokens on: 16,000 tokens of 40 + 8 + 8 heads of 128 71 us = 5.1 TB/s, 0.78 of a plain copy (rope_append_kernel
-// 67.5).  Tokens of a block, as many as leave two blocks to an SM: 16 / 8 / 4 tokens 71 / 76 / 95 us there, 16 / 4 / 1 at 1,449 tokens
-// 16.3 / 11.4 / 23.7.  Two rows' loads on their way and at most 80 registers (three blocks an SM); one row and four blocks 85 us.
-// ROWS: keys go to rows of their own instead of a cache, and there are no values (what a cache in 4 bits is filled from).
+// 12,675 tokens of 40 + 8 + 8 heads of 128 took 96 us, bound by instructions).
+// Bound: HBM from some thousand tokens on: 12,675 tokens of 40 + 8 + 8 heads of 128 in 32 sequences 71 us = 5.1 TB/s, 0.78 of a plain copy
+// (rope_append_kernel 67.5).  Tokens of a block, as many as leave two blocks to an SM if sequences fill theirs: 16 / 8 / 4 tokens
+// 71 / 76 / 95 us there, 16 / 4 / 1 at 1,503 tokens in 23 sequences 16.3 / 11.4 / 23.7.  A block takes tokens of one sequence, and the
+// number is chosen by the batch's tokens alone: many short sequences leave most of its threads without a row (sequences of one token,
+// 600 / 2,400 / 9,600 of them: 14.7 / 77 / 460 us, where rope_append_kernel, which deals rows to all threads, takes 5.4 / 17.7 / 64).
+// Two rows' loads on their way and at most 80 registers (three blocks an SM; the append's wide forms spill 24 bytes a thread, the
+// wide one from rows to rows that is not interleaved 8); one row and four blocks 85 us.
+// ROWS: keys go to rows of their own instead of a cache, and there are no values (what a cache in 4 bits is filled from): 12,675 tokens of
+// 40 + 8 heads 60 us = 5.2 TB/s, 1,503 of 28 + 4 8.6, of 9,600 sequences of one token 52 (it knows no sequences).
 // ------------------------------------------------------------------------------------------------------------------
 struct NormRopeArgs {
   const char *q, *k, *v, *q_gain, *k_gain;   // a NULL gain: that side is not normed

@@ -88,9 +88,10 @@ __device__ __forceinline__ uint32_t expand_pair(uint32_t word, uint32_t s2, uint
 
 // ------------------------------------------------------------------------------------------------------------------
 // Append.  A thread takes eight channels of a key and the same of a value, four threads a group; loads of 16 bytes and stores of 4
-// are contiguous over a warp; it keeps its head and channels and goes over tokens, two of them on their way.  Bound: HBM (2 D bytes of
-// a row in, D / 2 + D / 32 out) and the arithmetic of the codes: 16,000 tokens of 8 heads of 128 22 us = 3.8 TB/s.  (The first form,
-// a division of indexes, a clamp and a comparison for every channel, took 50 us with the read-back, this one 36.)
+// are contiguous over a warp; it keeps its head and channels and goes over tokens, two of them on their way.  Bound: the arithmetic
+// of the codes before HBM (2 D bytes of a row in, D / 2 + D / 32 out): 12,675 tokens of 8 heads of 128 22.7 us = 2.9 TB/s, 0.44 of a plain
+// copy, with issue slots 60 % and DRAM 26 % busy.  (The first form, a division of indexes, a clamp and a comparison for every channel,
+// took 50 us with the read-back, this one 36.)
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kPackThreads = 256, kPackMaxTokens = 32;
 
@@ -196,7 +197,8 @@ packed_append_kernel(const __grid_constant__ PackArgs a, unsigned* __restrict__ 
 
 // ------------------------------------------------------------------------------------------------------------------
 // Reading back: slots [0, lens[b]) of every sequence into a cache in 16 bits.  The same shape as the append, the other way round; codes
-// expand as for the products.  Bound: HBM: 16,000 slots of 8 heads of 128 14.7 us = 5.7 TB/s, 0.87 of a plain copy.
+// expand as for the products.  Bound: latency and instructions of small accesses (a thread loads 4 bytes of codes and one of a scale at a
+// time; issue slots 52 %, ALU 43 %): 12,694 slots of 8 heads of 128 14.6 us = 4.5 TB/s, 0.69 of a plain copy.
 // ------------------------------------------------------------------------------------------------------------------
 struct ReadArgs {
   const int32_t* lens;

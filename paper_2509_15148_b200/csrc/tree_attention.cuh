@@ -123,7 +123,8 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 // exponentials (1,400 of a round's 3,750 cycles) and products keeps the tensor pipe 55 % busy and the power cap sets the clock.
 // Probabilities are rounded because the tensor pipe multiplies 16-bit operands: the output's error against 64 bits is 0.0019 of it
 // in bf16 and 0.00028 in fp16, where the output's own rounding makes 0.0017 and 0.00021; the sums are of the unrounded ones.
-// Registers: ptxas spills 8 to 24 bytes a thread, loaded again 472 to 476 bytes' worth in kRowsOne and 140 to 148 in the others.
+// Registers: ptxas spills 8 to 24 bytes a thread, loaded again 472 to 476 bytes' worth in kRowsOne and 140 to 148 in the others; windowed
+// forms 20 in kRowsHalf (loaded again 192 to 196) and none in the others; packed forms 36 to 72 (52 to 80), none in kRowsHalf.
 // The running maximum that p refers to only moves when a row exceeds it by 2^8: p <= 256, and
 // O is rescaled (a pass over tensor memory) in a few tiles instead of in every one.
 // The slots may be cut into chunks of `chunk` tiles over CTAs (few rows, long caches); the parts are then joined by

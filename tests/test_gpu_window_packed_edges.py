@@ -1,5 +1,6 @@
 """Windowed and packed attention at their edges, in every form that a call may take: sequences of padding alone, pages that are gone or
-missing, infinities and NaN, the smallest scales and scores beyond fp32, thousands of sequences; the packed cache's small groups.
+missing, infinities and NaN, the smallest scales and scores beyond fp32, thousands of sequences; the packed cache's small groups and
+the ends of the norm's range.
 
 A call's form goes by the rows that a sequence's key head can have (drafted tokens times the query heads that share it): over a packed
 cache up to 8 and up to 16, in both up to 64, up to 128, more; over 16 bits also many short sequences.  ROWS has a batch of each.
@@ -278,4 +279,27 @@ def test_append_of_small_groups_is_the_format_to_the_byte(dtype):
         for s in range(whole * page, slots):
             c0, s0 = orc.slot_bytes(s % page, 64)
             assert torch.equal(pool[whole, 0, c0:c0 + 32], want[whole, 0, c0:c0 + 32]) and torch.equal(pool[whole, 0, s0:s0 + 2], want[whole, 0, s0:s0 + 2])
+    assert binding.last_device_status() == 0
+
+
+# ---- the norm's range ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("size", [1e-17, 1e18])
+@pytest.mark.parametrize("D, pad", [(64, 0), (256, 0), (256, 3)])
+def test_norm_without_eps_at_the_ends_of_its_range(D, pad, size):
+    """Rows of one channel of that size and of all channels near it; the tolerance of test_gpu_norm_rope.py."""
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x = torch.zeros(4, 2, D + pad, dtype=BF, device="cuda")
+    x[0, :, 5], x[1] = size, size
+    x[2:] = (torch.rand(2, 2, D + pad, generator=g, device="cuda") * size).to(BF)
+    x[2:, :, 7] = size
+    x = x[..., :D]
+    gain = (1 + 0.3 * torch.randn(D, generator=g, device="cuda")).to(BF)
+    freqs, pos = binding.rope_freqs(D, 10000.0)[0], [0, 5, 77, 4000]
+    out = torch.empty(4, 2, D, dtype=BF, device="cuda")
+    binding.norm_rope(x, None, i32(pos), freqs.cuda(), gain, None, 0.0, out, None)
+    for t in range(4):
+        row = x[t].double().cpu().numpy()
+        want = orc.norm_rotate(row, gain.double().cpu().numpy(), 0.0, pos[t], freqs.numpy())
+        d = 4e-6 * np.abs(orc.norm_rotate(row, gain.double().cpu().numpy(), 0.0, 0, [])).max(-1, keepdims=True)
+        assert (np.abs(out[t].double().cpu().numpy() - want) <= d + 2.0 ** -8 * (np.abs(want) + d)).all()
     assert binding.last_device_status() == 0
